@@ -309,6 +309,64 @@ RLM_API rlm_status rlm_mixer_decode(const rlm_tensor *x_t, const rlm_tensor *g_t
                                     const rlm_local *local, const rlm_coupling *coupling, rlm_conv_state *conv,
                                     rlm_tensor *z_t, const rlm_launch *launch);
 
+/* ------------------------------------------------- gated linear recurrence
+ * A recurrence whose decay depends on the input, one state per channel:
+ *
+ *   a_t = sigma(g_t),   h_t = a_t h_{t-1} + i_t,   y_t = h_t
+ *   i_t = (1 - a_t) x_t  (leak != 0)   or   i_t = x_t  (leak == 0)
+ *
+ * Fields may be views of wider tensors (the two halves of a fused projection's
+ * output, say): element (b, t, d) lies at ptr + b*stride_b + t*stride_l + d
+ * elements.  Strides are multiples of 16 bytes (those of an extent of 1 are not
+ * read) and ptr is 16-byte aligned; the rows of an output must not overlap one
+ * another, nor any input.  State and its gradient are fp32 [B][D], contiguous.
+ *
+ * lengths (nullable): int32 [B] on the device; row b's tokens from lengths[b] on are
+ * padding (values outside 0..L are clamped): x, g and dy are not read there, y, dx and
+ * dg are 0, and the state passes through (a row of length 0 returns its initial state).
+ * Paths: one kernel per call; where B * ceil(D / 64) is small, several blocks share a
+ * sequence and exchange their tiles' runs through the workspace (a cooperative launch
+ * with bounded waits).  Sums are fp32 in an order fixed by the shape. */
+typedef struct {
+    void *ptr;
+    rlm_dtype dtype;
+    int64_t B, L, D;
+    int64_t stride_b, stride_l;
+} rlm_strided;
+
+/* Tokens between the states that a training pass keeps for its backward pass. */
+#define RLM_SCAN_CHUNK 64
+
+/* Over a sequence.
+ *   x, g       [B][L][D] drive and gate pre-activation (one dtype)
+ *   state_in   nullable, h_{-1} (zero if NULL);  state_out  nullable, h_{L-1} (may be
+ *              state_in itself)
+ *   saved      nullable; fp32 [B][ceil(L / RLM_SCAN_CHUNK)][D], receives the state
+ *              before each chunk for rlm_scan_backward
+ * Workspace: rlm_scan_workspace_size. */
+RLM_API rlm_status rlm_scan_prefill(const rlm_strided *x, const rlm_strided *g, int leak, const float *state_in,
+                                    const rlm_strided *y, float *state_out, float *saved, const int32_t *lengths,
+                                    const rlm_launch *launch);
+
+/* Gradients of a scalar loss given dy = dl/dy and (nullable) d_state_out = dl/dh_{L-1}:
+ *   G_t = dy_t + a_{t+1} G_{t+1},  dx = (1 - a) G or G,  dg = a (1 - a) G (h_{t-1} - x_t)
+ *   or a (1 - a) G h_{t-1};  d_state_in (nullable output) = a_0 G_0.
+ * h is formed again in fp32 from `saved`, which the forward pass of the same x, g and
+ * lengths wrote.  dx and dg are overwritten. */
+RLM_API rlm_status rlm_scan_backward(const rlm_strided *dy, const rlm_strided *x, const rlm_strided *g,
+                                     const float *saved, int leak, const float *d_state_out, const rlm_strided *dx,
+                                     const rlm_strided *dg, float *d_state_in, const int32_t *lengths,
+                                     const rlm_launch *launch);
+
+/* One token: x_t, g_t and y_t are fields with L == 1; state is updated in place. */
+RLM_API rlm_status rlm_scan_decode(const rlm_strided *x_t, const rlm_strided *g_t, int leak, float *state,
+                                   const rlm_strided *y_t, const rlm_launch *launch);
+
+/* Bytes of workspace for rlm_scan_prefill and rlm_scan_backward of this shape (0 is
+ * possible), and of the `saved` buffer. */
+RLM_API size_t rlm_scan_workspace_size(int64_t B, int64_t L, int D, rlm_dtype dtype);
+RLM_API size_t rlm_scan_saved_size(int64_t B, int64_t L, int D);
+
 /* ------------------------------------------------------------------ utility
  * rlm_validate_params: copies p to the host (synchronous) and checks that every
  * value is finite and every gamma >= 0 (Sec. 3.1 requires alpha > 0; gamma = 0

@@ -26,6 +26,8 @@ __all__ = [
     "rlm_mix_backward_from", "rlm_state_init", "Local", "ConvState", "Coupling", "rlm_mixer_prefill",
     "rlm_mixer_decode",
     "rlm_prefill_workspace_size", "rlm_backward_workspace_size",
+    "rlm_scan_prefill", "rlm_scan_backward", "rlm_scan_decode", "rlm_scan_workspace_size", "rlm_scan_saved_size",
+    "scan_saved",
     "rlm_validate_params", "rlm_get_device_status", "rlm_status_string",
     "rlm_version", "rlm_kernels_launched", "RLM_OK", "RLM_ERR_INVALID_ARG", "RLM_ERR_UNSUPPORTED",
     "RLM_ERR_CUDA", "RLM_ERR_TIMEOUT", "RLM_F32", "RLM_BF16",
@@ -66,6 +68,12 @@ class _Coupling(ctypes.Structure):
 class _ConvState(ctypes.Structure):
     _fields_ = [("u", ctypes.c_void_p), ("dtype", ctypes.c_int), ("B", ctypes.c_int64),
                 ("D", ctypes.c_int), ("K", ctypes.c_int)]
+
+
+class _Strided(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("dtype", ctypes.c_int),
+                ("B", ctypes.c_int64), ("L", ctypes.c_int64), ("D", ctypes.c_int64),
+                ("stride_b", ctypes.c_int64), ("stride_l", ctypes.c_int64)]
 
 
 class _Launch(ctypes.Structure):
@@ -132,6 +140,16 @@ def load_library(build_if_missing: bool = False) -> ctypes.CDLL:
     lib.rlm_mix_prefill_noalloc.argtypes = [P(_Tensor), P(_Params), P(_Tensor), P(_State),
                                             ctypes.c_void_p]
     lib.rlm_mix_prefill_noalloc.restype = ctypes.c_int
+    F, V, I = P(_Strided), ctypes.c_void_p, ctypes.c_int
+    lib.rlm_scan_prefill.argtypes = [F, F, I, V, F, V, V, V, P(_Launch)]
+    lib.rlm_scan_backward.argtypes = [F, F, F, V, I, V, F, F, V, V, P(_Launch)]
+    lib.rlm_scan_decode.argtypes = [F, F, I, V, F, P(_Launch)]
+    for f in ("rlm_scan_prefill", "rlm_scan_backward", "rlm_scan_decode"):
+        getattr(lib, f).restype = ctypes.c_int
+    lib.rlm_scan_workspace_size.argtypes = [ctypes.c_int64, ctypes.c_int64, I, I]
+    lib.rlm_scan_saved_size.argtypes = [ctypes.c_int64, ctypes.c_int64, I]
+    for f in ("rlm_scan_workspace_size", "rlm_scan_saved_size"):
+        getattr(lib, f).restype = ctypes.c_size_t
     _lib = lib
     return lib
 
@@ -292,6 +310,30 @@ def _field(t: torch.Tensor) -> _Tensor:
     else:
         raise ValueError(f"fields are [B][L][D] (or [B][D] for one token), got {tuple(t.shape)}")
     return _Tensor(t.data_ptr(), _DT[t.dtype], B, L, D)
+
+
+def _strided(t: torch.Tensor, name: str) -> _Strided:
+    """A [B][L][D] (or, for one token, [B][D]) field, possibly a view with row strides."""
+    if t.dtype not in _DT:
+        raise ValueError(f"{name}: unsupported dtype {t.dtype}")
+    if not t.is_cuda or t.dim() not in (2, 3) or t.stride(-1) != 1:
+        raise ValueError(f"{name} must be a CUDA [B][L][D] (or [B][D]) tensor with unit channel stride, got "
+                         f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    if t.dim() == 2:
+        (B, D), L = t.shape, 1
+        return _Strided(t.data_ptr(), _DT[t.dtype], B, L, D, t.stride(0), D)
+    B, L, D = t.shape
+    return _Strided(t.data_ptr(), _DT[t.dtype], B, L, D, t.stride(0), t.stride(1))
+
+
+def _opt(t: torch.Tensor | None, dtype, shape, name: str):
+    """Pointer of an optional contiguous CUDA tensor of a fixed shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of shape {tuple(shape)}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
 def _stream(stream) -> int:
@@ -483,3 +525,71 @@ def rlm_mixer_decode(x_t: torch.Tensor, g_t: torch.Tensor | None, state: State, 
     _check(lib.rlm_mixer_decode(ctypes.byref(xt), ref(gt), ctypes.byref(state._c()), opt(local), opt(coupling),
                                 opt(conv),
                                 ctypes.byref(zt), ctypes.byref(_launch(stream, None))), "rlm_mixer_decode")
+
+
+# ------------------------------------------------- gated linear recurrence
+def rlm_scan_workspace_size(B: int, L: int, D: int, dtype) -> int:
+    return load_library().rlm_scan_workspace_size(B, L, D, _DT.get(dtype, dtype))
+
+
+def rlm_scan_saved_size(B: int, L: int, D: int) -> int:
+    return load_library().rlm_scan_saved_size(B, L, D)
+
+
+SCAN_CHUNK = 64         # RLM_SCAN_CHUNK: tokens between the states a training pass keeps
+
+
+def scan_saved(B: int, L: int, D: int, device="cuda") -> torch.Tensor:
+    """A buffer for rlm_scan_prefill's ``saved``: float32 [B][ceil(L / 64)][D]."""
+    return torch.empty(B, -(-L // SCAN_CHUNK), D, dtype=torch.float32, device=device)
+
+
+def rlm_scan_prefill(x: torch.Tensor, g: torch.Tensor, y: torch.Tensor, leak: bool = True,
+                     state_in: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
+                     saved: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Gated linear recurrence h_t = a_t h_{t-1} + i_t over a sequence, a = sigmoid(g),
+    i = (1 - a) x (``leak``) or x; y receives every h_t.  Fields [B][L][D] may have row
+    strides; states are float32 [B][D] (``state_out`` may be ``state_in``); ``lengths``
+    int32 [B] marks padding; ``saved`` (see ``scan_saved``) keeps what the backward
+    pass needs."""
+    lib = load_library()
+    xt, gt, yt = _strided(x, "x"), _strided(g, "g"), _strided(y, "y")
+    B, L, D = xt.B, xt.L, xt.D
+    if workspace is None:
+        workspace = _workspace(lib.rlm_scan_workspace_size(B, L, D, xt.dtype), x.device)
+    _check(lib.rlm_scan_prefill(ctypes.byref(xt), ctypes.byref(gt), int(leak),
+                                _opt(state_in, torch.float32, (B, D), "state_in"), ctypes.byref(yt),
+                                _opt(state_out, torch.float32, (B, D), "state_out"),
+                                _opt(saved, torch.float32, (B, -(-L // SCAN_CHUNK), D), "saved"),
+                                _opt(lengths, torch.int32, (B,), "lengths"),
+                                ctypes.byref(_launch(stream, workspace))), "rlm_scan_prefill")
+
+
+def rlm_scan_backward(dy: torch.Tensor, x: torch.Tensor, g: torch.Tensor, saved: torch.Tensor, dx: torch.Tensor,
+                      dg: torch.Tensor, leak: bool = True, d_state_out: torch.Tensor | None = None,
+                      d_state_in: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Gradients of rlm_scan_prefill: dx, dg and (optionally) of its initial state, for a
+    loss of y and, with ``d_state_out``, of the final state."""
+    lib = load_library()
+    dyt, xt, gt = _strided(dy, "dy"), _strided(x, "x"), _strided(g, "g")
+    dxt, dgt = _strided(dx, "dx"), _strided(dg, "dg")
+    B, L, D = xt.B, xt.L, xt.D
+    if workspace is None:
+        workspace = _workspace(lib.rlm_scan_workspace_size(B, L, D, xt.dtype), x.device)
+    _check(lib.rlm_scan_backward(ctypes.byref(dyt), ctypes.byref(xt), ctypes.byref(gt),
+                                 _opt(saved, torch.float32, (B, -(-L // SCAN_CHUNK), D), "saved"), int(leak),
+                                 _opt(d_state_out, torch.float32, (B, D), "d_state_out"), ctypes.byref(dxt),
+                                 ctypes.byref(dgt), _opt(d_state_in, torch.float32, (B, D), "d_state_in"),
+                                 _opt(lengths, torch.int32, (B,), "lengths"),
+                                 ctypes.byref(_launch(stream, workspace))), "rlm_scan_backward")
+
+
+def rlm_scan_decode(x_t: torch.Tensor, g_t: torch.Tensor, state: torch.Tensor, y_t: torch.Tensor, leak: bool = True,
+                    stream=None) -> None:
+    """One token of the gated linear recurrence; ``state`` (float32 [B][D]) advances in place."""
+    xt, gt, yt = _strided(x_t, "x_t"), _strided(g_t, "g_t"), _strided(y_t, "y_t")
+    _check(load_library().rlm_scan_decode(ctypes.byref(xt), ctypes.byref(gt), int(leak),
+                                          _opt(state, torch.float32, (xt.B, xt.D), "state"), ctypes.byref(yt),
+                                          ctypes.byref(_launch(stream, None))), "rlm_scan_decode")

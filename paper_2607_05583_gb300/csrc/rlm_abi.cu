@@ -11,6 +11,7 @@
 #include <mutex>
 #include <vector>
 
+#include "rlm_check.h"
 #include "rlm_internal.h"
 
 namespace rlm {
@@ -51,24 +52,6 @@ namespace {
 
 constexpr int kMaxModes = 64;
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-size_t elem_size(rlm_dtype dt) { return dt == RLM_BF16 ? 2 : 4; }
-
-rlm_status fail(rlm_status s, const char *fmt, ...) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof(buf), fmt, ap);
-    va_end(ap);
-    set_error("%s", buf);
-    return s;
-}
-
-rlm_status cuda_fail(cudaError_t e, const char *what) {
-    return fail(RLM_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
-}
-
 rlm_status check_tensor(const rlm_tensor *t, const char *name) {
     if (!t) return fail(RLM_ERR_INVALID_ARG, "%s is NULL", name);
     if (!t->ptr) return fail(RLM_ERR_INVALID_ARG, "%s->ptr is NULL", name);
@@ -97,11 +80,6 @@ size_t tensor_bytes(const rlm_tensor *t) {
     return (size_t)t->B * (size_t)t->L * (size_t)t->D * elem_size(t->dtype);
 }
 
-bool overlap(const void *a, size_t na, const void *b, size_t nb) {
-    const char *pa = static_cast<const char *>(a), *pb = static_cast<const char *>(b);
-    return pa < pb + nb && pb < pa + na;
-}
-
 rlm_status check_params(const rlm_params *p, int64_t D) {
     if (!p) return fail(RLM_ERR_INVALID_ARG, "params is NULL");
     const float *ps[4] = {p->decay, p->freq, p->amp, p->phase};
@@ -123,17 +101,6 @@ rlm_status check_state(const rlm_state *s, int64_t B, int64_t D, int M, const ch
     if (s->B != B || s->D != D || s->M != M)
         return fail(RLM_ERR_INVALID_ARG, "%s is [B=%d][D=%d][M=%d], expected [%lld][%lld][%d]", name,
                     s->B, s->D, s->M, (long long)B, (long long)D, M);
-    return RLM_OK;
-}
-
-rlm_status check_workspace(const rlm_launch *ln, size_t need) {
-    if (!ln) return fail(RLM_ERR_INVALID_ARG, "launch is NULL");
-    if (need == 0) return RLM_OK;
-    if (!ln->workspace) return fail(RLM_ERR_INVALID_ARG, "workspace is NULL but %zu bytes are needed", need);
-    if ((reinterpret_cast<uintptr_t>(ln->workspace) & 255u) != 0)
-        return fail(RLM_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
-    if (ln->workspace_bytes < need)
-        return fail(RLM_ERR_INVALID_ARG, "workspace has %zu bytes, %zu needed", ln->workspace_bytes, need);
     return RLM_OK;
 }
 
@@ -587,15 +554,17 @@ rlm_status rlm_validate_params(const rlm_params *p) {
 
 rlm_status rlm_get_device_status(const rlm_launch *ln) {
     if (!ln) return fail(RLM_ERR_INVALID_ARG, "launch is NULL");
-    int status = RLM_OK, bwd = RLM_OK, mix = RLM_OK, t32 = RLM_OK;
+    int status = RLM_OK, bwd = RLM_OK, mix = RLM_OK, t32 = RLM_OK, scan = RLM_OK;
     cudaError_t e = read_and_clear_device_status(&status, static_cast<cudaStream_t>(ln->stream));
     if (e == cudaSuccess) e = read_and_clear_bwd_status(&bwd, static_cast<cudaStream_t>(ln->stream));
     if (e == cudaSuccess) e = read_and_clear_mixer_status(&mix, static_cast<cudaStream_t>(ln->stream));
     if (e == cudaSuccess) e = read_and_clear_tc32_status(&t32, static_cast<cudaStream_t>(ln->stream));
+    if (e == cudaSuccess) e = read_and_clear_scan_status(&scan, static_cast<cudaStream_t>(ln->stream));
     if (e != cudaSuccess) return cuda_fail(e, "rlm_get_device_status");
     if (status == RLM_OK) status = bwd;
     if (status == RLM_OK) status = mix;
     if (status == RLM_OK) status = t32;
+    if (status == RLM_OK) status = scan;
     if (status != RLM_OK) return fail((rlm_status)status, "a bounded device-side wait expired");
     return RLM_OK;
 }

@@ -81,6 +81,20 @@ cudaError_t tc_prefill_rev(const void *x, void *y, int64_t B, int64_t L, int D, 
                            const float *freq, const float *amp, const float *phase, const float *state_in,
                            float *state_out, float *coef_out, void *ws, cudaStream_t st);
 
+// ---- gated linear recurrence (rlm_scan.cu) ----------------------------------
+// Arguments as checked by the C ABI; state_in / state_out / saved / lengths and
+// d_state_out / d_state_in may be null.  ws holds scan_ws_bytes().
+size_t scan_ws_bytes(int64_t B, int64_t L, int D, rlm_dtype dt);
+cudaError_t scan_forward(const rlm_strided &x, const rlm_strided &g, const rlm_strided &y, bool leak,
+                         const float *state_in, float *state_out, float *saved, const int *lengths, void *ws,
+                         cudaStream_t st);
+cudaError_t scan_backward(const rlm_strided &dy, const rlm_strided &x, const rlm_strided &g, const float *saved,
+                          bool leak, const float *d_state_out, const rlm_strided &dx, const rlm_strided &dg,
+                          float *d_state_in, const int *lengths, void *ws, cudaStream_t st);
+cudaError_t scan_step(const rlm_strided &x, const rlm_strided &g, const rlm_strided &y, bool leak, float *state,
+                      cudaStream_t st);
+cudaError_t read_and_clear_scan_status(int *status, cudaStream_t st);
+
 // ---- decode (rlm_decode.cu) -----------------------------------------------
 cudaError_t decode_step(const void *x_t, void *y_t, rlm_dtype dt, int B, int D, int M,
                         float *s, const float *coef, cudaStream_t st);
