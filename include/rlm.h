@@ -324,9 +324,9 @@ RLM_API rlm_status rlm_mixer_decode(const rlm_tensor *x_t, const rlm_tensor *g_t
  * lengths (nullable): int32 [B] on the device; row b's tokens from lengths[b] on are
  * padding (values outside 0..L are clamped): x, g and dy are not read there, y, dx and
  * dg are 0, and the state passes through (a row of length 0 returns its initial state).
- * Paths: one kernel per call; where B * ceil(D / 64) is small, several blocks share a
- * sequence and exchange their tiles' runs through the workspace (a cooperative launch
- * with bounded waits).  Sums are fp32 in an order fixed by the shape. */
+ * One kernel per call, no workspace; where there are few rows and channels, clusters of
+ * up to 8 blocks share a sequence and exchange their tiles' runs through distributed
+ * shared memory (with bounded waits).  Sums are fp32 in an order fixed by the shape. */
 typedef struct {
     void *ptr;
     rlm_dtype dtype;
@@ -342,8 +342,7 @@ typedef struct {
  *   state_in   nullable, h_{-1} (zero if NULL);  state_out  nullable, h_{L-1} (may be
  *              state_in itself)
  *   saved      nullable; fp32 [B][ceil(L / RLM_SCAN_CHUNK)][D], receives the state
- *              before each chunk for rlm_scan_backward
- * Workspace: rlm_scan_workspace_size. */
+ *              before each chunk for rlm_scan_backward */
 RLM_API rlm_status rlm_scan_prefill(const rlm_strided *x, const rlm_strided *g, int leak, const float *state_in,
                                     const rlm_strided *y, float *state_out, float *saved, const int32_t *lengths,
                                     const rlm_launch *launch);
@@ -362,9 +361,7 @@ RLM_API rlm_status rlm_scan_backward(const rlm_strided *dy, const rlm_strided *x
 RLM_API rlm_status rlm_scan_decode(const rlm_strided *x_t, const rlm_strided *g_t, int leak, float *state,
                                    const rlm_strided *y_t, const rlm_launch *launch);
 
-/* Bytes of workspace for rlm_scan_prefill and rlm_scan_backward of this shape (0 is
- * possible), and of the `saved` buffer. */
-RLM_API size_t rlm_scan_workspace_size(int64_t B, int64_t L, int D, rlm_dtype dtype);
+/* Bytes of the `saved` buffer. */
 RLM_API size_t rlm_scan_saved_size(int64_t B, int64_t L, int D);
 
 /* ------------------------------------------------------------------ utility

@@ -26,8 +26,7 @@ __all__ = [
     "rlm_mix_backward_from", "rlm_state_init", "Local", "ConvState", "Coupling", "rlm_mixer_prefill",
     "rlm_mixer_decode",
     "rlm_prefill_workspace_size", "rlm_backward_workspace_size",
-    "rlm_scan_prefill", "rlm_scan_backward", "rlm_scan_decode", "rlm_scan_workspace_size", "rlm_scan_saved_size",
-    "scan_saved",
+    "rlm_scan_prefill", "rlm_scan_backward", "rlm_scan_decode", "rlm_scan_saved_size", "scan_saved",
     "rlm_validate_params", "rlm_get_device_status", "rlm_status_string",
     "rlm_version", "rlm_kernels_launched", "RLM_OK", "RLM_ERR_INVALID_ARG", "RLM_ERR_UNSUPPORTED",
     "RLM_ERR_CUDA", "RLM_ERR_TIMEOUT", "RLM_F32", "RLM_BF16",
@@ -146,10 +145,8 @@ def load_library(build_if_missing: bool = False) -> ctypes.CDLL:
     lib.rlm_scan_decode.argtypes = [F, F, I, V, F, P(_Launch)]
     for f in ("rlm_scan_prefill", "rlm_scan_backward", "rlm_scan_decode"):
         getattr(lib, f).restype = ctypes.c_int
-    lib.rlm_scan_workspace_size.argtypes = [ctypes.c_int64, ctypes.c_int64, I, I]
     lib.rlm_scan_saved_size.argtypes = [ctypes.c_int64, ctypes.c_int64, I]
-    for f in ("rlm_scan_workspace_size", "rlm_scan_saved_size"):
-        getattr(lib, f).restype = ctypes.c_size_t
+    lib.rlm_scan_saved_size.restype = ctypes.c_size_t
     _lib = lib
     return lib
 
@@ -528,10 +525,6 @@ def rlm_mixer_decode(x_t: torch.Tensor, g_t: torch.Tensor | None, state: State, 
 
 
 # ------------------------------------------------- gated linear recurrence
-def rlm_scan_workspace_size(B: int, L: int, D: int, dtype) -> int:
-    return load_library().rlm_scan_workspace_size(B, L, D, _DT.get(dtype, dtype))
-
-
 def rlm_scan_saved_size(B: int, L: int, D: int) -> int:
     return load_library().rlm_scan_saved_size(B, L, D)
 
@@ -547,7 +540,7 @@ def scan_saved(B: int, L: int, D: int, device="cuda") -> torch.Tensor:
 def rlm_scan_prefill(x: torch.Tensor, g: torch.Tensor, y: torch.Tensor, leak: bool = True,
                      state_in: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
                      saved: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
-                     workspace: torch.Tensor | None = None, stream=None) -> None:
+                     stream=None) -> None:
     """Gated linear recurrence h_t = a_t h_{t-1} + i_t over a sequence, a = sigmoid(g),
     i = (1 - a) x (``leak``) or x; y receives every h_t.  Fields [B][L][D] may have row
     strides; states are float32 [B][D] (``state_out`` may be ``state_in``); ``lengths``
@@ -556,34 +549,30 @@ def rlm_scan_prefill(x: torch.Tensor, g: torch.Tensor, y: torch.Tensor, leak: bo
     lib = load_library()
     xt, gt, yt = _strided(x, "x"), _strided(g, "g"), _strided(y, "y")
     B, L, D = xt.B, xt.L, xt.D
-    if workspace is None:
-        workspace = _workspace(lib.rlm_scan_workspace_size(B, L, D, xt.dtype), x.device)
     _check(lib.rlm_scan_prefill(ctypes.byref(xt), ctypes.byref(gt), int(leak),
                                 _opt(state_in, torch.float32, (B, D), "state_in"), ctypes.byref(yt),
                                 _opt(state_out, torch.float32, (B, D), "state_out"),
                                 _opt(saved, torch.float32, (B, -(-L // SCAN_CHUNK), D), "saved"),
                                 _opt(lengths, torch.int32, (B,), "lengths"),
-                                ctypes.byref(_launch(stream, workspace))), "rlm_scan_prefill")
+                                ctypes.byref(_launch(stream, None))), "rlm_scan_prefill")
 
 
 def rlm_scan_backward(dy: torch.Tensor, x: torch.Tensor, g: torch.Tensor, saved: torch.Tensor, dx: torch.Tensor,
                       dg: torch.Tensor, leak: bool = True, d_state_out: torch.Tensor | None = None,
                       d_state_in: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
-                      workspace: torch.Tensor | None = None, stream=None) -> None:
+                      stream=None) -> None:
     """Gradients of rlm_scan_prefill: dx, dg and (optionally) of its initial state, for a
     loss of y and, with ``d_state_out``, of the final state."""
     lib = load_library()
     dyt, xt, gt = _strided(dy, "dy"), _strided(x, "x"), _strided(g, "g")
     dxt, dgt = _strided(dx, "dx"), _strided(dg, "dg")
     B, L, D = xt.B, xt.L, xt.D
-    if workspace is None:
-        workspace = _workspace(lib.rlm_scan_workspace_size(B, L, D, xt.dtype), x.device)
     _check(lib.rlm_scan_backward(ctypes.byref(dyt), ctypes.byref(xt), ctypes.byref(gt),
                                  _opt(saved, torch.float32, (B, -(-L // SCAN_CHUNK), D), "saved"), int(leak),
                                  _opt(d_state_out, torch.float32, (B, D), "d_state_out"), ctypes.byref(dxt),
                                  ctypes.byref(dgt), _opt(d_state_in, torch.float32, (B, D), "d_state_in"),
                                  _opt(lengths, torch.int32, (B,), "lengths"),
-                                 ctypes.byref(_launch(stream, workspace))), "rlm_scan_backward")
+                                 ctypes.byref(_launch(stream, None))), "rlm_scan_backward")
 
 
 def rlm_scan_decode(x_t: torch.Tensor, g_t: torch.Tensor, state: torch.Tensor, y_t: torch.Tensor, leak: bool = True,

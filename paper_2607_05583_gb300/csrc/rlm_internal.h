@@ -83,14 +83,13 @@ cudaError_t tc_prefill_rev(const void *x, void *y, int64_t B, int64_t L, int D, 
 
 // ---- gated linear recurrence (rlm_scan.cu) ----------------------------------
 // Arguments as checked by the C ABI; state_in / state_out / saved / lengths and
-// d_state_out / d_state_in may be null.  ws holds scan_ws_bytes().
-size_t scan_ws_bytes(int64_t B, int64_t L, int D, rlm_dtype dt);
+// d_state_out / d_state_in may be null.
 cudaError_t scan_forward(const rlm_strided &x, const rlm_strided &g, const rlm_strided &y, bool leak,
-                         const float *state_in, float *state_out, float *saved, const int *lengths, void *ws,
+                         const float *state_in, float *state_out, float *saved, const int *lengths,
                          cudaStream_t st);
 cudaError_t scan_backward(const rlm_strided &dy, const rlm_strided &x, const rlm_strided &g, const float *saved,
                           bool leak, const float *d_state_out, const rlm_strided &dx, const rlm_strided &dg,
-                          float *d_state_in, const int *lengths, void *ws, cudaStream_t st);
+                          float *d_state_in, const int *lengths, cudaStream_t st);
 cudaError_t scan_step(const rlm_strided &x, const rlm_strided &g, const rlm_strided &y, bool leak, float *state,
                       cudaStream_t st);
 cudaError_t read_and_clear_scan_status(int *status, cudaStream_t st);

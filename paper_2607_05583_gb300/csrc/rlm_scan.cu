@@ -12,24 +12,32 @@
 // reaches h_{t-1}, G_t = dy_t + C_{t+1} and C_t = a_t G_t; then
 //   leak  dx = b G, dg = a b G (h_{t-1} - x)      unit  dx = G, dg = a b G h_{t-1}.
 //
-// Bound by memory: 3 fields move in the forward pass and 5 in the backward pass,
-// about 20 instructions an element beside.  So each field is read once: a thread
-// holds kS tokens of two channels in registers, the runs of a tile's threads compose
-// through shuffles and shared memory, and the tiles' runs through a workspace.
+// Bound by memory: 3 fields move in the forward pass and 5 in the backward pass, and
+// each is read once.  At the measured copy rate an SM has about 33 instructions for each
+// bf16 element of the forward pass, so the arithmetic runs on channel pairs as packed
+// fp32 (f32x2), with -b in place of b (all signs then fall into the fma).
 //
-// Tiles.  A CTA of 256 threads covers P channel pairs (P = 4, 8, 16 or 32, the least
-// that holds D / 2) by 256 / P runs of kS tokens: 128-byte row slices at D >= 64, a
-// whole row below.  It walks its channels' tiles in time order with the carry in
-// registers, loading the next tile's fields while it works on this one.
+// Tiles.  Eight data warps of a CTA cover P channel pairs (P = 4, 8, 16 or 32) by
+// 256 / P runs of kS = 8 tokens, a thread per run and pair.  A warp copies the rows
+// that its own threads need (16-byte cp.async, out-of-range rows and padding filled
+// with zeros) into a private ring of kStages tiles, so no barrier guards the data.
+// A thread composes its run (first pass), keeps -b in registers, and once it knows the
+// state at the run's start walks the run again for the outputs (second pass).
 //
-// Segments.  Few channels (B ceil(D / 64) CTAs below the resident number) would
-// leave SMs idle, so nseg CTAs share a chain of tiles: in wave w CTA s takes tile
-// w nseg + s, publishes the tile's (A, H), reads those of the whole wave and composes
-// the ones before its own on top of the carry (and all of them for the next wave's
-// carry).  Nobody waits for a neighbour's output, so a wave costs one exchange
-// through L2, whatever nseg is, and no field is read twice.  The launch is
-// cooperative (all CTAs resident) and every wait is bounded.  The order of all
-// products and sums is fixed by the shape: results repeat bit for bit.
+// A ninth warp turns runs into states.  Its lane holds one channel pair of 8
+// consecutive runs (64 tokens, one saved chunk): it composes them, scans across lanes,
+// adds the carry and hands every run its start state.  The data warps work on the next
+// tile's first pass meanwhile: the second pass of tile w follows the first pass of
+// tile w + 1, so the hand-over, and the exchange below, are off their path.
+//
+// Segments.  Few channels would leave SMs idle, so a cluster of nseg CTAs (2, 4 or 8)
+// shares a chain of tiles: in wave w CTA s takes tile w nseg + s and sends the tile's
+// (A, H) into every member's shared memory (st.async, which also completes the
+// receiver's mbarrier, so data and readiness arrive together).  Each member composes the
+// entries before its own on top of the carry, and all of them for the next wave's carry.
+// Nobody waits for a neighbour's output: a wave costs one exchange, whatever nseg is, and
+// no field is read twice.  Every wait is bounded.  The order of all products and sums is
+// fixed by the shape: results repeat bit for bit.
 #include <algorithm>
 #include <mutex>
 #include <vector>
@@ -43,8 +51,10 @@ __device__ int g_scan_status = 0;
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
+constexpr int kDataThreads = 256;
+constexpr int kThreads = kDataThreads + 32;         // and the warp that turns runs into states
+constexpr int kS = 8;                               // tokens of a run
+constexpr int kBarRuns = 1, kBarStates = 3;         // named barriers, two of each by tile parity
 constexpr int kChunk = RLM_SCAN_CHUNK;              // tokens between saved states
 constexpr long long kWaitLimit = 4000000000ll;      // SM cycles: about 2 s
 
@@ -54,12 +64,6 @@ struct Pair;
 template <>
 struct Pair<__nv_bfloat16> {
     using Raw = uint32_t;
-    static __device__ __forceinline__ Raw load(const __nv_bfloat16 *p) {
-        Raw r;
-        asm("ld.global.nc.L1::no_allocate.b32 %0, [%1];" : "=r"(r) : "l"(p));
-        return r;
-    }
-    static __device__ __forceinline__ Raw zero() { return 0u; }
     static __device__ __forceinline__ float2 value(Raw r) {
         return make_float2(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u));
     }
@@ -71,25 +75,9 @@ struct Pair<__nv_bfloat16> {
 template <>
 struct Pair<float> {
     using Raw = float2;
-    static __device__ __forceinline__ Raw load(const float *p) {
-        Raw r;
-        asm("ld.global.nc.L1::no_allocate.v2.f32 {%0, %1}, [%2];" : "=f"(r.x), "=f"(r.y) : "l"(p));
-        return r;
-    }
-    static __device__ __forceinline__ Raw zero() { return make_float2(0.f, 0.f); }
     static __device__ __forceinline__ float2 value(Raw r) { return r; }
     static __device__ __forceinline__ void store(float *p, float2 v) { __stcs(reinterpret_cast<float2 *>(p), v); }
 };
-
-// Tokens of one thread's run.  The forward pass holds b (8 bytes), x and the next
-// tile's x and g for each token and channel pair, the backward pass also dy and
-// h_{t-1}: the largest powers of two that stay under 128 registers.
-template <typename T>
-constexpr int kFwdRun = sizeof(T) == 2 ? 16 : 8;
-constexpr int kBwdRun = 8;
-
-// 1 - sigma(g); g = +inf gives 0, -inf gives 1.
-__device__ __forceinline__ float rest(float g) { return __fdividef(1.0f, 1.0f + expf(g)); }
 
 template <typename T>
 struct ScanArgs {
@@ -101,9 +89,36 @@ struct ScanArgs {
     float *saved;               // [B][ceil(L / kChunk)][D]: h before each chunk (forward: nullable output)
     const int *lengths;         // nullable, [B]
     int L, D, groups, log2p, nseg, ntiles, nchunks;
-    float4 *agg;                // [chain][2][nseg][32]: (A, A', H, H') of a tile, by wave parity
-    unsigned *flag;             // [chain][nseg]: waves published
 };
+
+// Two channels' values in one 64-bit register.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pack(float2 v) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+    return r;
+}
+__device__ __forceinline__ float2 unpack(f32x2 v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+constexpr f32x2 kOne = 0x3f8000003f800000ull, kMinus = 0xbf800000bf800000ull;
 
 // (A, H) of two channels as (A.x, A.y, H.x, H.y); `later` o `earlier`.
 __device__ __forceinline__ float4 compose(float4 earlier, float4 later) {
@@ -137,301 +152,490 @@ __device__ __forceinline__ float4 lane_exclusive(float4 incl, int P, int lane) {
     return (kRev ? src < 32 : src >= 0) ? o : identity4();
 }
 
-// Waits until segment `flag` has published `want` waves; bounded.  The acquire
-// orders this thread's later loads of the published values.
-__device__ __forceinline__ void wait_published(const unsigned *flag, unsigned want, volatile int *abort_flag) {
+__device__ __forceinline__ void bar_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kThreads) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id) {
+    asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kThreads) : "memory");
+}
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+constexpr int kMaxSeg = 8;      // portable cluster size
+
+// What a cluster's members send one another: tile runs by wave parity.
+struct Peers {
+    float4 run[2][kMaxSeg][32];
+    unsigned long long full[2];     // mbarriers: one arrival (this CTA's) and the entries' bytes
+};
+
+// Bounded wait; after a timeout (now or earlier) the kernel runs on with what is there.
+__device__ __forceinline__ void wait_full(uint32_t bar, uint32_t parity, bool &gave_up) {
     long long t0 = 0;
     for (uint32_t it = 1;; ++it) {
-        unsigned v;
-        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(flag) : "memory");
-        if (v >= want) return;
+        uint32_t ok;
+        asm volatile(
+            "{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (ok || gave_up) return;
         if ((it & 255u) == 0) {
-            if (*abort_flag) return;
             const long long now = clock64();
             if (t0 == 0) {
                 t0 = now;
             } else if (now - t0 > kWaitLimit) {
-                *abort_flag = 1;
+                gave_up = true;
                 atomicExch(&g_scan_status, (int)RLM_ERR_TIMEOUT);
-                return;
             }
         }
     }
 }
 
-struct ScanShared {
-    float4 run[2][kWarps][32];          // a warp's composed run, by tile parity
-    float4 pre[2][kWarps][32];          // folds of a wave's tiles: those before this CTA's own,
-    float4 all[2][kWarps][32];          //   and all of them
-    int abort_flag;
+// One wave's exchange by the ninth warp: sends this tile's run `mine` (held by every lane
+// of a pair) to all members and returns the composition of the tiles before it (*pre) and
+// of the whole wave.  A member sends wave w + 2 only after it has received this one's wave
+// w + 1, which this warp sent after it had read wave w: the two buffers suffice.
+__device__ __forceinline__ void exchange(float4 mine, Peers &peers, int wave, int seg, int nseg, int P, int cp,
+                                         bool &gave_up, float4 *pre, float4 *all) {
+    const int lane = threadIdx.x & 31, par = wave & 1;
+    const uint32_t bar = smem_u32(&peers.full[par]), slot = smem_u32(&peers.run[par][seg][cp]);
+    if (lane == 0)
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(nseg * P * 16) : "memory");
+    for (int s = lane / P; s < nseg; s += 32 / P) {
+        uint32_t to, tb;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(slot), "r"(s));
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(tb) : "r"(bar), "r"(s));
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+                         to),
+                     "r"(__float_as_uint(mine.x)), "r"(__float_as_uint(mine.y)), "r"(__float_as_uint(mine.z)),
+                     "r"(__float_as_uint(mine.w)), "r"(tb)
+                     : "memory");
+    }
+    wait_full(bar, (wave >> 1) & 1, gave_up);
+    float4 fa = identity4();
+    *pre = fa;
+#pragma unroll
+    for (int s = 0; s < kMaxSeg; ++s) {
+        if (s < nseg) {
+            if (s == seg) *pre = fa;
+            fa = compose(fa, peers.run[par][s][cp]);
+        }
+    }
+    *all = fa;
+    __syncwarp();
+}
+
+// Set-up and end of a cluster: no member sends before all have their barriers, none
+// leaves while another may still send to it.
+__device__ __forceinline__ void open_peers(Peers &peers, int nseg) {
+    if (nseg < 2) return;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i)
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&peers.full[i])) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    cluster_sync();
+}
+__device__ __forceinline__ void close_peers(int nseg) {
+    if (nseg > 1) cluster_sync();
+}
+
+// What the warps of one scan CTA share.
+struct Where {
+    int lane, warp, P, cp, sc, seg, row, c, tile_tokens, len, n;
+    bool on;
 };
 
-// One wave's exchange: publishes this tile's run `mine` and returns the composition of
-// the tiles before it (*pre) and of the `live` tiles of the wave (*all).
-__device__ __forceinline__ void exchange(float4 mine, float4 *agg, unsigned *flag, int wave, int seg, int nseg, int live,
-                                         int P, int cp, ScanShared &sh, float4 *pre, float4 *all) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, par = wave & 1;
-    float4 *row = agg + (int64_t)par * nseg * 32;
-    if (warp == 0) {
-        if (lane < P) __stcg(row + seg * 32 + cp, mine);
-        __syncwarp();
-        if (lane == 0) {
-            __threadfence();
-            asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(flag + seg), "r"((unsigned)(wave + 1)) : "memory");
-        }
-    }
-    // Each run of threads folds its share of the wave's tiles.
-    const int parts = kThreads / P, part = tid / P;
-    const int lo = live * part / parts, hi = live * (part + 1) / parts;
-    for (int s = lo; s < hi; ++s) wait_published(flag + s, (unsigned)(wave + 1), &sh.abort_flag);
-    float4 fa = identity4(), fp = identity4();
-#pragma unroll 4
-    for (int s = lo; s < hi; ++s) {
-        const float4 v = __ldcg(row + s * 32 + cp);
-        if (s == seg) fp = fa;
-        fa = compose(fa, v);
-    }
-    if (seg >= hi) fp = fa;             // (a share that lies after `seg` keeps the identity)
-    fa = lane_scan<false>(fa, P, lane);
-    // Before-parts compose in the same order: full shares, then the one that holds `seg`.
-    fp = lane_scan<false>(fp, P, lane);
-    if (lane >= 32 - P) {
-        sh.all[par][warp][cp] = fa;
-        sh.pre[par][warp][cp] = fp;
-    }
-    __syncthreads();
-    float4 ta = identity4(), tp = identity4();
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        ta = compose(ta, sh.all[par][w][cp]);
-        tp = compose(tp, sh.pre[par][w][cp]);
-    }
-    *pre = tp;
-    *all = ta;
+template <typename T>
+__device__ __forceinline__ Where where(const ScanArgs<T> &a) {
+    Where w;
+    const int tid = threadIdx.x;
+    w.lane = tid & 31;
+    w.warp = tid >> 5;
+    w.P = 1 << a.log2p;
+    w.cp = tid & (w.P - 1);
+    w.sc = tid >> a.log2p;
+    const int chain = blockIdx.x / a.nseg;          // a cluster is one chain
+    w.seg = blockIdx.x - chain * a.nseg;
+    w.row = chain / a.groups;
+    w.c = (chain - w.row * a.groups) * 2 * w.P + 2 * w.cp;
+    w.on = w.c < a.D;
+    w.tile_tokens = (kDataThreads >> a.log2p) * kS;
+    w.len = a.lengths ? min(max(__ldg(a.lengths + w.row), 0), a.L) : a.L;
+    w.n = (a.ntiles + a.nseg - 1) / a.nseg;         // waves (in the last one, tiles past the end do nothing)
+    return w;
 }
 
-template <typename T, bool kLeak>
-__global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> a) {
-    constexpr int S = kFwdRun<T>;
-    using Raw = typename Pair<T>::Raw;
-    __shared__ ScanShared sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int P = 1 << a.log2p, cp = tid & (P - 1), sc = tid >> a.log2p;
-    const int chains = gridDim.x / a.nseg, seg = blockIdx.x / chains, chain = blockIdx.x - seg * chains;
-    const int row = chain / a.groups, c = (chain - row * a.groups) * 2 * P + 2 * cp;
-    const bool on = c < a.D;
-    const int T_ = (kThreads >> a.log2p) * S;
-    const int len = a.lengths ? min(max(a.lengths[row], 0), a.L) : a.L;
-    if (tid == 0) sh.abort_flag = 0;
-    const T *xp = a.x + row * a.x_b + c, *gp = a.g + row * a.g_b + c;
-    T *yp = a.y + row * a.y_b + c;
-    float2 carry = make_float2(0.f, 0.f);
-    if (a.state_in && on) carry = *reinterpret_cast<const float2 *>(a.state_in + (int64_t)row * a.D + c);
+// A warp's ring of tiles: kFields fields, (32 / P) runs of kS rows, each run a row's
+// size further on so that the runs' rows fall into different banks.
+template <typename T, int kFields, int kStages>
+struct Ring {
+    static constexpr int kFieldBytes = 32 * 2 * (int)sizeof(T) * (kS + 1);
+    static constexpr int kWarpBytes = kFields * kStages * kFieldBytes;
+    static constexpr int kBytes = kWarpBytes * (kDataThreads / 32);
+    static constexpr int kCopies = 2 * (int)sizeof(T) * kS * 32 / (16 * 32);    // 16-byte copies a lane, a field
+    uint32_t base;              // shared address of the warp's ring
+    uint32_t dst[kCopies];      // a lane's copies within a field
+    int row0, rows_apart;       // token (within the warp's rows) of the first copy; rows between copies
+    int c;                      // its first channel
+    int warp_t;                 // the warp's first token within the tile
+    uint32_t own;               // where a thread's own values start within a field
+    int row_bytes;
 
-    Raw xr[S], gr[S];
-    auto load = [&](int tile) {
-        const int t0 = tile * T_ + sc * S;
+    __device__ __forceinline__ Ring(const Where &w, const void *smem, int log2p, int c0) {
+        row_bytes = 2 * (int)sizeof(T) << log2p;
+        base = (uint32_t)__cvta_generic_to_shared(smem) + w.warp * kWarpBytes;
+        const int per_row = row_bytes / 16;
+        row0 = w.lane / per_row;
+        rows_apart = 32 / per_row;
+        const int col = w.lane - row0 * per_row;
+        c = c0 + col * (16 / (int)sizeof(T));
 #pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const bool ok = on && t0 + i < len;
-            xr[i] = ok ? Pair<T>::load(xp + (int64_t)(t0 + i) * a.x_l) : Pair<T>::zero();
-            gr[i] = ok ? Pair<T>::load(gp + (int64_t)(t0 + i) * a.g_l) : Pair<T>::zero();
+        for (int k = 0; k < kCopies; ++k) {
+            const int r = row0 + k * rows_apart;
+            dst[k] = (r / kS) * (kS + 1) * row_bytes + (r % kS) * row_bytes + col * 16;
         }
-    };
-    load(seg);
-    __syncthreads();
-    int wave = 0;
-    for (int tile = seg; tile < a.ntiles; tile += a.nseg, ++wave) {
-        const int t0 = tile * T_ + sc * S;
-        Raw xs[S];
-        float2 b[S];
-        float4 f = identity4();
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const float2 g = Pair<T>::value(gr[i]);
-            const bool ok = t0 + i < len;
-            b[i] = ok ? make_float2(rest(g.x), rest(g.y)) : make_float2(0.f, 0.f);   // past the end: the identity
-            xs[i] = xr[i];
-            const float2 x = Pair<T>::value(xs[i]);
-            f.x = fmaf(-b[i].x, f.x, f.x);
-            f.y = fmaf(-b[i].y, f.y, f.y);
-            f.z = kLeak ? fmaf(b[i].x, x.x - f.z, f.z) : fmaf(-b[i].x, f.z, f.z + x.x);
-            f.w = kLeak ? fmaf(b[i].y, x.y - f.w, f.w) : fmaf(-b[i].y, f.w, f.w + x.y);
-        }
-        if (tile + a.nseg < a.ntiles) load(tile + a.nseg);
-        const float4 incl = lane_scan<false>(f, P, lane);
-        const float4 excl = lane_exclusive<false>(incl, P, lane);
-        if (lane >= 32 - P) sh.run[wave & 1][warp][cp] = incl;
-        __syncthreads();
-        float4 before = identity4(), total = identity4();
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            if (w == warp) before = total;
-            total = compose(total, sh.run[wave & 1][w][cp]);
-        }
-        before = compose(before, excl);
-        float2 h;
-        if (a.nseg > 1) {
-            float4 pre, all;
-            exchange(total, a.agg + (int64_t)chain * 2 * a.nseg * 32, a.flag + (int64_t)chain * a.nseg, wave, seg,
-                     a.nseg, min(a.nseg, a.ntiles - wave * a.nseg), P, cp, sh, &pre, &all);
-            h = apply(before, apply(pre, carry));
-            carry = apply(all, carry);
-        } else {
-            h = apply(before, carry);
-            carry = apply(total, carry);
-        }
-        if (a.saved && on && t0 % kChunk == 0 && t0 < a.L)
-            *reinterpret_cast<float2 *>(a.saved + ((int64_t)row * a.nchunks + t0 / kChunk) * a.D + c) = h;
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const float2 x = Pair<T>::value(xs[i]);
-            h.x = kLeak ? fmaf(b[i].x, x.x - h.x, h.x) : fmaf(-b[i].x, h.x, h.x + x.x);
-            h.y = kLeak ? fmaf(b[i].y, x.y - h.y, h.y) : fmaf(-b[i].y, h.y, h.y + x.y);
-            if (on && t0 + i < a.L)
-                Pair<T>::store(yp + (int64_t)(t0 + i) * a.y_l, t0 + i < len ? h : make_float2(0.f, 0.f));
-        }
-        if (tile == a.ntiles - 1 && a.state_out && on && sc == (kThreads >> a.log2p) - 1)
-            *reinterpret_cast<float2 *>(a.state_out + (int64_t)row * a.D + c) = h;
+        warp_t = w.warp * (32 >> log2p) * kS;
+        own = (w.lane >> log2p) * (kS + 1) * row_bytes + w.cp * 2 * (int)sizeof(T);
     }
+    __device__ __forceinline__ uint32_t field(int stage, int f) const {
+        return base + (stage * kFields + f) * kFieldBytes;
+    }
+    // Copies one field of a tile; p: (row 0 of the batch row, the lane's first channel).
+    __device__ __forceinline__ void copy(int stage, int f, const T *p, int64_t stride, int t0, int len, bool on) const {
+        const uint32_t to = field(stage, f);
+#pragma unroll
+        for (int k = 0; k < kCopies; ++k) {
+            const int t = t0 + warp_t + row0 + k * rows_apart;
+            const bool ok = on && t >= 0 && t < len;
+            const T *src = ok ? p + (int64_t)t * stride : p;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + dst[k]), "l"(src), "r"(ok ? 16 : 0)
+                         : "memory");
+        }
+    }
+    __device__ __forceinline__ f32x2 value(int stage, int f, int i) const {
+        const uint32_t at = field(stage, f) + own + i * row_bytes;
+        if constexpr (sizeof(T) == 2) {
+            uint32_t r;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(at));
+            return pack(Pair<T>::value(r));
+        } else {
+            f32x2 r;
+            asm volatile("ld.shared.b64 %0, [%1];" : "=l"(r) : "r"(at));
+            return r;
+        }
+    }
+};
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+    __syncwarp();
 }
 
-template <typename T, bool kLeak>
-__global__ void __launch_bounds__(kThreads, 2) k_scan_backward(const ScanArgs<T> a) {
-    constexpr int S = kBwdRun;
-    using Raw = typename Pair<T>::Raw;
-    __shared__ ScanShared sh;
-    __shared__ float4 rev[2][kWarps][32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int P = 1 << a.log2p, cp = tid & (P - 1), sc = tid >> a.log2p;
-    const int chains = gridDim.x / a.nseg, seg = blockIdx.x / chains, chain = blockIdx.x - seg * chains;
-    const int row = chain / a.groups, c = (chain - row * a.groups) * 2 * P + 2 * cp;
-    const bool on = c < a.D;
-    const int T_ = (kThreads >> a.log2p) * S;
-    const int len = a.lengths ? min(max(a.lengths[row], 0), a.L) : a.L;
-    if (tid == 0) sh.abort_flag = 0;
-    const T *xp = a.x + row * a.x_b + c, *gp = a.g + row * a.g_b + c, *dyp = a.dy + row * a.dy_b + c;
-    T *dxp = a.dx + row * a.dx_b + c, *dgp = a.dg + row * a.dg_b + c;
-    float2 carry = make_float2(0.f, 0.f);       // C at the end of the wave
-    if (a.state_in && on) carry = *reinterpret_cast<const float2 *>(a.state_in + (int64_t)row * a.D + c);
-    // A chunk of saved-state distance is kChunk / S runs: 8 lanes-by-P of one warp or several warps.
-    const int wpc = max(1, (kChunk / S) * P / 32);
-
-    Raw xr[S], gr[S], dr[S];
-    float2 hs;                                   // the saved state before the thread's chunk
-    auto load = [&](int tile) {
-        const int t0 = tile * T_ + sc * S;
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const bool ok = on && t0 + i < len;
-            xr[i] = ok ? Pair<T>::load(xp + (int64_t)(t0 + i) * a.x_l) : Pair<T>::zero();
-            gr[i] = ok ? Pair<T>::load(gp + (int64_t)(t0 + i) * a.g_l) : Pair<T>::zero();
-            dr[i] = ok ? Pair<T>::load(dyp + (int64_t)(t0 + i) * a.dy_l) : Pair<T>::zero();
-        }
-        hs = make_float2(0.f, 0.f);
-        if (on && t0 < len)
-            hs = __ldg(reinterpret_cast<const float2 *>(a.saved + ((int64_t)row * a.nchunks + t0 / kChunk) * a.D + c));
-    };
-    load(a.ntiles - 1 - seg);
-    __syncthreads();
-    int wave = 0;
-    for (int back = seg; back < a.ntiles; back += a.nseg, ++wave) {
-        const int tile = a.ntiles - 1 - back, t0 = tile * T_ + sc * S;
-        Raw xs[S], ds[S];
-        float2 b[S];
-        float4 f = identity4(), r = identity4();
-        float2 h = hs;
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const float2 g = Pair<T>::value(gr[i]);
-            const bool ok = t0 + i < len;
-            b[i] = ok ? make_float2(rest(g.x), rest(g.y)) : make_float2(0.f, 0.f);
-            xs[i] = xr[i];
-            ds[i] = dr[i];
-            const float2 x = Pair<T>::value(xs[i]);
-            f.x = fmaf(-b[i].x, f.x, f.x);
-            f.y = fmaf(-b[i].y, f.y, f.y);
-            f.z = kLeak ? fmaf(b[i].x, x.x - f.z, f.z) : fmaf(-b[i].x, f.z, f.z + x.x);
-            f.w = kLeak ? fmaf(b[i].y, x.y - f.w, f.w) : fmaf(-b[i].y, f.w, f.w + x.y);
-        }
-        r.x = f.x;
-        r.y = f.y;
-#pragma unroll
-        for (int i = S - 1; i >= 0; --i) {
-            const float2 d = Pair<T>::value(ds[i]);
-            const float gx = d.x + r.z, gy = d.y + r.w;
-            r.z = fmaf(-b[i].x, gx, gx);
-            r.w = fmaf(-b[i].y, gy, gy);
-        }
-        if (back + a.nseg < a.ntiles) load(tile - a.nseg);
-        // Forward runs since the chunk's start (within the warp: only lanes of the same chunk).
-        float4 excl;
-        {
-            const int run = (lane >> a.log2p) & (kChunk / S - 1);      // place within the chunk's lanes
-            float4 v = f;
-            for (int d = 1; (d << a.log2p) < 32; d <<= 1) {
-                const float4 o = shfl4(v, (lane - (d << a.log2p)) & 31);
-                if (run >= d && lane >= (d << a.log2p)) v = compose(o, v);
-            }
-            const float4 o = shfl4(v, (lane - P) & 31);
-            excl = run >= 1 && lane >= P ? o : identity4();
-            if (lane >= 32 - P) sh.run[wave & 1][warp][cp] = v;
-        }
-        const float4 rincl = lane_scan<true>(r, P, lane);
-        const float4 rexcl = lane_exclusive<true>(rincl, P, lane);
-        if (lane < P) rev[wave & 1][warp][cp] = rincl;
-        __syncthreads();
-        float4 before = identity4();
-        const int w0 = warp - warp % wpc;
-        for (int w = w0; w < warp; ++w) before = compose(before, sh.run[wave & 1][w][cp]);
-        h = apply(compose(before, excl), h);
-        float4 after = identity4(), total = identity4();
-#pragma unroll
-        for (int w = kWarps - 1; w >= 0; --w) {
-            if (w == warp) after = total;
-            total = compose(total, rev[wave & 1][w][cp]);
-        }
-        after = compose(after, rexcl);
-        float2 C;
-        if (a.nseg > 1) {
-            float4 pre, all;
-            exchange(total, a.agg + (int64_t)chain * 2 * a.nseg * 32, a.flag + (int64_t)chain * a.nseg, wave, seg,
-                     a.nseg, min(a.nseg, a.ntiles - wave * a.nseg), P, cp, sh, &pre, &all);
-            C = apply(after, apply(pre, carry));
-            carry = apply(all, carry);
-        } else {
-            C = apply(after, carry);
-            carry = apply(total, carry);
-        }
-        float2 hp[S];
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const float2 x = Pair<T>::value(xs[i]);
-            hp[i] = h;
-            h.x = kLeak ? fmaf(b[i].x, x.x - h.x, h.x) : fmaf(-b[i].x, h.x, h.x + x.x);
-            h.y = kLeak ? fmaf(b[i].y, x.y - h.y, h.y) : fmaf(-b[i].y, h.y, h.y + x.y);
-        }
-#pragma unroll
-        for (int i = S - 1; i >= 0; --i) {
-            const float2 x = Pair<T>::value(xs[i]), d = Pair<T>::value(ds[i]);
-            const float gx = d.x + C.x, gy = d.y + C.y;
-            C.x = fmaf(-b[i].x, gx, gx);                // a G
-            C.y = fmaf(-b[i].y, gy, gy);
-            if (on && t0 + i < a.L) {
-                const bool ok = t0 + i < len;
-                const float2 zero = make_float2(0.f, 0.f);
-                float2 vx, vg;
-                vx.x = kLeak ? b[i].x * gx : gx;
-                vx.y = kLeak ? b[i].y * gy : gy;
-                vg.x = C.x * b[i].x * (kLeak ? hp[i].x - x.x : hp[i].x);
-                vg.y = C.y * b[i].y * (kLeak ? hp[i].y - x.y : hp[i].y);
-                Pair<T>::store(dxp + (int64_t)(t0 + i) * a.dx_l, ok ? vx : zero);
-                Pair<T>::store(dgp + (int64_t)(t0 + i) * a.dg_l, ok ? vg : zero);
-            }
-        }
-        if (tile == 0 && a.state_out && on && sc == 0)
-            *reinterpret_cast<float2 *>(a.state_out + (int64_t)row * a.D + c) = C;
+// -b = -1 / (1 + e^g); g = +inf gives -0, -inf gives -1.
+template <typename T>
+__device__ __forceinline__ f32x2 minus_rest(f32x2 g) {
+    float2 e;
+    if constexpr (sizeof(T) == 2) {
+        const float2 p = unpack(mul2(g, 0x3fb8aa3b3fb8aa3bull));       // log2(e)
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(p.x));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(p.y));
+    } else {
+        const float2 p = unpack(g);
+        e = make_float2(expf(p.x), expf(p.y));
     }
+    const float2 d = unpack(fma2(pack(e), kMinus, kMinus));
+    float2 r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(d.y));
+    return pack(r);
+}
+
+// One token: h - b (h - x) or (h + x) - b h; nb = -b.
+template <bool kLeak>
+__device__ __forceinline__ f32x2 advance(f32x2 h, f32x2 nb, f32x2 x) {
+    return kLeak ? fma2(nb, fma2(x, kMinus, h), h) : fma2(nb, h, add2(h, x));
+}
+
+// Resident CTAs per SM: what the rings leave room for.
+template <typename T>
+constexpr int kPerSm = sizeof(T) == 2 ? 2 : 1;
+
+// ----------------------------------------------------------------- forward
+template <typename T>
+constexpr int kFwdStages = sizeof(T) == 2 ? 4 : 5;
+template <typename T>
+using FwdRing = Ring<T, 2, kFwdStages<T>>;          // fields: x, g
+
+template <typename T, bool kLeak>
+__global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_forward(const ScanArgs<T> a) {
+    extern __shared__ __align__(16) unsigned char ring_mem[];
+    __shared__ Peers peers;
+    __shared__ float4 runs[2][kDataThreads];
+    __shared__ float2 states[2][kDataThreads];
+    const Where w = where(a);
+    constexpr int ST = kFwdStages<T>;
+    open_peers(peers, a.nseg);
+
+    if (w.warp == kDataThreads / 32) {
+        // Runs to states: lane (part, cp) holds runs 8 part .. 8 part + 7.
+        const int first = (w.lane / w.P) * 8 * w.P + w.cp;
+        float2 carry = make_float2(0.f, 0.f);
+        if (a.state_in && w.on) carry = *reinterpret_cast<const float2 *>(a.state_in + (int64_t)w.row * a.D + w.c);
+        bool gave_up = false;
+        for (int k = 0; k < w.n; ++k) {
+            const int par = k & 1, tile = k * a.nseg + w.seg;
+            bar_sync(kBarRuns + par);
+            float4 f = identity4();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f = compose(f, runs[par][first + j * w.P]);
+            const float4 incl = lane_scan<false>(f, w.P, w.lane);
+            const float4 excl = lane_exclusive<false>(incl, w.P, w.lane);
+            const float4 total = shfl4(incl, 32 - w.P + w.cp);
+            float2 h = carry;
+            if (a.nseg > 1) {
+                float4 pre, all;
+                exchange(total, peers, k, w.seg, a.nseg, w.P, w.cp, gave_up, &pre, &all);
+                h = apply(pre, carry);
+                carry = apply(all, carry);
+            } else {
+                carry = apply(total, carry);
+            }
+            h = apply(excl, h);
+            const int t0 = tile * w.tile_tokens + (w.lane / w.P) * kChunk;
+            if (a.saved && w.on && t0 < a.L)
+                *reinterpret_cast<float2 *>(a.saved + ((int64_t)w.row * a.nchunks + t0 / kChunk) * a.D + w.c) = h;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                states[par][first + j * w.P] = h;
+                h = apply(runs[par][first + j * w.P], h);
+            }
+            bar_arrive(kBarStates + par);
+        }
+        // Every member holds the same carry.  state_out may be state_in: all members have read it.
+        close_peers(a.nseg);
+        if (a.state_out && w.on && w.lane < w.P && w.seg == 0)
+            *reinterpret_cast<float2 *>(a.state_out + (int64_t)w.row * a.D + w.c) = carry;
+        return;
+    }
+
+    const FwdRing<T> ring(w, ring_mem, a.log2p, w.c - 2 * w.cp);
+    const bool on = ring.c < a.D;
+    const T *xp = a.x + w.row * a.x_b + (on ? ring.c : 0), *gp = a.g + w.row * a.g_b + (on ? ring.c : 0);
+    T *yp = a.y + w.row * a.y_b + w.c;
+    auto copy = [&](int k) {
+        if (k < w.n) {
+            const int t0 = (k * a.nseg + w.seg) * w.tile_tokens;
+            ring.copy(k % ST, 0, xp, a.x_l, t0, w.len, on);
+            ring.copy(k % ST, 1, gp, a.g_l, t0, w.len, on);
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int k = 0; k < ST; ++k) copy(k);
+    f32x2 nb[kS], nb1[kS];
+    for (int k = 0; k <= w.n; ++k) {
+        if (k < w.n) {
+            // Copies are one group a tile: tile k is in once at most the groups after it are open.
+            if (k == 0) copies_wait<ST - 1>(); else copies_wait<ST - 2>();
+            const int st = k % ST, t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
+            const bool full = t0 + kS <= w.len;
+            f32x2 A = kOne, H = 0;
+#pragma unroll
+            for (int i = 0; i < kS; ++i) {
+                nb1[i] = minus_rest<T>(ring.value(st, 1, i));
+                if (!full && t0 + i >= w.len) nb1[i] = 0;       // past the end: the identity (x is 0 there)
+                A = fma2(nb1[i], A, A);
+                H = advance<kLeak>(H, nb1[i], ring.value(st, 0, i));
+            }
+            const float2 fa = unpack(A), fh = unpack(H);
+            runs[k & 1][threadIdx.x] = make_float4(fa.x, fa.y, fh.x, fh.y);
+            bar_arrive(kBarRuns + (k & 1));
+        }
+        if (k > 0) {
+            const int q = k - 1, st = q % ST, t0 = (q * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
+            bar_sync(kBarStates + (q & 1));
+            f32x2 h = pack(states[q & 1][threadIdx.x]);
+            T *out = yp + (int64_t)t0 * a.y_l;
+            if (t0 + kS <= w.len) {
+#pragma unroll
+                for (int i = 0; i < kS; ++i) {
+                    h = advance<kLeak>(h, nb[i], ring.value(st, 0, i));
+                    if (w.on) Pair<T>::store(out, unpack(h));
+                    out += a.y_l;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kS; ++i) {
+                    h = advance<kLeak>(h, nb[i], ring.value(st, 0, i));
+                    if (w.on && t0 + i < a.L) Pair<T>::store(out, t0 + i < w.len ? unpack(h) : make_float2(0.f, 0.f));
+                    out += a.y_l;
+                }
+            }
+            __syncwarp();
+            copy(k + ST - 1);       // into the stage that the second pass has just left
+        }
+#pragma unroll
+        for (int i = 0; i < kS; ++i) nb[i] = nb1[i];
+    }
+    close_peers(a.nseg);
+}
+
+// ---------------------------------------------------------------- backward
+template <typename T>
+constexpr int kBwdStages = 3;
+template <typename T>
+using BwdRing = Ring<T, 3, kBwdStages<T>>;          // fields: x, g, dy
+
+template <typename T, bool kLeak>
+__global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_backward(const ScanArgs<T> a) {
+    extern __shared__ __align__(16) unsigned char ring_mem[];
+    // Gradients are carried negated: with -b at hand, b G = (-b)(-G) needs no sign.
+    __shared__ Peers peers;
+    __shared__ float4 runs[2][kDataThreads];        // (A, H) of a run
+    __shared__ float2 ends[2][kDataThreads];        // its -C from a zero C after it; then its -C
+    __shared__ float2 states[2][kDataThreads];
+    const Where w = where(a);
+    constexpr int ST = kBwdStages<T>;
+    open_peers(peers, a.nseg);
+
+    if (w.warp == kDataThreads / 32) {
+        // A lane's 8 runs are one chunk: their states follow from the chunk's saved state.
+        const int part = w.lane / w.P, first = part * 8 * w.P + w.cp;
+        float2 carry = make_float2(0.f, 0.f);       // -C after the wave
+        if (a.state_in && w.on) {
+            carry = *reinterpret_cast<const float2 *>(a.state_in + (int64_t)w.row * a.D + w.c);
+            carry = make_float2(-carry.x, -carry.y);
+        }
+        auto saved_at = [&](int k) {
+            const int t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens + part * kChunk;
+            if (k >= w.n || !w.on || t0 < 0 || t0 >= w.len) return make_float2(0.f, 0.f);
+            return __ldg(reinterpret_cast<const float2 *>(a.saved + ((int64_t)w.row * a.nchunks + t0 / kChunk) * a.D + w.c));
+        };
+        bool gave_up = false;
+        float2 next = saved_at(0);
+        for (int k = 0; k < w.n; ++k) {
+            const int par = k & 1;
+            float2 h = next;
+            next = saved_at(k + 1);
+            bar_sync(kBarRuns + par);
+            auto reverse_run = [&](int j) {
+                const float2 A = *reinterpret_cast<const float2 *>(&runs[par][first + j * w.P]);
+                const float2 e = ends[par][first + j * w.P];
+                return make_float4(A.x, A.y, e.x, e.y);
+            };
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                states[par][first + j * w.P] = h;
+                h = apply(runs[par][first + j * w.P], h);
+            }
+            float4 f = identity4();
+#pragma unroll
+            for (int j = 7; j >= 0; --j) f = compose(f, reverse_run(j));
+            const float4 incl = lane_scan<true>(f, w.P, w.lane);
+            const float4 excl = lane_exclusive<true>(incl, w.P, w.lane);
+            const float4 total = shfl4(incl, w.cp);
+            float2 C = carry;
+            if (a.nseg > 1) {
+                float4 pre, all;
+                exchange(total, peers, k, w.seg, a.nseg, w.P, w.cp, gave_up, &pre, &all);
+                C = apply(pre, carry);
+                carry = apply(all, carry);
+            } else {
+                carry = apply(total, carry);
+            }
+            C = apply(excl, C);
+#pragma unroll
+            for (int j = 7; j >= 0; --j) {
+                const float4 r = reverse_run(j);
+                ends[par][first + j * w.P] = C;
+                C = apply(r, C);
+            }
+            bar_arrive(kBarStates + par);
+        }
+        close_peers(a.nseg);
+        if (a.state_out && w.on && w.lane < w.P && w.seg == 0)
+            *reinterpret_cast<float2 *>(a.state_out + (int64_t)w.row * a.D + w.c) = make_float2(-carry.x, -carry.y);
+        return;
+    }
+
+    const BwdRing<T> ring(w, ring_mem, a.log2p, w.c - 2 * w.cp);
+    const bool on = ring.c < a.D;
+    const int cc = on ? ring.c : 0;
+    const T *xp = a.x + w.row * a.x_b + cc, *gp = a.g + w.row * a.g_b + cc, *dp = a.dy + w.row * a.dy_b + cc;
+    T *dxp = a.dx + w.row * a.dx_b + w.c, *dgp = a.dg + w.row * a.dg_b + w.c;
+    auto copy = [&](int k) {
+        if (k < w.n) {
+            const int t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens;
+            ring.copy(k % ST, 0, xp, a.x_l, t0, w.len, on);
+            ring.copy(k % ST, 1, gp, a.g_l, t0, w.len, on);
+            ring.copy(k % ST, 2, dp, a.dy_l, t0, w.len, on);
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int k = 0; k < ST; ++k) copy(k);
+    f32x2 nb[kS], nb1[kS];
+    for (int k = 0; k <= w.n; ++k) {
+        if (k < w.n) {
+            if (k == 0) copies_wait<ST - 1>(); else copies_wait<ST - 2>();
+            const int st = k % ST, t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens + w.sc * kS;
+            const bool full = t0 >= 0 && t0 + kS <= w.len;
+            f32x2 A = kOne, H = 0, R = 0;
+#pragma unroll
+            for (int i = 0; i < kS; ++i) {
+                nb1[i] = minus_rest<T>(ring.value(st, 1, i));
+                if (!full && (t0 < 0 || t0 + i >= w.len)) nb1[i] = 0;
+                A = fma2(nb1[i], A, A);
+                H = advance<kLeak>(H, nb1[i], ring.value(st, 0, i));
+            }
+#pragma unroll
+            for (int i = kS - 1; i >= 0; --i) {
+                const f32x2 G = fma2(ring.value(st, 2, i), kMinus, R);
+                R = fma2(nb1[i], G, G);
+            }
+            const float2 fa = unpack(A), fh = unpack(H);
+            runs[k & 1][threadIdx.x] = make_float4(fa.x, fa.y, fh.x, fh.y);
+            ends[k & 1][threadIdx.x] = unpack(R);
+            bar_arrive(kBarRuns + (k & 1));
+        }
+        if (k > 0) {
+            const int q = k - 1, st = q % ST, t0 = (a.ntiles - 1 - (q * a.nseg + w.seg)) * w.tile_tokens + w.sc * kS;
+            bar_sync(kBarStates + (q & 1));
+            f32x2 h = pack(states[q & 1][threadIdx.x]), C = pack(ends[q & 1][threadIdx.x]);
+            f32x2 v[kS];                                // h_{t-1} - x or h_{t-1}
+#pragma unroll
+            for (int i = 0; i < kS; ++i) {
+                const f32x2 x = ring.value(st, 0, i);
+                v[i] = kLeak ? fma2(x, kMinus, h) : h;
+                h = advance<kLeak>(h, nb[i], x);
+            }
+            const bool full = t0 >= 0 && t0 + kS <= w.len;
+            T *ox = dxp + (int64_t)(t0 + kS - 1) * a.dx_l, *og = dgp + (int64_t)(t0 + kS - 1) * a.dg_l;
+#pragma unroll
+            for (int i = kS - 1; i >= 0; --i) {
+                const f32x2 G = fma2(ring.value(st, 2, i), kMinus, C);
+                C = fma2(nb[i], G, G);                  // a G
+                float2 vx = unpack(mul2(kLeak ? nb[i] : kMinus, G));
+                float2 vg = unpack(mul2(mul2(C, nb[i]), v[i]));
+                if (!full && t0 + i >= w.len) vx = vg = make_float2(0.f, 0.f);
+                if (full ? w.on : w.on && t0 >= 0 && t0 + i < a.L) {
+                    Pair<T>::store(ox, vx);
+                    Pair<T>::store(og, vg);
+                }
+                ox -= a.dx_l;
+                og -= a.dg_l;
+            }
+            __syncwarp();
+            copy(k + ST - 1);
+        }
+#pragma unroll
+        for (int i = 0; i < kS; ++i) nb[i] = nb1[i];
+    }
+    close_peers(a.nseg);
 }
 
 // One token for each row: a thread per channel pair.  Bound by the launch up to a few
@@ -456,71 +660,79 @@ __global__ void __launch_bounds__(256) k_scan_step(const T *x, const T *g, T *y,
         const float2 gv = Pair<T>::value(*reinterpret_cast<const Raw *>(g + row * g_b + c));
         const float2 xv = Pair<T>::value(*reinterpret_cast<const Raw *>(x + row * x_b + c));
         float2 *sp = reinterpret_cast<float2 *>(state) + i;
-        float2 h = *sp;
-        const float bx = rest(gv.x), by = rest(gv.y);
-        h.x = kLeak ? fmaf(bx, xv.x - h.x, h.x) : fmaf(-bx, h.x, h.x + xv.x);
-        h.y = kLeak ? fmaf(by, xv.y - h.y, h.y) : fmaf(-by, h.y, h.y + xv.y);
+        const float2 h = unpack(advance<kLeak>(pack(*sp), minus_rest<T>(pack(gv)), pack(xv)));
         *sp = h;
         Pair<T>::store(y + row * y_b + c, h);
     }
     asm volatile("griddepcontrol.launch_dependents;" :::);
 }
 
+// Relative cost of a byte with rows of 4, 8, 16 and 32 channel pairs.
+constexpr double kRowCost[4] = {1.6, 1.25, 1.02, 1.0};
+
 struct ScanPlan {
-    int log2p, groups, tile, ntiles, nseg;
+    int log2p, groups, ntiles, nseg;
     int64_t chains;
 };
 
-// Resident CTAs of the scan kernels: two per SM (their launch bounds).
-ScanPlan scan_plan(int64_t B, int64_t L, int D, int run) {
-    ScanPlan p;
-    p.log2p = 2;
-    while (p.log2p < 5 && (2 << p.log2p) < D) ++p.log2p;
-    p.groups = (D + (2 << p.log2p) - 1) / (2 << p.log2p);
-    p.tile = (kThreads >> p.log2p) * run;
-    p.ntiles = (int)((L + p.tile - 1) / p.tile);
-    p.chains = B * p.groups;
-    // As many segments as keep every CTA resident, evened out over the waves.
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(p.ntiles, 2 * (int64_t)sm_count() / p.chains));
-    const int waves = (int)((p.ntiles + most - 1) / most);
-    p.nseg = (p.ntiles + waves - 1) / waves;
-    return p;
+// Channel pairs per CTA and segments per chain.  Time goes by rounds of resident CTAs,
+// a CTA's tiles and a few tiles' worth of start and end; rows of 64 bytes and less cost
+// more per byte (measured: see kRowCost).  The plan depends on the shape alone.
+ScanPlan scan_plan(int64_t B, int64_t L, int D, rlm_dtype dt) {
+    const int64_t slots = (dt == RLM_BF16 ? kPerSm<__nv_bfloat16> : kPerSm<float>) * (int64_t)sm_count();
+    ScanPlan best = {};
+    double best_cost = 0;
+    for (int lp = 5; lp >= 2; --lp) {
+        if (lp > 2 && (2 << (lp - 1)) >= D) continue;       // a narrower group already holds the row
+        ScanPlan p;
+        p.log2p = lp;
+        p.groups = (D + (2 << lp) - 1) / (2 << lp);
+        p.chains = B * p.groups;
+        const int tile = (kDataThreads >> lp) * kS;
+        p.ntiles = (int)((L + tile - 1) / tile);
+        for (p.nseg = 1; p.nseg <= kMaxSeg && p.nseg <= p.ntiles; p.nseg *= 2) {
+            // A cluster's CTAs sit in one GPC, which clusters do not fill evenly.
+            const int64_t room = p.nseg == 1 ? slots : slots * 27 / 32;
+            const int64_t rounds = (p.chains * p.nseg + room - 1) / room;
+            const int waves = (p.ntiles + p.nseg - 1) / p.nseg;
+            const double cost = (double)rounds * (waves + 4) * kRowCost[lp - 2];
+            if (best_cost == 0 || cost < best_cost * 0.999) {
+                best_cost = cost;
+                best = p;
+            }
+        }
+    }
+    return best;
 }
-
-size_t plan_ws_bytes(const ScanPlan &p) {
-    if (p.nseg < 2) return 0;
-    return (size_t)p.chains * p.nseg * (2 * 32 * sizeof(float4) + sizeof(unsigned));
-}
-
-int forward_run(rlm_dtype dt) { return dt == RLM_BF16 ? kFwdRun<__nv_bfloat16> : kFwdRun<float>; }
 
 template <typename T>
-cudaError_t launch_scan(void (*kernel)(const ScanArgs<T>), ScanArgs<T> &a, const ScanPlan &p, void *ws,
+cudaError_t launch_scan(void (*kernel)(const ScanArgs<T>), int smem, ScanArgs<T> &a, const ScanPlan &p,
                         cudaStream_t st) {
     a.groups = p.groups;
     a.log2p = p.log2p;
     a.nseg = p.nseg;
     a.ntiles = p.ntiles;
     a.nchunks = (a.L + kChunk - 1) / kChunk;
-    const dim3 grid((unsigned)(p.chains * p.nseg));
-    count_launches(1);
-    if (p.nseg < 2) {
-        a.agg = nullptr;
-        a.flag = nullptr;
-        kernel<<<grid, kThreads, 0, st>>>(a);
-        return cudaGetLastError();
-    }
-    a.agg = static_cast<float4 *>(ws);
-    a.flag = reinterpret_cast<unsigned *>(a.agg + (size_t)p.chains * p.nseg * 2 * 32);
-    cudaError_t e = cudaMemsetAsync(a.flag, 0, (size_t)p.chains * p.nseg * sizeof(unsigned), st);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    void *args[] = {&a};
-    return cudaLaunchCooperativeKernel(reinterpret_cast<const void *>(kernel), grid, dim3(kThreads), args, 0, st);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p.chains * p.nseg));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.nseg;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    count_launches(1);
+    return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <typename T>
 cudaError_t forward_t(const rlm_strided &x, const rlm_strided &g, const rlm_strided &y, bool leak, const float *sin,
-                      float *sout, float *saved, const int *lengths, void *ws, cudaStream_t st) {
+                      float *sout, float *saved, const int *lengths, cudaStream_t st) {
     ScanArgs<T> a = {};
     a.x = static_cast<const T *>(x.ptr);
     a.g = static_cast<const T *>(g.ptr);
@@ -533,14 +745,14 @@ cudaError_t forward_t(const rlm_strided &x, const rlm_strided &g, const rlm_stri
     a.lengths = lengths;
     a.L = (int)x.L;
     a.D = (int)x.D;
-    return launch_scan(leak ? k_scan_forward<T, true> : k_scan_forward<T, false>, a,
-                       scan_plan(x.B, x.L, (int)x.D, kFwdRun<T>), ws, st);
+    return launch_scan(leak ? k_scan_forward<T, true> : k_scan_forward<T, false>, FwdRing<T>::kBytes, a,
+                       scan_plan(x.B, x.L, (int)x.D, x.dtype), st);
 }
 
 template <typename T>
 cudaError_t backward_t(const rlm_strided &dy, const rlm_strided &x, const rlm_strided &g, const float *saved, bool leak,
                        const float *dsout, const rlm_strided &dx, const rlm_strided &dg, float *dsin,
-                       const int *lengths, void *ws, cudaStream_t st) {
+                       const int *lengths, cudaStream_t st) {
     ScanArgs<T> a = {};
     a.x = static_cast<const T *>(x.ptr);
     a.g = static_cast<const T *>(g.ptr);
@@ -556,8 +768,8 @@ cudaError_t backward_t(const rlm_strided &dy, const rlm_strided &x, const rlm_st
     a.lengths = lengths;
     a.L = (int)x.L;
     a.D = (int)x.D;
-    return launch_scan(leak ? k_scan_backward<T, true> : k_scan_backward<T, false>, a,
-                       scan_plan(x.B, x.L, (int)x.D, kBwdRun), ws, st);
+    return launch_scan(leak ? k_scan_backward<T, true> : k_scan_backward<T, false>, BwdRing<T>::kBytes, a,
+                       scan_plan(x.B, x.L, (int)x.D, x.dtype), st);
 }
 
 template <typename T>
@@ -582,24 +794,20 @@ cudaError_t step_t(const rlm_strided &x, const rlm_strided &g, const rlm_strided
 
 }  // namespace
 
-size_t scan_ws_bytes(int64_t B, int64_t L, int D, rlm_dtype dt) {
-    return std::max(plan_ws_bytes(scan_plan(B, L, D, forward_run(dt))), plan_ws_bytes(scan_plan(B, L, D, kBwdRun)));
-}
-
 cudaError_t scan_forward(const rlm_strided &x, const rlm_strided &g, const rlm_strided &y, bool leak,
-                         const float *state_in, float *state_out, float *saved, const int *lengths, void *ws,
+                         const float *state_in, float *state_out, float *saved, const int *lengths,
                          cudaStream_t st) {
     if (x.dtype == RLM_BF16)
-        return forward_t<__nv_bfloat16>(x, g, y, leak, state_in, state_out, saved, lengths, ws, st);
-    return forward_t<float>(x, g, y, leak, state_in, state_out, saved, lengths, ws, st);
+        return forward_t<__nv_bfloat16>(x, g, y, leak, state_in, state_out, saved, lengths, st);
+    return forward_t<float>(x, g, y, leak, state_in, state_out, saved, lengths, st);
 }
 
 cudaError_t scan_backward(const rlm_strided &dy, const rlm_strided &x, const rlm_strided &g, const float *saved,
                           bool leak, const float *d_state_out, const rlm_strided &dx, const rlm_strided &dg,
-                          float *d_state_in, const int *lengths, void *ws, cudaStream_t st) {
+                          float *d_state_in, const int *lengths, cudaStream_t st) {
     if (x.dtype == RLM_BF16)
-        return backward_t<__nv_bfloat16>(dy, x, g, saved, leak, d_state_out, dx, dg, d_state_in, lengths, ws, st);
-    return backward_t<float>(dy, x, g, saved, leak, d_state_out, dx, dg, d_state_in, lengths, ws, st);
+        return backward_t<__nv_bfloat16>(dy, x, g, saved, leak, d_state_out, dx, dg, d_state_in, lengths, st);
+    return backward_t<float>(dy, x, g, saved, leak, d_state_out, dx, dg, d_state_in, lengths, st);
 }
 
 cudaError_t scan_step(const rlm_strided &x, const rlm_strided &g, const rlm_strided &y, bool leak, float *state,

@@ -110,11 +110,6 @@ rlm_status check_apart(std::initializer_list<Region> outs, std::initializer_list
 
 extern "C" {
 
-size_t rlm_scan_workspace_size(int64_t B, int64_t L, int D, rlm_dtype dtype) {
-    if (check_shape(B, L, D, "shape") != RLM_OK || (dtype != RLM_F32 && dtype != RLM_BF16)) return 0;
-    return scan_ws_bytes(B, L, D, dtype);
-}
-
 size_t rlm_scan_saved_size(int64_t B, int64_t L, int D) {
     if (check_shape(B, L, D, "shape") != RLM_OK) return 0;
     return (size_t)B * (size_t)((L + RLM_SCAN_CHUNK - 1) / RLM_SCAN_CHUNK) * (size_t)D * sizeof(float);
@@ -140,8 +135,8 @@ rlm_status rlm_scan_prefill(const rlm_strided *x_, const rlm_strided *g_, int le
         return fail(RLM_ERR_INVALID_ARG, "state_in and state_out overlap without being the same buffer");
     if (saved && ((state_in && overlap(saved, vb, state_in, sb)) || (state_out && overlap(saved, vb, state_out, sb))))
         return fail(RLM_ERR_INVALID_ARG, "saved overlaps state_in or state_out");
-    if ((s = check_workspace(ln, scan_ws_bytes(x.B, x.L, (int)x.D, x.dtype))) != RLM_OK) return s;
-    const cudaError_t e = scan_forward(x, g, y, leak != 0, state_in, state_out, saved, lengths, ln->workspace,
+    if (!ln) return fail(RLM_ERR_INVALID_ARG, "launch is NULL");
+    const cudaError_t e = scan_forward(x, g, y, leak != 0, state_in, state_out, saved, lengths,
                                        static_cast<cudaStream_t>(ln->stream));
     if (e != cudaSuccess) return cuda_fail(e, "rlm_scan_prefill launch");
     return RLM_OK;
@@ -174,9 +169,9 @@ rlm_status rlm_scan_backward(const rlm_strided *dy_, const rlm_strided *x_, cons
         return fail(RLM_ERR_INVALID_ARG, "d_state_in overlaps saved");
     if (d_state_in && d_state_out && d_state_in != d_state_out && overlap(d_state_in, sb, d_state_out, sb))
         return fail(RLM_ERR_INVALID_ARG, "d_state_in and d_state_out overlap without being the same buffer");
-    if ((s = check_workspace(ln, scan_ws_bytes(x.B, x.L, (int)x.D, x.dtype))) != RLM_OK) return s;
+    if (!ln) return fail(RLM_ERR_INVALID_ARG, "launch is NULL");
     const cudaError_t e = scan_backward(dy, x, g, saved, leak != 0, d_state_out, dx, dg, d_state_in, lengths,
-                                        ln->workspace, static_cast<cudaStream_t>(ln->stream));
+                                        static_cast<cudaStream_t>(ln->stream));
     if (e != cudaSuccess) return cuda_fail(e, "rlm_scan_backward launch");
     return RLM_OK;
 }

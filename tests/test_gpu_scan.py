@@ -162,7 +162,7 @@ def test_extreme_gates():
 
 @pytest.mark.parametrize("B,L,D", [(1, 4096, 64), (4, 4096, 256), (1, 40000, 8)])
 def test_repeats_bit_for_bit_and_on_another_stream(B, L, D):
-    """Segmented launches: the exchange's order is fixed, and its flags need no state from call to call."""
+    """Segmented launches: the exchange's order is fixed."""
     (x, g, dy), rng = fields(B, L, D, "bf16", 8)
     dh = torch.from_numpy(rng.standard_normal((B, D))).float().cuda()
     first = run(x, g, dy, True, None, dh, None)
@@ -176,15 +176,13 @@ def test_repeats_bit_for_bit_and_on_another_stream(B, L, D):
 
 
 def test_graph_replays():
-    """A captured call may be replayed with new inputs: its flags are cleared in the graph."""
+    """A captured call may be replayed with new inputs."""
     (x, g, dy), _ = fields(1, 4096, 64, "f32", 8)
-    y, ws = torch.empty_like(x), torch.empty(rlm.rlm_scan_workspace_size(1, 4096, 64, torch.float32), dtype=torch.uint8,
-                                             device="cuda")
-    assert ws.numel() > 0
-    rlm.rlm_scan_prefill(x, g, y, workspace=ws)
+    y = torch.empty_like(x)
+    rlm.rlm_scan_prefill(x, g, y)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        rlm.rlm_scan_prefill(x, g, y, workspace=ws)
+        rlm.rlm_scan_prefill(x, g, y)
     for k in range(3):
         x.copy_(torch.randn_like(x))
         graph.replay()

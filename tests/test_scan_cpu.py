@@ -32,7 +32,8 @@ def launch(nbytes=1 << 30):
 def prefill(lib, x=None, g=None, y=None, sin=FAKE + 10 * GB, sout=FAKE + 11 * GB, saved=FAKE + 12 * GB, lengths=None,
             ln=None):
     f = lambda v, k: field(k) if v is None else v
-    return lib.rlm_scan_prefill(ref(f(x, 0)), ref(f(g, 1)), 1, sin, ref(f(y, 2)), sout, saved, lengths, ln or launch())
+    return lib.rlm_scan_prefill(ref(f(x, 0)), ref(f(g, 1)), 1, sin, ref(f(y, 2)), sout, saved, lengths,
+                                launch() if ln is None else ln)
 
 
 BAD = {
@@ -55,7 +56,7 @@ BAD = {
     "states overlap": dict(sin=FAKE + 10 * GB, sout=FAKE + 10 * GB + 256),
     "saved over state": dict(saved=FAKE + 11 * GB),
     "lengths misaligned": dict(lengths=FAKE + 2),
-    "small workspace": dict(ln=launch(16)),
+    "no launch": dict(ln=ctypes.POINTER(rlm._Launch)()),
 }
 
 
@@ -74,7 +75,7 @@ def test_limits(lib):
 def backward(lib, dy=None, x=None, g=None, dx=None, dg=None, saved=FAKE + 12 * GB, dsin=FAKE + 13 * GB):
     f = lambda v, k: field(k) if v is None else v
     return lib.rlm_scan_backward(ref(f(dy, 0)), ref(f(x, 1)), ref(f(g, 2)), saved, 1, None, ref(f(dx, 3)),
-                                 ref(f(dg, 4)), dsin, None, launch(16))
+                                 ref(f(dg, 4)), dsin, None, ctypes.POINTER(rlm._Launch)())
 
 
 def test_backward_refusals(lib):
@@ -82,9 +83,9 @@ def test_backward_refusals(lib):
            dict(dg=field(4, dt=rlm.RLM_F32)), dict(dx=field(3, sl=0, sb=0))]
     for kw in bad:
         assert backward(lib, **kw) == rlm.RLM_ERR_INVALID_ARG, kw
-    # Two halves of one buffer are apart: the call gets as far as its workspace.
+    # Two halves of one buffer are apart: the call gets as far as its launch context.
     assert backward(lib, dx=field(3, sl=128), dg=field(3, sl=128, off=128)) == rlm.RLM_ERR_INVALID_ARG
-    assert b"workspace" in lib.rlm_last_error()
+    assert b"launch is NULL" in lib.rlm_last_error()
 
 
 def test_decode_refusals(lib):
@@ -100,6 +101,3 @@ def test_decode_refusals(lib):
 def test_sizes(lib):
     assert rlm.rlm_scan_saved_size(2, 65, 8) == 2 * 2 * 8 * 4
     assert rlm.rlm_scan_saved_size(0, 65, 8) == 0
-    assert rlm.rlm_scan_workspace_size(1, 1, 8, rlm.RLM_F32) == 0
-    assert rlm.rlm_scan_workspace_size(4096, 1000, 512, rlm.RLM_BF16) == 0      # channels fill the GPU
-    assert rlm.rlm_scan_workspace_size(1, 32768, 256, rlm.RLM_BF16) > 0
