@@ -88,7 +88,7 @@ struct ScanArgs {
     float *state_out;           // forward: h_{L-1}; backward: dl/dh_{-1}; nullable
     float *saved;               // [B][ceil(L / kChunk)][D]: h before each chunk (forward: nullable output)
     const int *lengths;         // nullable, [B]
-    int L, D, groups, log2p, nseg, ntiles, nchunks;
+    int L, D, groups, nseg, ntiles, nchunks;
 };
 
 // Two channels' values in one 64-bit register.
@@ -248,82 +248,87 @@ struct Where {
     bool on;
 };
 
-template <typename T>
+template <int kLog2P, typename T>
 __device__ __forceinline__ Where where(const ScanArgs<T> &a) {
     Where w;
     const int tid = threadIdx.x;
     w.lane = tid & 31;
     w.warp = tid >> 5;
-    w.P = 1 << a.log2p;
+    w.P = 1 << kLog2P;
     w.cp = tid & (w.P - 1);
-    w.sc = tid >> a.log2p;
+    w.sc = tid >> kLog2P;
     const int chain = blockIdx.x / a.nseg;          // a cluster is one chain
     w.seg = blockIdx.x - chain * a.nseg;
     w.row = chain / a.groups;
     w.c = (chain - w.row * a.groups) * 2 * w.P + 2 * w.cp;
     w.on = w.c < a.D;
-    w.tile_tokens = (kDataThreads >> a.log2p) * kS;
+    w.tile_tokens = (kDataThreads >> kLog2P) * kS;
     w.len = a.lengths ? min(max(__ldg(a.lengths + w.row), 0), a.L) : a.L;
     w.n = (a.ntiles + a.nseg - 1) / a.nseg;         // waves (in the last one, tiles past the end do nothing)
     return w;
 }
 
-// A warp's ring of tiles: kFields fields, (32 / P) runs of kS rows, each run a row's
-// size further on so that the runs' rows fall into different banks.
-template <typename T, int kFields, int kStages>
+// A warp's ring of tiles: kFields fields, 32 / P runs of kS rows, each run a row's size
+// further on so that the runs' rows fall into different banks.
+template <typename T, int kFields, int kStages, int kLog2P>
 struct Ring {
-    static constexpr int kFieldBytes = 32 * 2 * (int)sizeof(T) * (kS + 1);
-    static constexpr int kWarpBytes = kFields * kStages * kFieldBytes;
+    static constexpr int kRowBytes = 2 * (int)sizeof(T) << kLog2P;
+    static constexpr int kRunBytes = (kS + 1) * kRowBytes;
+    static constexpr int kFieldBytes = (32 >> kLog2P) * kRunBytes;
+    static constexpr int kStageBytes = kFields * kFieldBytes;
+    static constexpr int kWarpBytes = kStages * kStageBytes;
     static constexpr int kBytes = kWarpBytes * (kDataThreads / 32);
-    static constexpr int kCopies = 2 * (int)sizeof(T) * kS * 32 / (16 * 32);    // 16-byte copies a lane, a field
-    uint32_t base;              // shared address of the warp's ring
-    uint32_t dst[kCopies];      // a lane's copies within a field
-    int row0, rows_apart;       // token (within the warp's rows) of the first copy; rows between copies
-    int c;                      // its first channel
-    int warp_t;                 // the warp's first token within the tile
-    uint32_t own;               // where a thread's own values start within a field
-    int row_bytes;
+    static constexpr int kPerRow = kRowBytes / 16;          // 16-byte copies a row
+    static constexpr int kRows = (32 >> kLog2P) * kS;       // a warp's rows (tokens) of a tile
+    static constexpr int kCopies = kRows * kPerRow / 32;    // copies a lane, a field
+    static constexpr int kApart = 32 / kPerRow;             // rows between a lane's copies
+    uint32_t base, dst, own;    // shared addresses: the warp's ring; a lane's first copy, its own values in a field
+    int row, c;                 // row and channel of a lane's first copy
 
-    __device__ __forceinline__ Ring(const Where &w, const void *smem, int log2p, int c0) {
-        row_bytes = 2 * (int)sizeof(T) << log2p;
+    __device__ __forceinline__ Ring(const Where &w, const void *smem) {
         base = (uint32_t)__cvta_generic_to_shared(smem) + w.warp * kWarpBytes;
-        const int per_row = row_bytes / 16;
-        row0 = w.lane / per_row;
-        rows_apart = 32 / per_row;
-        const int col = w.lane - row0 * per_row;
-        c = c0 + col * (16 / (int)sizeof(T));
+        const int r = w.lane / kPerRow, col = w.lane % kPerRow;
+        dst = base + place(r) + col * 16;
+        row = w.warp * kRows + r;
+        c = w.c - 2 * w.cp + col * (16 / (int)sizeof(T));
+        own = base + (w.lane >> kLog2P) * kRunBytes + w.cp * 2 * (int)sizeof(T);
+    }
+    static __host__ __device__ constexpr int place(int r) { return (r / kS) * kRunBytes + (r % kS) * kRowBytes; }
+    // Copies one field of the tile from token t0 on; p: the batch row's token 0 at the lane's channel.
+    __device__ __forceinline__ void copy(int stage, int f, const T *p, int64_t stride, int t0, int tokens, int len,
+                                         bool on) const {
+        const uint32_t to = dst + stage * kStageBytes + f * kFieldBytes;
+        const T *src = p + (int64_t)(t0 + row) * stride;
+        if (on && t0 >= 0 && t0 + tokens <= len) {
 #pragma unroll
-        for (int k = 0; k < kCopies; ++k) {
-            const int r = row0 + k * rows_apart;
-            dst[k] = (r / kS) * (kS + 1) * row_bytes + (r % kS) * row_bytes + col * 16;
-        }
-        warp_t = w.warp * (32 >> log2p) * kS;
-        own = (w.lane >> log2p) * (kS + 1) * row_bytes + w.cp * 2 * (int)sizeof(T);
-    }
-    __device__ __forceinline__ uint32_t field(int stage, int f) const {
-        return base + (stage * kFields + f) * kFieldBytes;
-    }
-    // Copies one field of a tile; p: (row 0 of the batch row, the lane's first channel).
-    __device__ __forceinline__ void copy(int stage, int f, const T *p, int64_t stride, int t0, int len, bool on) const {
-        const uint32_t to = field(stage, f);
+            for (int k = 0; k < kCopies; ++k) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + place(k * kApart)), "l"(src)
+                             : "memory");
+                src += kApart * stride;
+            }
+        } else {
 #pragma unroll
-        for (int k = 0; k < kCopies; ++k) {
-            const int t = t0 + warp_t + row0 + k * rows_apart;
-            const bool ok = on && t >= 0 && t < len;
-            const T *src = ok ? p + (int64_t)t * stride : p;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + dst[k]), "l"(src), "r"(ok ? 16 : 0)
-                         : "memory");
+            for (int k = 0; k < kCopies; ++k) {
+                const int t = t0 + row + k * kApart;
+                const bool ok = on && t >= 0 && t < len;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + place(k * kApart)),
+                             "l"(ok ? src : p), "r"(ok ? 16 : 0)
+                             : "memory");
+                src += kApart * stride;
+            }
         }
     }
+    // A thread's channel pair of token i of its run.
     __device__ __forceinline__ f32x2 value(int stage, int f, int i) const {
-        const uint32_t at = field(stage, f) + own + i * row_bytes;
+        const uint32_t at = own + stage * kStageBytes;
+        const int off = f * kFieldBytes + i * kRowBytes;
         if constexpr (sizeof(T) == 2) {
             uint32_t r;
-            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(at));
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(at + off));
             return pack(Pair<T>::value(r));
         } else {
             f32x2 r;
-            asm volatile("ld.shared.b64 %0, [%1];" : "=l"(r) : "r"(at));
+            asm volatile("ld.shared.b64 %0, [%1];" : "=l"(r) : "r"(at + off));
             return r;
         }
     }
@@ -360,6 +365,22 @@ __device__ __forceinline__ f32x2 advance(f32x2 h, f32x2 nb, f32x2 x) {
     return kLeak ? fma2(nb, fma2(x, kMinus, h), h) : fma2(nb, h, add2(h, x));
 }
 
+// first(0), first(1), second(0), first(2), second(1), ...: each pass's -b in one of two
+// register arrays.
+template <typename First, typename Second>
+__device__ __forceinline__ void two_passes(int n, First first, Second second) {
+    f32x2 even[kS], odd[kS];
+    first(0, even);
+    for (int k = 1;; k += 2) {
+        if (k < n) first(k, odd);
+        second(k - 1, even);
+        if (k >= n) return;
+        if (k + 1 < n) first(k + 1, even);
+        second(k, odd);
+        if (k + 1 >= n) return;
+    }
+}
+
 // Resident CTAs per SM: what the rings leave room for.
 template <typename T>
 constexpr int kPerSm = sizeof(T) == 2 ? 2 : 1;
@@ -367,16 +388,16 @@ constexpr int kPerSm = sizeof(T) == 2 ? 2 : 1;
 // ----------------------------------------------------------------- forward
 template <typename T>
 constexpr int kFwdStages = sizeof(T) == 2 ? 4 : 5;
-template <typename T>
-using FwdRing = Ring<T, 2, kFwdStages<T>>;          // fields: x, g
+template <typename T, int kLog2P>
+using FwdRing = Ring<T, 2, kFwdStages<T>, kLog2P>;          // fields: x, g
 
-template <typename T, bool kLeak>
+template <typename T, bool kLeak, int kLog2P>
 __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_forward(const ScanArgs<T> a) {
     extern __shared__ __align__(16) unsigned char ring_mem[];
     __shared__ Peers peers;
     __shared__ float4 runs[2][kDataThreads];
     __shared__ float2 states[2][kDataThreads];
-    const Where w = where(a);
+    const Where w = where<kLog2P>(a);
     constexpr int ST = kFwdStages<T>;
     open_peers(peers, a.nseg);
 
@@ -422,75 +443,75 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_forward(const Scan
         return;
     }
 
-    const FwdRing<T> ring(w, ring_mem, a.log2p, w.c - 2 * w.cp);
+    const FwdRing<T, kLog2P> ring(w, ring_mem);
     const bool on = ring.c < a.D;
     const T *xp = a.x + w.row * a.x_b + (on ? ring.c : 0), *gp = a.g + w.row * a.g_b + (on ? ring.c : 0);
     T *yp = a.y + w.row * a.y_b + w.c;
     auto copy = [&](int k) {
         if (k < w.n) {
             const int t0 = (k * a.nseg + w.seg) * w.tile_tokens;
-            ring.copy(k % ST, 0, xp, a.x_l, t0, w.len, on);
-            ring.copy(k % ST, 1, gp, a.g_l, t0, w.len, on);
+            ring.copy(k % ST, 0, xp, a.x_l, t0, w.tile_tokens, w.len, on);
+            ring.copy(k % ST, 1, gp, a.g_l, t0, w.tile_tokens, w.len, on);
         }
         copies_commit();
     };
 #pragma unroll
     for (int k = 0; k < ST; ++k) copy(k);
-    f32x2 nb[kS], nb1[kS];
-    for (int k = 0; k <= w.n; ++k) {
-        if (k < w.n) {
-            // Copies are one group a tile: tile k is in once at most the groups after it are open.
-            if (k == 0) copies_wait<ST - 1>(); else copies_wait<ST - 2>();
-            const int st = k % ST, t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
-            const bool full = t0 + kS <= w.len;
-            f32x2 A = kOne, H = 0;
+    auto first = [&](int k, f32x2 (&nb)[kS]) {
+        // Copies are one group a tile: tile k is in once at most the groups after it are open.
+        if (k == 0) copies_wait<ST - 1>(); else copies_wait<ST - 2>();
+        const int st = k % ST, t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
+#pragma unroll
+        for (int i = 0; i < kS; ++i) nb[i] = minus_rest<T>(ring.value(st, 1, i));
+        if (t0 + kS > w.len) {                          // past the end: the identity (x is 0 there)
+#pragma unroll
+            for (int i = 0; i < kS; ++i)
+                if (t0 + i >= w.len) nb[i] = 0;
+        }
+        f32x2 A = kOne, H = 0;
+#pragma unroll
+        for (int i = 0; i < kS; ++i) {
+            A = fma2(nb[i], A, A);
+            H = advance<kLeak>(H, nb[i], ring.value(st, 0, i));
+        }
+        const float2 fa = unpack(A), fh = unpack(H);
+        runs[k & 1][threadIdx.x] = make_float4(fa.x, fa.y, fh.x, fh.y);
+        bar_arrive(kBarRuns + (k & 1));
+    };
+    auto second = [&](int k, const f32x2 (&nb)[kS]) {
+        const int st = k % ST, t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
+        bar_sync(kBarStates + (k & 1));
+        f32x2 h = pack(states[k & 1][threadIdx.x]);
+        T *out = yp + (int64_t)t0 * a.y_l;
+        if (w.on && t0 + kS <= w.len) {
 #pragma unroll
             for (int i = 0; i < kS; ++i) {
-                nb1[i] = minus_rest<T>(ring.value(st, 1, i));
-                if (!full && t0 + i >= w.len) nb1[i] = 0;       // past the end: the identity (x is 0 there)
-                A = fma2(nb1[i], A, A);
-                H = advance<kLeak>(H, nb1[i], ring.value(st, 0, i));
+                h = advance<kLeak>(h, nb[i], ring.value(st, 0, i));
+                Pair<T>::store(out, unpack(h));
+                out += a.y_l;
             }
-            const float2 fa = unpack(A), fh = unpack(H);
-            runs[k & 1][threadIdx.x] = make_float4(fa.x, fa.y, fh.x, fh.y);
-            bar_arrive(kBarRuns + (k & 1));
-        }
-        if (k > 0) {
-            const int q = k - 1, st = q % ST, t0 = (q * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
-            bar_sync(kBarStates + (q & 1));
-            f32x2 h = pack(states[q & 1][threadIdx.x]);
-            T *out = yp + (int64_t)t0 * a.y_l;
-            if (t0 + kS <= w.len) {
+        } else if (w.on) {
 #pragma unroll
-                for (int i = 0; i < kS; ++i) {
-                    h = advance<kLeak>(h, nb[i], ring.value(st, 0, i));
-                    if (w.on) Pair<T>::store(out, unpack(h));
-                    out += a.y_l;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kS; ++i) {
-                    h = advance<kLeak>(h, nb[i], ring.value(st, 0, i));
-                    if (w.on && t0 + i < a.L) Pair<T>::store(out, t0 + i < w.len ? unpack(h) : make_float2(0.f, 0.f));
-                    out += a.y_l;
-                }
+            for (int i = 0; i < kS; ++i) {
+                h = advance<kLeak>(h, nb[i], ring.value(st, 0, i));
+                if (t0 + i < a.L) Pair<T>::store(out, t0 + i < w.len ? unpack(h) : make_float2(0.f, 0.f));
+                out += a.y_l;
             }
-            __syncwarp();
-            copy(k + ST - 1);       // into the stage that the second pass has just left
         }
-#pragma unroll
-        for (int i = 0; i < kS; ++i) nb[i] = nb1[i];
-    }
+        __syncwarp();
+        copy(k + ST);           // into the stage that this pass has just left
+    };
+    two_passes(w.n, first, second);
     close_peers(a.nseg);
 }
 
 // ---------------------------------------------------------------- backward
 template <typename T>
 constexpr int kBwdStages = 3;
-template <typename T>
-using BwdRing = Ring<T, 3, kBwdStages<T>>;          // fields: x, g, dy
+template <typename T, int kLog2P>
+using BwdRing = Ring<T, 3, kBwdStages<T>, kLog2P>;          // fields: x, g, dy
 
-template <typename T, bool kLeak>
+template <typename T, bool kLeak, int kLog2P>
 __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_backward(const ScanArgs<T> a) {
     extern __shared__ __align__(16) unsigned char ring_mem[];
     // Gradients are carried negated: with -b at hand, b G = (-b)(-G) needs no sign.
@@ -498,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_backward(const Sca
     __shared__ float4 runs[2][kDataThreads];        // (A, H) of a run
     __shared__ float2 ends[2][kDataThreads];        // its -C from a zero C after it; then its -C
     __shared__ float2 states[2][kDataThreads];
-    const Where w = where(a);
+    const Where w = where<kLog2P>(a);
     constexpr int ST = kBwdStages<T>;
     open_peers(peers, a.nseg);
 
@@ -562,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_backward(const Sca
         return;
     }
 
-    const BwdRing<T> ring(w, ring_mem, a.log2p, w.c - 2 * w.cp);
+    const BwdRing<T, kLog2P> ring(w, ring_mem);
     const bool on = ring.c < a.D;
     const int cc = on ? ring.c : 0;
     const T *xp = a.x + w.row * a.x_b + cc, *gp = a.g + w.row * a.g_b + cc, *dp = a.dy + w.row * a.dy_b + cc;
@@ -570,71 +591,86 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_backward(const Sca
     auto copy = [&](int k) {
         if (k < w.n) {
             const int t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens;
-            ring.copy(k % ST, 0, xp, a.x_l, t0, w.len, on);
-            ring.copy(k % ST, 1, gp, a.g_l, t0, w.len, on);
-            ring.copy(k % ST, 2, dp, a.dy_l, t0, w.len, on);
+            ring.copy(k % ST, 0, xp, a.x_l, t0, w.tile_tokens, w.len, on);
+            ring.copy(k % ST, 1, gp, a.g_l, t0, w.tile_tokens, w.len, on);
+            ring.copy(k % ST, 2, dp, a.dy_l, t0, w.tile_tokens, w.len, on);
         }
         copies_commit();
     };
 #pragma unroll
     for (int k = 0; k < ST; ++k) copy(k);
-    f32x2 nb[kS], nb1[kS];
-    for (int k = 0; k <= w.n; ++k) {
-        if (k < w.n) {
-            if (k == 0) copies_wait<ST - 1>(); else copies_wait<ST - 2>();
-            const int st = k % ST, t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens + w.sc * kS;
-            const bool full = t0 >= 0 && t0 + kS <= w.len;
-            f32x2 A = kOne, H = 0, R = 0;
+    auto first = [&](int k, f32x2 (&nb)[kS]) {
+        if (k == 0) copies_wait<ST - 1>(); else copies_wait<ST - 2>();
+        const int st = k % ST, t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens + w.sc * kS;
 #pragma unroll
-            for (int i = 0; i < kS; ++i) {
-                nb1[i] = minus_rest<T>(ring.value(st, 1, i));
-                if (!full && (t0 < 0 || t0 + i >= w.len)) nb1[i] = 0;
-                A = fma2(nb1[i], A, A);
-                H = advance<kLeak>(H, nb1[i], ring.value(st, 0, i));
-            }
+        for (int i = 0; i < kS; ++i) nb[i] = minus_rest<T>(ring.value(st, 1, i));
+        if (t0 < 0 || t0 + kS > w.len) {
 #pragma unroll
-            for (int i = kS - 1; i >= 0; --i) {
-                const f32x2 G = fma2(ring.value(st, 2, i), kMinus, R);
-                R = fma2(nb1[i], G, G);
-            }
-            const float2 fa = unpack(A), fh = unpack(H);
-            runs[k & 1][threadIdx.x] = make_float4(fa.x, fa.y, fh.x, fh.y);
-            ends[k & 1][threadIdx.x] = unpack(R);
-            bar_arrive(kBarRuns + (k & 1));
+            for (int i = 0; i < kS; ++i)
+                if (t0 < 0 || t0 + i >= w.len) nb[i] = 0;
         }
-        if (k > 0) {
-            const int q = k - 1, st = q % ST, t0 = (a.ntiles - 1 - (q * a.nseg + w.seg)) * w.tile_tokens + w.sc * kS;
-            bar_sync(kBarStates + (q & 1));
-            f32x2 h = pack(states[q & 1][threadIdx.x]), C = pack(ends[q & 1][threadIdx.x]);
-            f32x2 v[kS];                                // h_{t-1} - x or h_{t-1}
+        f32x2 A = kOne, H = 0, R = 0;
 #pragma unroll
-            for (int i = 0; i < kS; ++i) {
-                const f32x2 x = ring.value(st, 0, i);
-                v[i] = kLeak ? fma2(x, kMinus, h) : h;
-                h = advance<kLeak>(h, nb[i], x);
-            }
-            const bool full = t0 >= 0 && t0 + kS <= w.len;
-            T *ox = dxp + (int64_t)(t0 + kS - 1) * a.dx_l, *og = dgp + (int64_t)(t0 + kS - 1) * a.dg_l;
+        for (int i = 0; i < kS; ++i) {
+            A = fma2(nb[i], A, A);
+            H = advance<kLeak>(H, nb[i], ring.value(st, 0, i));
+        }
+#pragma unroll
+        for (int i = kS - 1; i >= 0; --i) {
+            const f32x2 G = fma2(ring.value(st, 2, i), kMinus, R);
+            R = fma2(nb[i], G, G);
+        }
+        const float2 fa = unpack(A), fh = unpack(H);
+        runs[k & 1][threadIdx.x] = make_float4(fa.x, fa.y, fh.x, fh.y);
+        ends[k & 1][threadIdx.x] = unpack(R);
+        bar_arrive(kBarRuns + (k & 1));
+    };
+    auto second = [&](int k, const f32x2 (&nb)[kS]) {
+        const int st = k % ST, t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens + w.sc * kS;
+        bar_sync(kBarStates + (k & 1));
+        f32x2 h = pack(states[k & 1][threadIdx.x]), C = pack(ends[k & 1][threadIdx.x]);
+        f32x2 v[kS];                                    // h_{t-1} - x or h_{t-1}
+#pragma unroll
+        for (int i = 0; i < kS; ++i) {
+            const f32x2 x = ring.value(st, 0, i);
+            v[i] = kLeak ? fma2(x, kMinus, h) : h;
+            h = advance<kLeak>(h, nb[i], x);
+        }
+        T *ox = dxp + (int64_t)(t0 + kS - 1) * a.dx_l, *og = dgp + (int64_t)(t0 + kS - 1) * a.dg_l;
+        auto token = [&](int i, float2 &vx, float2 &vg) {
+            const f32x2 G = fma2(ring.value(st, 2, i), kMinus, C);
+            C = fma2(nb[i], G, G);                      // a G
+            vx = unpack(mul2(kLeak ? nb[i] : kMinus, G));
+            vg = unpack(mul2(mul2(C, nb[i]), v[i]));
+        };
+        if (w.on && t0 >= 0 && t0 + kS <= w.len) {
 #pragma unroll
             for (int i = kS - 1; i >= 0; --i) {
-                const f32x2 G = fma2(ring.value(st, 2, i), kMinus, C);
-                C = fma2(nb[i], G, G);                  // a G
-                float2 vx = unpack(mul2(kLeak ? nb[i] : kMinus, G));
-                float2 vg = unpack(mul2(mul2(C, nb[i]), v[i]));
-                if (!full && t0 + i >= w.len) vx = vg = make_float2(0.f, 0.f);
-                if (full ? w.on : w.on && t0 >= 0 && t0 + i < a.L) {
+                float2 vx, vg;
+                token(i, vx, vg);
+                Pair<T>::store(ox, vx);
+                Pair<T>::store(og, vg);
+                ox -= a.dx_l;
+                og -= a.dg_l;
+            }
+        } else if (w.on && t0 >= 0) {
+#pragma unroll
+            for (int i = kS - 1; i >= 0; --i) {
+                float2 vx, vg;
+                token(i, vx, vg);
+                if (t0 + i >= w.len) vx = vg = make_float2(0.f, 0.f);
+                if (t0 + i < a.L) {
                     Pair<T>::store(ox, vx);
                     Pair<T>::store(og, vg);
                 }
                 ox -= a.dx_l;
                 og -= a.dg_l;
             }
-            __syncwarp();
-            copy(k + ST - 1);
         }
-#pragma unroll
-        for (int i = 0; i < kS; ++i) nb[i] = nb1[i];
-    }
+        __syncwarp();
+        copy(k + ST);
+    };
+    two_passes(w.n, first, second);
     close_peers(a.nseg);
 }
 
@@ -667,6 +703,26 @@ __global__ void __launch_bounds__(256) k_scan_step(const T *x, const T *g, T *y,
     asm volatile("griddepcontrol.launch_dependents;" :::);
 }
 
+template <typename T>
+struct ScanKernel {
+    void (*fn)(const ScanArgs<T>);
+    int smem;
+};
+template <typename T, bool kLeak, int kLog2P>
+ScanKernel<T> kernel_of(bool backward) {
+    if (backward) return {k_scan_backward<T, kLeak, kLog2P>, BwdRing<T, kLog2P>::kBytes};
+    return {k_scan_forward<T, kLeak, kLog2P>, FwdRing<T, kLog2P>::kBytes};
+}
+template <typename T, bool kLeak>
+ScanKernel<T> kernel_of(bool backward, int log2p) {
+    switch (log2p) {
+        case 2: return kernel_of<T, kLeak, 2>(backward);
+        case 3: return kernel_of<T, kLeak, 3>(backward);
+        case 4: return kernel_of<T, kLeak, 4>(backward);
+        default: return kernel_of<T, kLeak, 5>(backward);
+    }
+}
+
 // Relative cost of a byte with rows of 4, 8, 16 and 32 channel pairs.
 constexpr double kRowCost[4] = {1.6, 1.25, 1.02, 1.0};
 
@@ -675,15 +731,52 @@ struct ScanPlan {
     int64_t chains;
 };
 
-// Channel pairs per CTA and segments per chain.  Time goes by rounds of resident CTAs,
-// a CTA's tiles and a few tiles' worth of start and end; rows of 64 bytes and less cost
-// more per byte (measured: see kRowCost).  The plan depends on the shape alone.
-ScanPlan scan_plan(int64_t B, int64_t L, int D, rlm_dtype dt) {
-    const int64_t slots = (dt == RLM_BF16 ? kPerSm<__nv_bfloat16> : kPerSm<float>) * (int64_t)sm_count();
+// Resident CTAs of a kernel on the current device in clusters of nseg (a cluster's CTAs
+// sit in one GPC, so large ones do not fill every SM).  Asked once for each kernel.
+template <typename T>
+int64_t resident(const ScanKernel<T> &k, int nseg) {
+    struct Key {
+        const void *fn;
+        int dev, nseg;
+        int64_t ctas;
+    };
+    static std::mutex mu;
+    static std::vector<Key> known;
+    int dev = 0;
+    cudaGetDevice(&dev);
+    const void *fn = reinterpret_cast<const void *>(k.fn);
+    std::lock_guard<std::mutex> lock(mu);
+    for (const Key &e : known)
+        if (e.fn == fn && e.dev == dev && e.nseg == nseg) return e.ctas;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)nseg);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)k.smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)nseg;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, k.fn, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+    }
+    known.push_back({fn, dev, nseg, (int64_t)n * nseg});
+    return (int64_t)n * nseg;
+}
+
+// Channel pairs per CTA and segments per chain: the least of rounds of resident CTAs times
+// a CTA's waves, with a few waves' worth for its start and end.
+template <typename T>
+ScanPlan scan_plan(int64_t B, int64_t L, int D, bool backward, bool leak) {
     ScanPlan best = {};
     double best_cost = 0;
     for (int lp = 5; lp >= 2; --lp) {
         if (lp > 2 && (2 << (lp - 1)) >= D) continue;       // a narrower group already holds the row
+        const ScanKernel<T> k = leak ? kernel_of<T, true>(backward, lp) : kernel_of<T, false>(backward, lp);
         ScanPlan p;
         p.log2p = lp;
         p.groups = (D + (2 << lp) - 1) / (2 << lp);
@@ -691,8 +784,8 @@ ScanPlan scan_plan(int64_t B, int64_t L, int D, rlm_dtype dt) {
         const int tile = (kDataThreads >> lp) * kS;
         p.ntiles = (int)((L + tile - 1) / tile);
         for (p.nseg = 1; p.nseg <= kMaxSeg && p.nseg <= p.ntiles; p.nseg *= 2) {
-            // A cluster's CTAs sit in one GPC, which clusters do not fill evenly.
-            const int64_t room = p.nseg == 1 ? slots : slots * 27 / 32;
+            const int64_t room = resident(k, p.nseg);
+            if (room < 1) continue;
             const int64_t rounds = (p.chains * p.nseg + room - 1) / room;
             const int waves = (p.ntiles + p.nseg - 1) / p.nseg;
             const double cost = (double)rounds * (waves + 4) * kRowCost[lp - 2];
@@ -706,19 +799,20 @@ ScanPlan scan_plan(int64_t B, int64_t L, int D, rlm_dtype dt) {
 }
 
 template <typename T>
-cudaError_t launch_scan(void (*kernel)(const ScanArgs<T>), int smem, ScanArgs<T> &a, const ScanPlan &p,
-                        cudaStream_t st) {
+cudaError_t launch_scan(bool backward, bool leak, ScanArgs<T> &a, int64_t B, cudaStream_t st) {
+    const ScanPlan p = scan_plan<T>(B, a.L, a.D, backward, leak);
+    if (p.nseg < 1) return cudaErrorInvalidConfiguration;
+    const ScanKernel<T> k = leak ? kernel_of<T, true>(backward, p.log2p) : kernel_of<T, false>(backward, p.log2p);
     a.groups = p.groups;
-    a.log2p = p.log2p;
     a.nseg = p.nseg;
     a.ntiles = p.ntiles;
     a.nchunks = (a.L + kChunk - 1) / kChunk;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.chains * p.nseg));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.dynamicSmemBytes = (size_t)k.smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -727,7 +821,7 @@ cudaError_t launch_scan(void (*kernel)(const ScanArgs<T>), int smem, ScanArgs<T>
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     count_launches(1);
-    return cudaLaunchKernelEx(&cfg, kernel, a);
+    return cudaLaunchKernelEx(&cfg, k.fn, a);
 }
 
 template <typename T>
@@ -745,8 +839,7 @@ cudaError_t forward_t(const rlm_strided &x, const rlm_strided &g, const rlm_stri
     a.lengths = lengths;
     a.L = (int)x.L;
     a.D = (int)x.D;
-    return launch_scan(leak ? k_scan_forward<T, true> : k_scan_forward<T, false>, FwdRing<T>::kBytes, a,
-                       scan_plan(x.B, x.L, (int)x.D, x.dtype), st);
+    return launch_scan(false, leak, a, x.B, st);
 }
 
 template <typename T>
@@ -768,8 +861,7 @@ cudaError_t backward_t(const rlm_strided &dy, const rlm_strided &x, const rlm_st
     a.lengths = lengths;
     a.L = (int)x.L;
     a.D = (int)x.D;
-    return launch_scan(leak ? k_scan_backward<T, true> : k_scan_backward<T, false>, BwdRing<T>::kBytes, a,
-                       scan_plan(x.B, x.L, (int)x.D, x.dtype), st);
+    return launch_scan(true, leak, a, x.B, st);
 }
 
 template <typename T>
