@@ -364,6 +364,49 @@ RLM_API rlm_status rlm_scan_decode(const rlm_strided *x_t, const rlm_strided *g_
 /* Bytes of the `saved` buffer. */
 RLM_API size_t rlm_scan_saved_size(int64_t B, int64_t L, int D);
 
+/* ------------------------------------------------------------ linear layer
+ *   z = x w^T + bias,   y = act(z) + residual
+ * the projections around the mixers.  Matrices are row-major with a row pitch ld in
+ * elements: x [R][K], w [N][K], residual, pre and y [R][N], all RLM_BF16; bias fp32 [N].
+ * K and N are multiples of 8, up to 2^20; R up to 2^24.  Pointers are 16-byte aligned and
+ * ld is a multiple of 16 bytes.  Sums are fp32; y (and pre) are rounded once. */
+typedef struct {
+    void *ptr;
+    rlm_dtype dtype;
+    int64_t rows, cols, ld;
+} rlm_matrix;
+
+typedef enum {
+    RLM_ACT_NONE = 0,
+    RLM_ACT_SILU = 1,      /* z sigma(z) */
+    RLM_ACT_GELU = 2,      /* z sigma(2 sqrt(2/pi) (z + 0.044715 z^3)), the tanh form */
+    RLM_ACT_SIGMOID = 3    /* sigma(z) */
+} rlm_act;
+
+/*   bias      nullable
+ *   residual  nullable; may be y itself (the residual stream updated in place)
+ *   pre       nullable output: z, which rlm_linear_backward needs unless act is none
+ *   y         output; must not overlap x, w, bias or pre
+ * Workspace: rlm_linear_workspace_size (partial sums where a product has few tiles). */
+RLM_API rlm_status rlm_linear(const rlm_matrix *x, const rlm_matrix *w, const float *bias, rlm_act act,
+                              const rlm_matrix *residual, const rlm_matrix *pre, const rlm_matrix *y,
+                              const rlm_launch *launch);
+
+/* Gradients given dy = dl/dy (the residual's gradient is dy itself):
+ *   dz = dy act'(pre),  dx = dz w,  dw = dz^T x,  dbias = sum of dz over the rows
+ *   pre     z as the forward pass kept it; NULL if and only if act is none
+ *   dx      nullable output [R][K] RLM_BF16
+ *   dw      nullable output [N][K] RLM_BF16 or RLM_F32
+ *   dbias   nullable output, fp32 [N]
+ * Outputs are overwritten; at least one is given.  dz is rounded to bf16 for the products,
+ * dbias is summed from its fp32 values.  Workspace: rlm_linear_backward_workspace_size. */
+RLM_API rlm_status rlm_linear_backward(const rlm_matrix *dy, const rlm_matrix *x, const rlm_matrix *w,
+                                       const rlm_matrix *pre, rlm_act act, const rlm_matrix *dx, const rlm_matrix *dw,
+                                       float *dbias, const rlm_launch *launch);
+
+RLM_API size_t rlm_linear_workspace_size(int64_t R, int64_t K, int64_t N);
+RLM_API size_t rlm_linear_backward_workspace_size(int64_t R, int64_t K, int64_t N, rlm_act act);
+
 /* ------------------------------------------------------------------ utility
  * rlm_validate_params: copies p to the host (synchronous) and checks that every
  * value is finite and every gamma >= 0 (Sec. 3.1 requires alpha > 0; gamma = 0

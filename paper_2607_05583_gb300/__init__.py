@@ -27,6 +27,7 @@ __all__ = [
     "rlm_mixer_decode",
     "rlm_prefill_workspace_size", "rlm_backward_workspace_size",
     "rlm_scan_prefill", "rlm_scan_backward", "rlm_scan_decode", "rlm_scan_saved_size", "scan_saved",
+    "rlm_linear", "rlm_linear_backward", "rlm_linear_workspace_size", "rlm_linear_backward_workspace_size",
     "rlm_validate_params", "rlm_get_device_status", "rlm_status_string",
     "rlm_version", "rlm_kernels_launched", "RLM_OK", "RLM_ERR_INVALID_ARG", "RLM_ERR_UNSUPPORTED",
     "RLM_ERR_CUDA", "RLM_ERR_TIMEOUT", "RLM_F32", "RLM_BF16",
@@ -73,6 +74,11 @@ class _Strided(ctypes.Structure):
     _fields_ = [("ptr", ctypes.c_void_p), ("dtype", ctypes.c_int),
                 ("B", ctypes.c_int64), ("L", ctypes.c_int64), ("D", ctypes.c_int64),
                 ("stride_b", ctypes.c_int64), ("stride_l", ctypes.c_int64)]
+
+
+class _Matrix(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("dtype", ctypes.c_int),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64)]
 
 
 class _Launch(ctypes.Structure):
@@ -147,6 +153,15 @@ def load_library(build_if_missing: bool = False) -> ctypes.CDLL:
         getattr(lib, f).restype = ctypes.c_int
     lib.rlm_scan_saved_size.argtypes = [ctypes.c_int64, ctypes.c_int64, I]
     lib.rlm_scan_saved_size.restype = ctypes.c_size_t
+    X, Q = P(_Matrix), ctypes.c_int64
+    lib.rlm_linear.argtypes = [X, X, V, I, X, X, X, P(_Launch)]
+    lib.rlm_linear_backward.argtypes = [X, X, X, X, I, X, X, V, P(_Launch)]
+    lib.rlm_linear_workspace_size.argtypes = [Q, Q, Q]
+    lib.rlm_linear_backward_workspace_size.argtypes = [Q, Q, Q, I]
+    for f in ("rlm_linear", "rlm_linear_backward"):
+        getattr(lib, f).restype = ctypes.c_int
+    for f in ("rlm_linear_workspace_size", "rlm_linear_backward_workspace_size"):
+        getattr(lib, f).restype = ctypes.c_size_t
     _lib = lib
     return lib
 
@@ -321,6 +336,19 @@ def _strided(t: torch.Tensor, name: str) -> _Strided:
         return _Strided(t.data_ptr(), _DT[t.dtype], B, L, D, t.stride(0), D)
     B, L, D = t.shape
     return _Strided(t.data_ptr(), _DT[t.dtype], B, L, D, t.stride(0), t.stride(1))
+
+
+def _matrix(t: torch.Tensor, name: str) -> _Matrix:
+    """A row-major matrix [...][cols] whose leading dimensions share one row pitch."""
+    if t.dtype not in _DT:
+        raise ValueError(f"{name}: unsupported dtype {t.dtype}")
+    if not t.is_cuda or t.dim() < 2 or t.stride(-1) != 1:
+        raise ValueError(f"{name} must be a CUDA matrix [...][cols] with unit column stride, got {tuple(t.shape)} with "
+                         f"strides {t.stride()} on {t.device}")
+    if t.dim() > 2:
+        t = t.view(-1, t.shape[-1])        # raises where the rows do not share one pitch
+    rows, cols = t.shape
+    return _Matrix(t.data_ptr(), _DT[t.dtype], rows, cols, t.stride(0) if rows > 1 else cols)
 
 
 def _opt(t: torch.Tensor | None, dtype, shape, name: str):
@@ -582,3 +610,55 @@ def rlm_scan_decode(x_t: torch.Tensor, g_t: torch.Tensor, state: torch.Tensor, y
     _check(load_library().rlm_scan_decode(ctypes.byref(xt), ctypes.byref(gt), int(leak),
                                           _opt(state, torch.float32, (xt.B, xt.D), "state"), ctypes.byref(yt),
                                           ctypes.byref(_launch(stream, None))), "rlm_scan_decode")
+
+
+# ------------------------------------------------------------ linear layer
+ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "sigmoid": 3}
+
+
+def _act(act: str) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, got {act!r}")
+    return ACTIVATIONS[act]
+
+
+def rlm_linear_workspace_size(R: int, K: int, N: int) -> int:
+    return load_library().rlm_linear_workspace_size(R, K, N)
+
+
+def rlm_linear_backward_workspace_size(R: int, K: int, N: int, act: str = "none") -> int:
+    return load_library().rlm_linear_backward_workspace_size(R, K, N, _act(act))
+
+
+def rlm_linear(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, bias: torch.Tensor | None = None,
+               residual: torch.Tensor | None = None, act: str = "none", pre: torch.Tensor | None = None,
+               workspace: torch.Tensor | None = None, stream=None) -> None:
+    """y = act(x w^T + bias) + residual.  x [...][K], w [N][K], y and residual [...][N] bfloat16 (rows
+    may be strided), bias float32 [N]; act is "none", "silu", "gelu" (tanh form) or "sigmoid".
+    ``pre`` receives x w^T + bias for the backward pass; ``residual`` may be ``y`` itself."""
+    lib = load_library()
+    xt, wt, yt = _matrix(x, "x"), _matrix(w, "w"), _matrix(y, "y")
+    rt = _matrix(residual, "residual") if residual is not None else None
+    pt = _matrix(pre, "pre") if pre is not None else None
+    if workspace is None:
+        workspace = _workspace(lib.rlm_linear_workspace_size(xt.rows, xt.cols, wt.rows), x.device)
+    ref = lambda c: ctypes.byref(c) if c is not None else None
+    _check(lib.rlm_linear(ctypes.byref(xt), ctypes.byref(wt), _opt(bias, torch.float32, (wt.rows,), "bias"), _act(act),
+                          ref(rt), ref(pt), ctypes.byref(yt), ctypes.byref(_launch(stream, workspace))), "rlm_linear")
+
+
+def rlm_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, dx: torch.Tensor | None = None,
+                        dw: torch.Tensor | None = None, dbias: torch.Tensor | None = None, act: str = "none",
+                        pre: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Gradients of rlm_linear: dx (bfloat16), dw (bfloat16 or float32) and dbias (float32), each
+    optional.  ``pre`` is what the forward pass kept (needed unless act is "none")."""
+    lib = load_library()
+    dyt, xt, wt = _matrix(dy, "dy"), _matrix(x, "x"), _matrix(w, "w")
+    opt = lambda t, name: _matrix(t, name) if t is not None else None
+    pt, dxt, dwt = opt(pre, "pre"), opt(dx, "dx"), opt(dw, "dw")
+    if workspace is None:
+        workspace = _workspace(lib.rlm_linear_backward_workspace_size(xt.rows, xt.cols, wt.rows, _act(act)), x.device)
+    ref = lambda c: ctypes.byref(c) if c is not None else None
+    _check(lib.rlm_linear_backward(ctypes.byref(dyt), ctypes.byref(xt), ctypes.byref(wt), ref(pt), _act(act), ref(dxt),
+                                   ref(dwt), _opt(dbias, torch.float32, (wt.rows,), "dbias"),
+                                   ctypes.byref(_launch(stream, workspace))), "rlm_linear_backward")

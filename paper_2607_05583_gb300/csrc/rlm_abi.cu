@@ -554,17 +554,19 @@ rlm_status rlm_validate_params(const rlm_params *p) {
 
 rlm_status rlm_get_device_status(const rlm_launch *ln) {
     if (!ln) return fail(RLM_ERR_INVALID_ARG, "launch is NULL");
-    int status = RLM_OK, bwd = RLM_OK, mix = RLM_OK, t32 = RLM_OK, scan = RLM_OK;
+    int status = RLM_OK, bwd = RLM_OK, mix = RLM_OK, t32 = RLM_OK, scan = RLM_OK, lin = RLM_OK;
     cudaError_t e = read_and_clear_device_status(&status, static_cast<cudaStream_t>(ln->stream));
     if (e == cudaSuccess) e = read_and_clear_bwd_status(&bwd, static_cast<cudaStream_t>(ln->stream));
     if (e == cudaSuccess) e = read_and_clear_mixer_status(&mix, static_cast<cudaStream_t>(ln->stream));
     if (e == cudaSuccess) e = read_and_clear_tc32_status(&t32, static_cast<cudaStream_t>(ln->stream));
     if (e == cudaSuccess) e = read_and_clear_scan_status(&scan, static_cast<cudaStream_t>(ln->stream));
+    if (e == cudaSuccess) e = read_and_clear_linear_status(&lin, static_cast<cudaStream_t>(ln->stream));
     if (e != cudaSuccess) return cuda_fail(e, "rlm_get_device_status");
     if (status == RLM_OK) status = bwd;
     if (status == RLM_OK) status = mix;
     if (status == RLM_OK) status = t32;
     if (status == RLM_OK) status = scan;
+    if (status == RLM_OK) status = lin;
     if (status != RLM_OK) return fail((rlm_status)status, "a bounded device-side wait expired");
     return RLM_OK;
 }

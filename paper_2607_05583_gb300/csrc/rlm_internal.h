@@ -94,6 +94,18 @@ cudaError_t scan_step(const rlm_strided &x, const rlm_strided &g, const rlm_stri
                       cudaStream_t st);
 cudaError_t read_and_clear_scan_status(int *status, cudaStream_t st);
 
+// ---- linear layer (rlm_linear.cu) --------------------------------------------
+// y = act(x w^T + bias) + residual and its gradients; nullable arguments as in the C ABI.
+size_t linear_ws_bytes(int64_t R, int64_t K, int64_t N);
+size_t linear_backward_ws_bytes(int64_t R, int64_t K, int64_t N, int act);
+cudaError_t linear_forward(const rlm_matrix &x, const rlm_matrix &w, const float *bias, int act,
+                           const rlm_matrix *residual, const rlm_matrix *pre, const rlm_matrix &y, void *ws,
+                           cudaStream_t st);
+cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm_matrix &w, const rlm_matrix *pre,
+                            int act, const rlm_matrix *dx, const rlm_matrix *dw, float *dbias, void *ws,
+                            cudaStream_t st);
+cudaError_t read_and_clear_linear_status(int *status, cudaStream_t st);
+
 // ---- decode (rlm_decode.cu) -----------------------------------------------
 cudaError_t decode_step(const void *x_t, void *y_t, rlm_dtype dt, int B, int D, int M,
                         float *s, const float *coef, cudaStream_t st);

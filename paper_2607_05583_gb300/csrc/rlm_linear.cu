@@ -1,0 +1,724 @@
+// rlm_linear.cu -- matrix products with fused epilogues: a linear layer and its gradients.
+//
+//   forward   z = x w^T + bias, y = act(z) + residual         x [R][K], w [N][K]
+//   backward  dz = dy act'(z);  dx = dz w;  dw = dz^T x;  dbias = sum over rows of dz
+//
+// The three products are one kernel, C[M][N] = sum_k A[m][k] B[n][k], whose operands lie
+// either with the contraction index contiguous (K-major) or with the row index contiguous
+// (MN-major): x w^T is K, K; dz w is K, MN; dz^T x is MN, MN.  TMA brings either form into
+// 128-byte swizzled shared memory and tcgen05.mma reads either, so nothing is transposed.
+//
+// k_gemm.  Persistent, one CTA per SM, 128 x kBN tiles (kBN = 256 or 128), contraction
+// steps of 64.  Warp 8 feeds a ring of operand stages, one thread of warp 9 issues the
+// MMAs into one of two TMEM accumulators, warps 0-7 empty the other: warp w owns TMEM
+// lanes 32 (w mod 4) .. + 31 and half w / 4 of the columns, 64 bytes of output at a time,
+// from registers through its own 2 KB staging buffers (two, 64-byte swizzle) to TMA
+// stores, which clip at the matrix's edge.  A product of few tiles is cut along the
+// contraction (splits): partial sums go to the workspace in fp32 and k_finish adds them in
+// order and applies the epilogue.  Accumulation is fp32 throughout; results repeat bit for
+// bit.
+//
+// dz is rounded to bf16 once, the operand type of the two products that read it; dbias is
+// summed from the fp32 values.
+#include <algorithm>
+#include <mutex>
+#include <vector>
+
+#include "rlm_device.cuh"
+#include "rlm_internal.h"
+#include "rlm_umma.cuh"
+
+namespace rlm {
+
+__device__ int g_linear_status = 0;
+
+namespace {
+
+using namespace umma;
+using bf16 = __nv_bfloat16;
+
+// ------------------------------------------------------------- activations
+__device__ __forceinline__ float sigmoidf(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+constexpr float kBend1 = 1.5957691216f, kBend3 = 0.0713548163f;     // 2 sqrt(2 / pi), and times 0.044715
+
+template <int kAct>
+__device__ __forceinline__ float act(float z) {
+    if (kAct == RLM_ACT_SILU) return z * sigmoidf(z);
+    if (kAct == RLM_ACT_SIGMOID) return sigmoidf(z);
+    if (kAct == RLM_ACT_GELU) return z * sigmoidf(z * fmaf(kBend3 * z, z, kBend1));
+    return z;
+}
+__device__ __forceinline__ float act_of(int kind, float z) {
+    switch (kind) {
+        case RLM_ACT_SILU: return act<RLM_ACT_SILU>(z);
+        case RLM_ACT_SIGMOID: return act<RLM_ACT_SIGMOID>(z);
+        case RLM_ACT_GELU: return act<RLM_ACT_GELU>(z);
+        default: return z;
+    }
+}
+// act'(z).  1 - sigma is formed as sigma(-z): the difference would lose it for large z.
+__device__ __forceinline__ float act_grad(int kind, float z) {
+    if (kind == RLM_ACT_SIGMOID) return sigmoidf(z) * sigmoidf(-z);
+    if (kind == RLM_ACT_SILU) return sigmoidf(z) * fmaf(z, sigmoidf(-z), 1.0f);
+    const float u = z * fmaf(kBend3 * z, z, kBend1), du = fmaf(3.0f * kBend3 * z, z, kBend1);
+    return sigmoidf(u) * fmaf(z * du, sigmoidf(-u), 1.0f);
+}
+
+// -------------------------------------------------------------------- gemm
+constexpr int kBM = 128, kBK = 64;
+constexpr int kEpiWarps = 8;
+constexpr int kGemmThreads = (kEpiWarps + 2) * 32;
+constexpr int kStageOut = 2048;                 // one warp's staging buffer: 32 rows of 64 bytes
+
+template <int kBN>
+struct GemmCfg {
+    static constexpr int kA = kBM * kBK * 2, kB = kBN * kBK * 2, kStage = kA + kB;
+    static constexpr int kStages = kBN == 256 ? 4 : 6;
+    static constexpr int kOffOut = kStages * kStage;
+    static constexpr int kOffBar = kOffOut + kEpiWarps * 2 * kStageOut;
+    static constexpr int kBars = 2 * kStages + 4;
+    static constexpr int kOffMisc = kOffBar + kBars * 8;
+    static constexpr int kSmem = kOffMisc + 16 + 1024;          // and room to align the ring
+    static_assert(kSmem <= 232448, "shared memory budget");
+};
+
+struct GemmArgs {
+    int M, N, K;                // output rows and columns, contraction
+    int tiles_m, tiles_n, splits, steps_per_split, steps;
+    const float *bias;          // nullable [N]
+    const bf16 *residual;       // nullable [M][ld]
+    int64_t residual_ld;
+    int act;
+    int want_pre;
+};
+
+// Order of the tiles: columns of kGroup row tiles, so that the CTAs at work share operands in L2.
+constexpr int kGroup = 16;
+__device__ __forceinline__ void tile_of(int t, const GemmArgs &g, int &tm, int &tn) {
+    const int per = kGroup * g.tiles_n, grp = t / per, first = grp * kGroup;
+    const int rows = min(kGroup, g.tiles_m - first), in = t - grp * per;
+    tn = in / rows;
+    tm = first + in - tn * rows;
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float lo16(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float hi16(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+
+__device__ __forceinline__ void st_shared16(uint32_t a, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+// Byte offset of 16-byte piece p of row r in a staging buffer (64-byte TMA swizzle).
+__device__ __forceinline__ uint32_t piece(int r, int p) { return r * 64 + ((p ^ ((r >> 1) & 3)) << 4); }
+
+// kOutF32: the raw sums as fp32 (partial sums, or a gradient kept in fp32); otherwise the
+// epilogue act(sum + bias) + residual as bf16, and, if asked, sum + bias as bf16 (map_pre).
+template <bool kAMn, bool kBMn, int kBN, bool kOutF32, int kAct>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+           const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_pre, const GemmArgs g) {
+    using Cfg = GemmCfg<kBN>;
+    constexpr int ST = Cfg::kStages;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
+    const uint32_t base = smem_u32(smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t bars = base + Cfg::kOffBar;
+    const uint32_t full = bars, empty = bars + ST * 8, acc_full = bars + 2 * ST * 8, acc_empty = acc_full + 16;
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + Cfg::kOffMisc);
+    uint32_t *tmem_at = reinterpret_cast<uint32_t *>(smem + Cfg::kOffMisc + 8);
+
+    if (tid == 0) {
+        for (int i = 0; i < ST; ++i) {
+            bar_init(full + i * 8, 1);
+            bar_init(empty + i * 8, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(acc_full + i * 8, 1);
+            bar_init(acc_empty + i * 8, kEpiWarps);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kEpiWarps) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_at)),
+                     "n"(2 * kBN)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if (lane == 0) {
+            prefetch_map(&map_a);
+            prefetch_map(&map_b);
+            prefetch_map(&map_c);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_at;
+    const int units = g.tiles_m * g.tiles_n * g.splits;
+
+    if (warp == kEpiWarps) {
+        if (lane == 0) {
+            int it = 0;
+            bool ok = true;
+            for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+                const int split = u % g.splits;
+                int tm, tn;
+                tile_of(u / g.splits, g, tm, tn);
+                const int s0 = split * g.steps_per_split, s1 = min(g.steps, s0 + g.steps_per_split);
+                for (int s = s0; s < s1; ++s, ++it) {
+                    const int st = it % ST;
+                    if (it >= ST && !(ok = wait_bar(empty + st * 8, (it / ST - 1) & 1, abort_flag, &g_linear_status))) break;
+                    const uint32_t a = base + st * Cfg::kStage, b = a + Cfg::kA, bar = full + st * 8;
+                    bar_expect_tx(bar, Cfg::kStage);
+                    if (kAMn) {
+#pragma unroll
+                        for (int j = 0; j < kBM / 64; ++j)
+                            tma_load_2d(a + j * 8192, &map_a, tm * kBM + j * 64, s * kBK, bar);
+                    } else {
+                        tma_load_2d(a, &map_a, s * kBK, tm * kBM, bar);
+                    }
+                    if (kBMn) {
+#pragma unroll
+                        for (int j = 0; j < kBN / 64; ++j)
+                            tma_load_2d(b + j * 8192, &map_b, tn * kBN + j * 64, s * kBK, bar);
+                    } else {
+                        tma_load_2d(b, &map_b, s * kBK, tn * kBN, bar);
+                    }
+                }
+            }
+            // Copies in flight land before the CTA may end (after a timeout; otherwise they have).
+            for (int i = max(0, it - ST); i < it; ++i)
+                for (int n = 0; n < 1 << 22 && !bar_try(full + (i % ST) * 8, (i / ST) & 1); ++n) {}
+        }
+    } else if (warp == kEpiWarps + 1) {
+        if (lane == 0) {
+            constexpr uint32_t id = idesc(kBM, kBN, kAMn, kBMn);
+            int it = 0, n = 0;
+            bool ok = true;
+            for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++n) {
+                const int split = u % g.splits;
+                const int s0 = split * g.steps_per_split, s1 = min(g.steps, s0 + g.steps_per_split);
+                const int buf = n & 1;
+                const uint32_t d = tmem + buf * kBN;
+                if (n >= 2 && !(ok = wait_bar(acc_empty + buf * 8, (n / 2 - 1) & 1, abort_flag, &g_linear_status))) break;
+                fence_after();
+                for (int s = s0; s < s1; ++s, ++it) {
+                    const int st = it % ST;
+                    if (!(ok = wait_bar(full + st * 8, (it / ST) & 1, abort_flag, &g_linear_status))) break;
+                    fence_after();
+                    const uint32_t a = base + st * Cfg::kStage, b = a + Cfg::kA;
+#pragma unroll
+                    for (int k = 0; k < kBK / 16; ++k) {
+                        const uint64_t da = kAMn ? desc(a + k * 2048, 8192, 1024) : desc(a + k * 32, 16, 1024);
+                        const uint64_t db = kBMn ? desc(b + k * 2048, 8192, 1024) : desc(b + k * 32, 16, 1024);
+                        asm volatile(
+                            "{ .reg .pred p; setp.ne.b32 p, %4, 0;\n"
+                            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
+                            "l"(da), "l"(db), "r"(id), "r"((uint32_t)(s > s0 || k > 0))
+                            : "memory");
+                    }
+                    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                                     empty + st * 8)
+                                 : "memory");
+                }
+                asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(acc_full +
+                                                                                                                 buf * 8)
+                             : "memory");
+            }
+        }
+    } else {
+        constexpr int kCols = kOutF32 ? 16 : 32;            // output columns of one 64-byte chunk
+        const uint32_t out = base + Cfg::kOffOut + warp * 2 * kStageOut;
+        int n = 0, slot = 0;
+        for (int u = blockIdx.x; u < units; u += gridDim.x, ++n) {
+            const int split = u % g.splits;
+            int tm, tn;
+            tile_of(u / g.splits, g, tm, tn);
+            const int row0 = tm * kBM + (warp & 3) * 32, col0 = tn * kBN + (warp >> 2) * (kBN / 2);
+            const int buf = n & 1;
+            if (!wait_bar(acc_full + buf * 8, (n / 2) & 1, abort_flag, &g_linear_status)) break;
+            fence_after();
+            const uint32_t acc = tmem + buf * kBN + (warp >> 2) * (kBN / 2) + ((uint32_t)(warp & 3) << 21);
+            for (int c = 0; c < kBN / 2; c += kCols) {
+                const int col = col0 + c;
+                const bool live = row0 < g.M && col < g.N;
+                uint32_t v[32];
+                uint4 res[4];
+                if (!kOutF32 && g.residual && live) {
+                    // Eight rows of 64 bytes a request; handed to the rows' lanes through the staging buffer.
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = row0 + i * 8 + (lane >> 2), cc = col + (lane & 3) * 8;
+                        res[i] = r < g.M && cc < g.N
+                                     ? __ldg(reinterpret_cast<const uint4 *>(g.residual + (int64_t)r * g.residual_ld + cc))
+                                     : make_uint4(0, 0, 0, 0);
+                    }
+                }
+                tmem_ld16(acc + c, v);
+                if (!kOutF32) tmem_ld16(acc + c + 16, v + 16);
+                tmem_wait_ld();
+                if (c + kCols >= kBN / 2) {                 // the last read of this accumulator
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(acc_empty + buf * 8);
+                }
+                if (!live) continue;
+                if constexpr (kOutF32) {
+                    if (lane == 0) store_wait_read<1>();
+                    __syncwarp();
+                    const uint32_t to = out + slot * kStageOut;
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+                        st_shared16(to + piece(lane, p), make_uint4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]));
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_3d(&map_c, to, col, row0, split);
+                        store_commit();
+                    }
+                    slot ^= 1;
+                } else {
+                float z[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(v[i]);
+                if (g.bias) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        if (col + q * 4 < g.N) {
+                            const float4 b = __ldg(reinterpret_cast<const float4 *>(g.bias + col + q * 4));
+                            z[4 * q] += b.x;
+                            z[4 * q + 1] += b.y;
+                            z[4 * q + 2] += b.z;
+                            z[4 * q + 3] += b.w;
+                        }
+                    }
+                }
+                if (g.want_pre) {
+                    if (lane == 0) store_wait_read<1>();
+                    __syncwarp();
+                    const uint32_t to = out + slot * kStageOut;
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+                        st_shared16(to + piece(lane, p), make_uint4(pack2(z[8 * p], z[8 * p + 1]), pack2(z[8 * p + 2], z[8 * p + 3]),
+                                                                    pack2(z[8 * p + 4], z[8 * p + 5]), pack2(z[8 * p + 6], z[8 * p + 7])));
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_3d(&map_pre, to, col, row0, 0);
+                        store_commit();
+                    }
+                    slot ^= 1;
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) z[i] = act<kAct>(z[i]);
+                if (lane == 0) store_wait_read<1>();
+                __syncwarp();
+                const uint32_t to = out + slot * kStageOut;
+                if (g.residual) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) st_shared16(to + piece(i * 8 + (lane >> 2), lane & 3), res[i]);
+                    __syncwarp();
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        const uint4 r = ld_shared16(to + piece(lane, p));
+                        z[8 * p] += lo16(r.x), z[8 * p + 1] += hi16(r.x), z[8 * p + 2] += lo16(r.y), z[8 * p + 3] += hi16(r.y);
+                        z[8 * p + 4] += lo16(r.z), z[8 * p + 5] += hi16(r.z), z[8 * p + 6] += lo16(r.w), z[8 * p + 7] += hi16(r.w);
+                    }
+                    __syncwarp();
+                }
+#pragma unroll
+                for (int p = 0; p < 4; ++p)
+                    st_shared16(to + piece(lane, p), make_uint4(pack2(z[8 * p], z[8 * p + 1]), pack2(z[8 * p + 2], z[8 * p + 3]),
+                                                                pack2(z[8 * p + 4], z[8 * p + 5]), pack2(z[8 * p + 6], z[8 * p + 7])));
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store_3d(&map_c, to, col, row0, 0);
+                    store_commit();
+                }
+                slot ^= 1;
+                }
+            }
+        }
+        if (lane == 0) store_wait_all();
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == kEpiWarps)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(2 * kBN));
+}
+
+// ------------------------------------------------- sums of split products
+// part [splits][M][N] fp32, added in order, then the epilogue; a thread per 4 columns.
+struct FinishArgs {
+    const float *part;
+    int64_t M;
+    int N, splits, act, out_f32;
+    const float *bias;
+    const bf16 *residual;
+    int64_t residual_ld, out_ld, pre_ld;
+    void *out;
+    bf16 *pre;
+};
+__global__ void __launch_bounds__(256) k_finish(const FinishArgs f) {
+    const int64_t q = f.N / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= f.M * q) return;
+    const int64_t row = i / q;
+    const int col = (int)(i - row * q) * 4;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < f.splits; ++k) {
+        const float4 v = __ldcs(reinterpret_cast<const float4 *>(f.part + ((int64_t)k * f.M + row) * f.N + col));
+        s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    if (f.out_f32) {
+        *reinterpret_cast<float4 *>(static_cast<float *>(f.out) + row * f.out_ld + col) = s;
+        return;
+    }
+    if (f.bias) {
+        const float4 b = __ldg(reinterpret_cast<const float4 *>(f.bias + col));
+        s.x += b.x, s.y += b.y, s.z += b.z, s.w += b.w;
+    }
+    if (f.pre) *reinterpret_cast<uint2 *>(f.pre + row * f.pre_ld + col) = make_uint2(pack2(s.x, s.y), pack2(s.z, s.w));
+    s.x = act_of(f.act, s.x), s.y = act_of(f.act, s.y), s.z = act_of(f.act, s.z), s.w = act_of(f.act, s.w);
+    if (f.residual) {
+        const uint2 r = *reinterpret_cast<const uint2 *>(f.residual + row * f.residual_ld + col);
+        s.x += lo16(r.x), s.y += hi16(r.x), s.z += lo16(r.y), s.w += hi16(r.y);
+    }
+    *reinterpret_cast<uint2 *>(static_cast<bf16 *>(f.out) + row * f.out_ld + col) = make_uint2(pack2(s.x, s.y), pack2(s.z, s.w));
+}
+
+// --------------------------------------------- dz = dy act'(z), and dbias
+// Blocks of kDzRows rows by 256 columns, a thread per 8 columns and every eighth row.  Bound by
+// its 6 bytes an element (2 without an activation).  The block's column sums go to
+// `part` [row blocks][N], which k_column_sum adds in order.
+constexpr int kDzRows = 128;
+struct DzArgs {
+    const bf16 *dy, *pre;
+    bf16 *dz;               // nullable (no activation: dy serves)
+    float *part;            // nullable (no dbias)
+    int64_t R, dy_ld, pre_ld;
+    int N, act;
+};
+__global__ void __launch_bounds__(256) k_dz(const DzArgs a) {
+    __shared__ float sums[8][256];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int col = blockIdx.y * 256 + lane * 8;
+    const int64_t r0 = (int64_t)blockIdx.x * kDzRows, r1 = min(a.R, r0 + kDzRows);
+    float s[8] = {};
+    if (col < a.N) {
+#pragma unroll 4
+        for (int64_t r = r0 + warp; r < r1; r += 8) {
+            const uint4 d = __ldg(reinterpret_cast<const uint4 *>(a.dy + r * a.dy_ld + col));
+            float v[8] = {lo16(d.x), hi16(d.x), lo16(d.y), hi16(d.y), lo16(d.z), hi16(d.z), lo16(d.w), hi16(d.w)};
+            if (a.dz) {
+                const uint4 p = __ldg(reinterpret_cast<const uint4 *>(a.pre + r * a.pre_ld + col));
+                const float z[8] = {lo16(p.x), hi16(p.x), lo16(p.y), hi16(p.y), lo16(p.z), hi16(p.z), lo16(p.w), hi16(p.w)};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= act_grad(a.act, z[i]);
+                *reinterpret_cast<uint4 *>(a.dz + r * a.N + col) =
+                    make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] += v[i];
+        }
+    }
+    if (!a.part) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[warp][lane * 8 + i] = s[i];
+    __syncthreads();
+    const int c = blockIdx.y * 256 + threadIdx.x;
+    if (c < a.N) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) t += sums[w][threadIdx.x];
+        a.part[(int64_t)blockIdx.x * a.N + c] = t;
+    }
+}
+// Column sums of part [n][N]: 32 columns a block, 32 row strides, then a fixed-order sum.
+__global__ void __launch_bounds__(1024) k_column_sum(const float *part, int64_t n, int N, float *out) {
+    __shared__ float sums[32][33];
+    const int c = threadIdx.x & 31, w = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+    float s = 0.f;
+    if (col < N)
+        for (int64_t r = w; r < n; r += 32) s += part[r * N + col];
+    sums[w][c] = s;
+    __syncthreads();
+    if (w == 0 && col < N) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t += sums[i][c];
+        out[col] = t;
+    }
+}
+
+// ---------------------------------------------------------------- host side
+using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+    static EncodeFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeFn>(p);
+    });
+    return fn;
+}
+
+// An operand: rows of `inner` contiguous bf16, `outer` of them, ld apart; boxes of 64 x box_rows.
+bool operand_map(CUtensorMap *map, const void *ptr, int64_t inner, int64_t outer, int64_t ld, int box_rows) {
+    EncodeFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+    cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    cuuint32_t one[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(ptr), dims, strides, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// An output [planes][rows][cols]: boxes of 64 bytes by 32 rows.
+bool output_map(CUtensorMap *map, void *ptr, bool f32, int64_t cols, int64_t rows, int64_t ld, int planes) {
+    EncodeFn fn = encode_fn();
+    if (!fn) return false;
+    const int es = f32 ? 4 : 2;
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    cuuint64_t strides[2] = {(cuuint64_t)ld * es, (cuuint64_t)ld * rows * es};
+    cuuint32_t box[3] = {(cuuint32_t)(64 / es), 32, 1};
+    cuuint32_t one[3] = {1, 1, 1};
+    return fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, ptr, dims, strides, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct GemmPlan {
+    int bn, splits, steps_per_split, steps, tiles_m, tiles_n;
+};
+
+// Tile width and splits: the least of rounds of CTAs times a CTA's steps (with two steps'
+// worth for its start), 128-wide tiles costing 1.2 of their share of a 256-wide one, and
+// splits the bytes of their partial sums (a step of a 256-wide tile moves 48 KB).
+GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K) {
+    GemmPlan best = {};
+    double best_cost = 0;
+    const int sms = sm_count();
+    for (int bn : {256, 128}) {
+        const int64_t tm = (M + kBM - 1) / kBM, tn = (N + bn - 1) / bn;
+        const int steps = (int)((K + kBK - 1) / kBK);
+        for (int splits = 1; splits <= 16 && splits <= steps; ++splits) {
+            const int per = (steps + splits - 1) / splits;
+            if ((steps + per - 1) / per != splits) continue;
+            if (splits > 1 && tm * tn * splits > sms) break;        // more work units than SMs: nothing to fill
+            const int64_t rounds = (tm * tn * splits + sms - 1) / sms;
+            const double step = bn == 256 ? 1.0 : 0.6;
+            double cost = (double)rounds * ((per + 2) * step + (bn == 256 ? 3.0 : 1.5));
+            if (splits > 1) cost += 8.0 + 8.0 * (double)splits * M * N / (6.0e12 * 0.3e-6);
+            if (best_cost == 0 || cost < best_cost) {
+                best_cost = cost;
+                best = {bn, splits, per, steps, (int)tm, (int)tn};
+            }
+        }
+    }
+    return best;
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+size_t gemm_ws(const GemmPlan &p, int64_t M, int64_t N) {
+    return p.splits > 1 ? round256((size_t)p.splits * M * N * sizeof(float)) : 0;
+}
+
+struct Operand {
+    const void *ptr;
+    int64_t ld;
+};
+struct Epilogue {
+    const float *bias = nullptr;
+    const bf16 *residual = nullptr;
+    int64_t residual_ld = 0;
+    int act = RLM_ACT_NONE;
+    void *out = nullptr;
+    int64_t out_ld = 0;
+    bool out_f32 = false;
+    void *pre = nullptr;
+    int64_t pre_ld = 0;
+};
+
+template <bool kAMn, bool kBMn, int kBN, bool kOutF32, int kAct>
+cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, const CUtensorMap &mp,
+                        const GemmArgs &g, cudaStream_t st) {
+    auto *fn = k_gemm<kAMn, kBMn, kBN, kOutF32, kAct>;
+    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<kBN>::kSmem);
+    if (e != cudaSuccess) return e;
+    const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits;
+    fn<<<(unsigned)std::min<int64_t>(units, sm_count()), kGemmThreads, GemmCfg<kBN>::kSmem, st>>>(ma, mb, mc, mp, g);
+    count_launches(1);
+    return cudaGetLastError();
+}
+
+template <bool kAMn, bool kBMn, int kBN>
+cudaError_t pick_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, const CUtensorMap &mp,
+                      const GemmArgs &g, bool f32, cudaStream_t st) {
+    if (f32) return launch_gemm<kAMn, kBMn, kBN, true, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
+    if constexpr (!kAMn && !kBMn) {         // only the forward product has an activation
+        switch (g.act) {
+            case RLM_ACT_SILU: return launch_gemm<kAMn, kBMn, kBN, false, RLM_ACT_SILU>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_GELU: return launch_gemm<kAMn, kBMn, kBN, false, RLM_ACT_GELU>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_SIGMOID: return launch_gemm<kAMn, kBMn, kBN, false, RLM_ACT_SIGMOID>(ma, mb, mc, mp, g, st);
+            default: break;
+        }
+    }
+    return launch_gemm<kAMn, kBMn, kBN, false, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
+}
+
+template <bool kAMn, bool kBMn>
+cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Epilogue &ep, float *part, cudaStream_t st) {
+    const GemmPlan p = gemm_plan(M, N, K);
+    CUtensorMap ma, mb, mc, mp;
+    if (!(kAMn ? operand_map(&ma, a.ptr, M, K, a.ld, 64) : operand_map(&ma, a.ptr, K, M, a.ld, kBM)) ||
+        !(kBMn ? operand_map(&mb, b.ptr, N, K, b.ld, 64) : operand_map(&mb, b.ptr, K, N, b.ld, p.bn)))
+        return cudaErrorInvalidValue;
+    const bool split = p.splits > 1;
+    if (!(split ? output_map(&mc, part, true, N, M, N, p.splits)
+                : output_map(&mc, ep.out, ep.out_f32, N, M, ep.out_ld, 1)))
+        return cudaErrorInvalidValue;
+    mp = mc;
+    if (!split && ep.pre && !output_map(&mp, ep.pre, false, N, M, ep.pre_ld, 1)) return cudaErrorInvalidValue;
+    GemmArgs g = {};
+    g.M = (int)M, g.N = (int)N, g.K = (int)K;
+    g.tiles_m = p.tiles_m, g.tiles_n = p.tiles_n;
+    g.splits = p.splits, g.steps_per_split = p.steps_per_split, g.steps = p.steps;
+    if (!split) {
+        g.bias = ep.bias;
+        g.residual = ep.residual;
+        g.residual_ld = ep.residual_ld;
+        g.act = ep.act;
+        g.want_pre = ep.pre != nullptr;
+    }
+    const bool f32 = split || ep.out_f32;
+    cudaError_t e = p.bn == 256 ? pick_gemm<kAMn, kBMn, 256>(ma, mb, mc, mp, g, f32, st)
+                                : pick_gemm<kAMn, kBMn, 128>(ma, mb, mc, mp, g, f32, st);
+    if (e != cudaSuccess || !split) return e;
+    FinishArgs f = {};
+    f.part = part;
+    f.M = M;
+    f.N = (int)N;
+    f.splits = p.splits;
+    f.act = ep.act;
+    f.out_f32 = ep.out_f32;
+    f.bias = ep.bias;
+    f.residual = ep.residual;
+    f.residual_ld = ep.residual_ld;
+    f.out = ep.out;
+    f.out_ld = ep.out_ld;
+    f.pre = static_cast<bf16 *>(ep.pre);
+    f.pre_ld = ep.pre_ld;
+    k_finish<<<(unsigned)((M * (N / 4) + 255) / 256), 256, 0, st>>>(f);
+    count_launches(1);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t linear_ws_bytes(int64_t R, int64_t K, int64_t N) { return gemm_ws(gemm_plan(R, N, K), R, N); }
+
+size_t linear_backward_ws_bytes(int64_t R, int64_t K, int64_t N, int act) {
+    const size_t dz = act == RLM_ACT_NONE ? 0 : round256((size_t)R * N * 2);
+    const size_t sums = round256((size_t)((R + kDzRows - 1) / kDzRows) * N * sizeof(float));
+    return dz + sums + std::max(gemm_ws(gemm_plan(R, K, N), R, K), gemm_ws(gemm_plan(N, K, R), N, K));
+}
+
+cudaError_t linear_forward(const rlm_matrix &x, const rlm_matrix &w, const float *bias, int act_kind,
+                           const rlm_matrix *residual, const rlm_matrix *pre, const rlm_matrix &y, void *ws,
+                           cudaStream_t st) {
+    Epilogue ep;
+    ep.bias = bias;
+    ep.act = act_kind;
+    if (residual) {
+        ep.residual = static_cast<const bf16 *>(residual->ptr);
+        ep.residual_ld = residual->ld;
+    }
+    if (pre) {
+        ep.pre = pre->ptr;
+        ep.pre_ld = pre->ld;
+    }
+    ep.out = y.ptr;
+    ep.out_ld = y.ld;
+    return gemm<false, false>({x.ptr, x.ld}, {w.ptr, w.ld}, x.rows, w.rows, x.cols, ep, static_cast<float *>(ws), st);
+}
+
+cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm_matrix &w, const rlm_matrix *pre,
+                            int act_kind, const rlm_matrix *dx, const rlm_matrix *dw, float *dbias, void *ws,
+                            cudaStream_t st) {
+    const int64_t R = x.rows, K = x.cols, N = w.rows;
+    char *at = static_cast<char *>(ws);
+    Operand dz = {dy.ptr, dy.ld};
+    if (act_kind != RLM_ACT_NONE || dbias) {
+        DzArgs a = {};
+        a.dy = static_cast<const bf16 *>(dy.ptr);
+        a.dy_ld = dy.ld;
+        a.R = R;
+        a.N = (int)N;
+        a.act = act_kind;
+        if (act_kind != RLM_ACT_NONE) {
+            a.pre = static_cast<const bf16 *>(pre->ptr);
+            a.pre_ld = pre->ld;
+            a.dz = reinterpret_cast<bf16 *>(at);
+            at += round256((size_t)R * N * 2);
+            dz = {a.dz, N};
+        }
+        const int64_t blocks = (R + kDzRows - 1) / kDzRows;
+        if (dbias) a.part = reinterpret_cast<float *>(at);
+        at += round256((size_t)blocks * N * sizeof(float));
+        k_dz<<<dim3((unsigned)blocks, (unsigned)((N + 255) / 256)), 256, 0, st>>>(a);
+        count_launches(1);
+        cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        if (dbias) {
+            k_column_sum<<<(unsigned)((N + 31) / 32), 1024, 0, st>>>(a.part, blocks, (int)N, dbias);
+            count_launches(1);
+            if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        }
+    }
+    float *part = reinterpret_cast<float *>(at);
+    if (dx) {
+        Epilogue ep;
+        ep.out = dx->ptr;
+        ep.out_ld = dx->ld;
+        const cudaError_t e = gemm<false, true>(dz, {w.ptr, w.ld}, R, K, N, ep, part, st);
+        if (e != cudaSuccess) return e;
+    }
+    if (dw) {
+        Epilogue ep;
+        ep.out = dw->ptr;
+        ep.out_ld = dw->ld;
+        ep.out_f32 = dw->dtype == RLM_F32;
+        return gemm<true, true>(dz, {x.ptr, x.ld}, N, K, R, ep, part, st);
+    }
+    return cudaSuccess;
+}
+
+cudaError_t read_and_clear_linear_status(int *status, cudaStream_t st) {
+    cudaError_t e = cudaMemcpyFromSymbolAsync(status, g_linear_status, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
+    if (e != cudaSuccess) return e;
+    if ((e = cudaStreamSynchronize(st)) != cudaSuccess) return e;
+    if (*status == RLM_OK) return cudaSuccess;
+    const int zero = 0;
+    if ((e = cudaMemcpyToSymbolAsync(g_linear_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, st)) != cudaSuccess)
+        return e;
+    return cudaStreamSynchronize(st);
+}
+
+}  // namespace rlm

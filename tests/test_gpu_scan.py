@@ -1,7 +1,7 @@
 """The gated linear recurrence on the GPU against the token-by-token fp64 recurrence.
 
-Tolerances.  bf16 fields: one rounding of an fp32 result, at most 2^-9 of the element, so
-2^-8 of the norm and of the largest element leaves a factor of two for the fp32 part.
+Tolerances.  bf16 fields: one rounding of an fp32 result, at most 2^-8 of the element: 2^-8
+of the norm and of the largest element (the fp32 part is below the rounding of a tie).
 fp32: a state remembers 1 / (1 - a) tokens, up to about 3000 for the gates drawn here,
 each step rounding by 2^-24 of the state: at most 2e-4 if all errors align, about
 sqrt(3000) 2^-24 = 3e-6 if they do not; 2e-5 of the norm and 1e-4 of the largest."""
