@@ -407,6 +407,45 @@ RLM_API rlm_status rlm_linear_backward(const rlm_matrix *dy, const rlm_matrix *x
 RLM_API size_t rlm_linear_workspace_size(int64_t R, int64_t K, int64_t N);
 RLM_API size_t rlm_linear_backward_workspace_size(int64_t R, int64_t K, int64_t N, rlm_act act);
 
+/* --------------------------------------------------------------- optimizer
+ * One AdamW step (decoupled weight decay) over many tensors, in place:
+ *
+ *   g' = s g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
+ *   p = p (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *
+ * Weights and gradients are RLM_F32 or RLM_BF16 (one type each for the call); moments are
+ * fp32 (bits = 32) or 8-bit floats (bits = 8).  With a master copy (bf16 weights only) the
+ * step reads and writes the fp32 master and the weight receives it rounded; without one,
+ * bf16 weights are rounded to nearest at every step.
+ *
+ * 8-bit moments: exp_avg holds m and exp_avg_sq holds sqrt(v) as E4M3 codes (4 exponent
+ * bits, 3 mantissa bits, one byte each) of blocks of RLM_ADAMW_BLOCK values; value = code *
+ * scale of its block, the scale a power of two.  All-zero codes with any finite scale are
+ * zero moments.  A nonzero sqrt(v) is never rounded to zero. */
+#define RLM_ADAMW_BLOCK 256
+
+typedef struct {
+    void *param;
+    const void *grad;
+    void *exp_avg, *exp_avg_sq;                     /* fp32 [n], or codes [n] */
+    float *exp_avg_scale, *exp_avg_sq_scale;        /* 8-bit moments: fp32 [ceil(n / RLM_ADAMW_BLOCK)] */
+    float *master;                                  /* fp32 [n], or NULL for every tensor of the call */
+    int64_t n;                                      /* >= 1 */
+} rlm_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;     /* lr, eps, wd >= 0; betas in [0, 1) */
+    int64_t step;                                   /* t, >= 1 */
+} rlm_adamw_hyper;
+
+/* tensors: HOST array of count entries (>= 1), read before the call returns; buffers of a
+ * call must not overlap.  Any n and any element alignment; 16-byte aligned buffers (8 for
+ * codes) move fastest.  grad_scale: nullable device scalar s (1 if NULL); if it is not
+ * finite the step changes nothing.  Non-finite gradients are not looked for.  One launch
+ * per 400 tensors, no workspace. */
+RLM_API rlm_status rlm_adamw_step(const rlm_adamw_tensor *tensors, int count, rlm_dtype param, rlm_dtype grad, int bits,
+                                  const rlm_adamw_hyper *hyper, const float *grad_scale, const rlm_launch *launch);
+
 /* ------------------------------------------------------------------ utility
  * rlm_validate_params: copies p to the host (synchronous) and checks that every
  * value is finite and every gamma >= 0 (Sec. 3.1 requires alpha > 0; gamma = 0

@@ -28,6 +28,7 @@ __all__ = [
     "rlm_prefill_workspace_size", "rlm_backward_workspace_size",
     "rlm_scan_prefill", "rlm_scan_backward", "rlm_scan_decode", "rlm_scan_saved_size", "scan_saved",
     "rlm_linear", "rlm_linear_backward", "rlm_linear_workspace_size", "rlm_linear_backward_workspace_size",
+    "AdamState", "AdamGroup", "rlm_adamw_step",
     "rlm_validate_params", "rlm_get_device_status", "rlm_status_string",
     "rlm_version", "rlm_kernels_launched", "RLM_OK", "RLM_ERR_INVALID_ARG", "RLM_ERR_UNSUPPORTED",
     "RLM_ERR_CUDA", "RLM_ERR_TIMEOUT", "RLM_F32", "RLM_BF16",
@@ -79,6 +80,17 @@ class _Strided(ctypes.Structure):
 class _Matrix(ctypes.Structure):
     _fields_ = [("ptr", ctypes.c_void_p), ("dtype", ctypes.c_int),
                 ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64)]
+
+
+class _AdamTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p),
+                ("exp_avg_sq", ctypes.c_void_p), ("exp_avg_scale", ctypes.c_void_p),
+                ("exp_avg_sq_scale", ctypes.c_void_p), ("master", ctypes.c_void_p), ("n", ctypes.c_int64)]
+
+
+class _AdamHyper(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64)]
 
 
 class _Launch(ctypes.Structure):
@@ -158,7 +170,8 @@ def load_library(build_if_missing: bool = False) -> ctypes.CDLL:
     lib.rlm_linear_backward.argtypes = [X, X, X, X, I, X, X, V, P(_Launch)]
     lib.rlm_linear_workspace_size.argtypes = [Q, Q, Q]
     lib.rlm_linear_backward_workspace_size.argtypes = [Q, Q, Q, I]
-    for f in ("rlm_linear", "rlm_linear_backward"):
+    lib.rlm_adamw_step.argtypes = [P(_AdamTensor), I, I, I, I, P(_AdamHyper), V, P(_Launch)]
+    for f in ("rlm_linear", "rlm_linear_backward", "rlm_adamw_step"):
         getattr(lib, f).restype = ctypes.c_int
     for f in ("rlm_linear_workspace_size", "rlm_linear_backward_workspace_size"):
         getattr(lib, f).restype = ctypes.c_size_t
@@ -662,3 +675,90 @@ def rlm_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, dx: 
     _check(lib.rlm_linear_backward(ctypes.byref(dyt), ctypes.byref(xt), ctypes.byref(wt), ref(pt), _act(act), ref(dxt),
                                    ref(dwt), _opt(dbias, torch.float32, (wt.rows,), "dbias"),
                                    ctypes.byref(_launch(stream, workspace))), "rlm_linear_backward")
+
+
+# --------------------------------------------------------------- optimizer
+ADAMW_BLOCK = 256       # RLM_ADAMW_BLOCK: values that share a scale of the 8-bit moments
+
+
+@dataclass
+class AdamState:
+    """Moments of one tensor of n values: m and v float32 [n], or (8 bits) codes float8_e4m3fn
+    [n] of m and of sqrt(v) with the scales float32 [ceil(n / 256)] of their blocks."""
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scale: torch.Tensor | None = None
+    v_scale: torch.Tensor | None = None
+
+    @classmethod
+    def zeros(cls, param: torch.Tensor, bits: int = 32):
+        n, dev = param.numel(), param.device
+        if bits == 32:
+            return cls(*(torch.zeros(n, dtype=torch.float32, device=dev) for _ in range(2)))
+        if bits != 8:
+            raise ValueError(f"bits must be 8 or 32, got {bits}")
+        k = -(-n // ADAMW_BLOCK)
+        return cls(*(torch.zeros(n, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn) for _ in range(2)),
+                   *(torch.ones(k, dtype=torch.float32, device=dev) for _ in range(2)))
+
+    @property
+    def bits(self) -> int:
+        return 32 if self.m.dtype == torch.float32 else 8
+
+    def values(self) -> tuple[torch.Tensor, torch.Tensor]:
+        """m and v as float32, whatever they are kept in."""
+        if self.bits == 32:
+            return self.m, self.v
+        wide = lambda s: s.repeat_interleave(ADAMW_BLOCK)[: self.m.numel()]
+        return self.m.float() * wide(self.m_scale), (self.v.float() * wide(self.v_scale)).square()
+
+
+class AdamGroup:
+    """The tensors of an optimizer step, checked and laid out once: weights (float32 or
+    bfloat16), gradients (float32 or bfloat16), their AdamState and, for bfloat16 weights,
+    optional float32 master copies.  It keeps the tensors; gradients are read from the same
+    buffers at every step."""
+
+    def __init__(self, params, grads, states, masters=None):
+        params, grads, states = list(params), list(grads), list(states)
+        masters = [None] * len(params) if masters is None else list(masters)
+        if not params or not len(params) == len(grads) == len(states) == len(masters):
+            raise ValueError("AdamGroup needs as many grads, states (and masters) as params, and at least one")
+        self.tensors = params, grads, states, masters
+        self.param_dtype, self.grad_dtype, self.bits = params[0].dtype, grads[0].dtype, states[0].bits
+        if self.param_dtype not in _DT or self.grad_dtype not in _DT:
+            raise ValueError(f"weights are {self.param_dtype}, gradients {self.grad_dtype}: need float32 or bfloat16")
+        self._c = (_AdamTensor * len(params))()
+        code = torch.float32 if self.bits == 32 else torch.float8_e4m3fn
+        self.device = params[0].device
+        for i, (p, g, s, w) in enumerate(zip(params, grads, states, masters)):
+            n = p.numel()
+            need = [(p, self.param_dtype, n, "weight"), (g, self.grad_dtype, n, "gradient"), (s.m, code, n, "m"),
+                    (s.v, code, n, "v")]
+            if w is not None:
+                need.append((w, torch.float32, n, "master"))
+            if self.bits == 8:
+                k = -(-n // ADAMW_BLOCK)
+                need += [(s.m_scale, torch.float32, k, "m_scale"), (s.v_scale, torch.float32, k, "v_scale")]
+            for t, dtype, size, name in need:
+                if t is None or t.dtype != dtype or t.numel() != size or not t.is_contiguous() or not t.is_cuda \
+                        or t.device != self.device:
+                    raise ValueError(f"tensor {i}: {name} must be a contiguous {dtype} tensor of {size} values on "
+                                     f"{self.device}")
+            ptr = lambda t: t.data_ptr() if t is not None else None
+            self._c[i] = _AdamTensor(ptr(p), ptr(g), ptr(s.m), ptr(s.v), ptr(s.m_scale) if self.bits == 8 else None,
+                                     ptr(s.v_scale) if self.bits == 8 else None, ptr(w), n)
+
+
+def rlm_adamw_step(group: AdamGroup, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+                   eps: float = 1e-8, weight_decay: float = 0.01, grad_scale: torch.Tensor | None = None,
+                   stream=None) -> None:
+    """One AdamW step (``step`` counts from 1) over a group's tensors, in place.  ``grad_scale``, a float32
+    CUDA scalar, multiplies every gradient; a value that is not finite skips the step."""
+    if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or not grad_scale.is_cuda):
+        raise ValueError("grad_scale must be a CUDA float32 scalar")
+    h = _AdamHyper(lr, beta1, beta2, eps, weight_decay, step)
+    _check(load_library().rlm_adamw_step(group._c, len(group._c), _DT[group.param_dtype], _DT[group.grad_dtype],
+                                         group.bits, ctypes.byref(h),
+                                         grad_scale.data_ptr() if grad_scale is not None else None,
+                                         ctypes.byref(_launch(stream, None))), "rlm_adamw_step")
