@@ -339,29 +339,30 @@ def _field(t: torch.Tensor) -> _Tensor:
 
 def _strided(t: torch.Tensor, name: str) -> _Strided:
     """A [B][L][D] (or, for one token, [B][D]) field, possibly a view with row strides."""
-    if t.dtype not in _DT:
+    dt, shape, st = _DT.get(t.dtype), t.shape, t.stride()
+    if dt is None:
         raise ValueError(f"{name}: unsupported dtype {t.dtype}")
-    if not t.is_cuda or t.dim() not in (2, 3) or t.stride(-1) != 1:
+    if not t.is_cuda or len(shape) not in (2, 3) or st[-1] != 1:
         raise ValueError(f"{name} must be a CUDA [B][L][D] (or [B][D]) tensor with unit channel stride, got "
-                         f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
-    if t.dim() == 2:
-        (B, D), L = t.shape, 1
-        return _Strided(t.data_ptr(), _DT[t.dtype], B, L, D, t.stride(0), D)
-    B, L, D = t.shape
-    return _Strided(t.data_ptr(), _DT[t.dtype], B, L, D, t.stride(0), t.stride(1))
+                         f"{tuple(shape)} with strides {st} on {t.device}")
+    if len(shape) == 2:
+        return _Strided(t.data_ptr(), dt, shape[0], 1, shape[1], st[0], shape[1])
+    return _Strided(t.data_ptr(), dt, *shape, st[0], st[1])
 
 
 def _matrix(t: torch.Tensor, name: str) -> _Matrix:
     """A row-major matrix [...][cols] whose leading dimensions share one row pitch."""
-    if t.dtype not in _DT:
+    dt, shape, st = _DT.get(t.dtype), t.shape, t.stride()
+    if dt is None:
         raise ValueError(f"{name}: unsupported dtype {t.dtype}")
-    if not t.is_cuda or t.dim() < 2 or t.stride(-1) != 1:
-        raise ValueError(f"{name} must be a CUDA matrix [...][cols] with unit column stride, got {tuple(t.shape)} with "
-                         f"strides {t.stride()} on {t.device}")
-    if t.dim() > 2:
-        t = t.view(-1, t.shape[-1])        # raises where the rows do not share one pitch
-    rows, cols = t.shape
-    return _Matrix(t.data_ptr(), _DT[t.dtype], rows, cols, t.stride(0) if rows > 1 else cols)
+    if not t.is_cuda or len(shape) < 2 or st[-1] != 1:
+        raise ValueError(f"{name} must be a CUDA matrix [...][cols] with unit column stride, got {tuple(shape)} with "
+                         f"strides {st} on {t.device}")
+    if len(shape) > 2:
+        t = t.view(-1, shape[-1])          # raises where the rows do not share one pitch
+        shape, st = t.shape, t.stride()
+    rows, cols = shape
+    return _Matrix(t.data_ptr(), dt, rows, cols, st[0] if rows > 1 else cols)
 
 
 def _opt(t: torch.Tensor | None, dtype, shape, name: str):
@@ -376,7 +377,7 @@ def _opt(t: torch.Tensor | None, dtype, shape, name: str):
 
 def _stream(stream) -> int:
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)
@@ -590,12 +591,12 @@ def rlm_scan_prefill(x: torch.Tensor, g: torch.Tensor, y: torch.Tensor, leak: bo
     lib = load_library()
     xt, gt, yt = _strided(x, "x"), _strided(g, "g"), _strided(y, "y")
     B, L, D = xt.B, xt.L, xt.D
-    _check(lib.rlm_scan_prefill(ctypes.byref(xt), ctypes.byref(gt), int(leak),
-                                _opt(state_in, torch.float32, (B, D), "state_in"), ctypes.byref(yt),
+    _check(lib.rlm_scan_prefill(xt, gt, int(leak),
+                                _opt(state_in, torch.float32, (B, D), "state_in"), yt,
                                 _opt(state_out, torch.float32, (B, D), "state_out"),
                                 _opt(saved, torch.float32, (B, -(-L // SCAN_CHUNK), D), "saved"),
                                 _opt(lengths, torch.int32, (B,), "lengths"),
-                                ctypes.byref(_launch(stream, None))), "rlm_scan_prefill")
+                                _launch(stream, None)), "rlm_scan_prefill")
 
 
 def rlm_scan_backward(dy: torch.Tensor, x: torch.Tensor, g: torch.Tensor, saved: torch.Tensor, dx: torch.Tensor,
@@ -608,21 +609,21 @@ def rlm_scan_backward(dy: torch.Tensor, x: torch.Tensor, g: torch.Tensor, saved:
     dyt, xt, gt = _strided(dy, "dy"), _strided(x, "x"), _strided(g, "g")
     dxt, dgt = _strided(dx, "dx"), _strided(dg, "dg")
     B, L, D = xt.B, xt.L, xt.D
-    _check(lib.rlm_scan_backward(ctypes.byref(dyt), ctypes.byref(xt), ctypes.byref(gt),
+    _check(lib.rlm_scan_backward(dyt, xt, gt,
                                  _opt(saved, torch.float32, (B, -(-L // SCAN_CHUNK), D), "saved"), int(leak),
-                                 _opt(d_state_out, torch.float32, (B, D), "d_state_out"), ctypes.byref(dxt),
-                                 ctypes.byref(dgt), _opt(d_state_in, torch.float32, (B, D), "d_state_in"),
+                                 _opt(d_state_out, torch.float32, (B, D), "d_state_out"), dxt,
+                                 dgt, _opt(d_state_in, torch.float32, (B, D), "d_state_in"),
                                  _opt(lengths, torch.int32, (B,), "lengths"),
-                                 ctypes.byref(_launch(stream, None))), "rlm_scan_backward")
+                                 _launch(stream, None)), "rlm_scan_backward")
 
 
 def rlm_scan_decode(x_t: torch.Tensor, g_t: torch.Tensor, state: torch.Tensor, y_t: torch.Tensor, leak: bool = True,
                     stream=None) -> None:
     """One token of the gated linear recurrence; ``state`` (float32 [B][D]) advances in place."""
     xt, gt, yt = _strided(x_t, "x_t"), _strided(g_t, "g_t"), _strided(y_t, "y_t")
-    _check(load_library().rlm_scan_decode(ctypes.byref(xt), ctypes.byref(gt), int(leak),
-                                          _opt(state, torch.float32, (xt.B, xt.D), "state"), ctypes.byref(yt),
-                                          ctypes.byref(_launch(stream, None))), "rlm_scan_decode")
+    _check(load_library().rlm_scan_decode(xt, gt, int(leak),
+                                          _opt(state, torch.float32, (xt.B, xt.D), "state"), yt,
+                                          _launch(stream, None)), "rlm_scan_decode")
 
 
 # ------------------------------------------------------------ linear layer
@@ -655,9 +656,8 @@ def rlm_linear(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, bias: torch.Te
     pt = _matrix(pre, "pre") if pre is not None else None
     if workspace is None:
         workspace = _workspace(lib.rlm_linear_workspace_size(xt.rows, xt.cols, wt.rows), x.device)
-    ref = lambda c: ctypes.byref(c) if c is not None else None
-    _check(lib.rlm_linear(ctypes.byref(xt), ctypes.byref(wt), _opt(bias, torch.float32, (wt.rows,), "bias"), _act(act),
-                          ref(rt), ref(pt), ctypes.byref(yt), ctypes.byref(_launch(stream, workspace))), "rlm_linear")
+    _check(lib.rlm_linear(xt, wt, _opt(bias, torch.float32, (wt.rows,), "bias"), _act(act),
+                          rt, pt, yt, _launch(stream, workspace)), "rlm_linear")
 
 
 def rlm_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, dx: torch.Tensor | None = None,
@@ -671,10 +671,9 @@ def rlm_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, dx: 
     pt, dxt, dwt = opt(pre, "pre"), opt(dx, "dx"), opt(dw, "dw")
     if workspace is None:
         workspace = _workspace(lib.rlm_linear_backward_workspace_size(xt.rows, xt.cols, wt.rows, _act(act)), x.device)
-    ref = lambda c: ctypes.byref(c) if c is not None else None
-    _check(lib.rlm_linear_backward(ctypes.byref(dyt), ctypes.byref(xt), ctypes.byref(wt), ref(pt), _act(act), ref(dxt),
-                                   ref(dwt), _opt(dbias, torch.float32, (wt.rows,), "dbias"),
-                                   ctypes.byref(_launch(stream, workspace))), "rlm_linear_backward")
+    _check(lib.rlm_linear_backward(dyt, xt, wt, pt, _act(act), dxt,
+                                   dwt, _opt(dbias, torch.float32, (wt.rows,), "dbias"),
+                                   _launch(stream, workspace)), "rlm_linear_backward")
 
 
 # --------------------------------------------------------------- optimizer
@@ -759,6 +758,6 @@ def rlm_adamw_step(group: AdamGroup, step: int, lr: float, beta1: float = 0.9, b
         raise ValueError("grad_scale must be a CUDA float32 scalar")
     h = _AdamHyper(lr, beta1, beta2, eps, weight_decay, step)
     _check(load_library().rlm_adamw_step(group._c, len(group._c), _DT[group.param_dtype], _DT[group.grad_dtype],
-                                         group.bits, ctypes.byref(h),
+                                         group.bits, h,
                                          grad_scale.data_ptr() if grad_scale is not None else None,
-                                         ctypes.byref(_launch(stream, None))), "rlm_adamw_step")
+                                         _launch(stream, None)), "rlm_adamw_step")

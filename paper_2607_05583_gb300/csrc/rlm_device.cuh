@@ -50,6 +50,34 @@ __device__ __forceinline__ float2 lambda_pow(float gamma, float omega, float n) 
     return make_float2(r * fmaf(-pe, sp, cp), r * fmaf(pe, cp, sp));
 }
 
+// Two fp32 values in one 64-bit register, and the packed arithmetic on them (each half
+// rounded as the scalar operation rounds it).
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pack(float2 v) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+    return r;
+}
+__device__ __forceinline__ float2 unpack(f32x2 v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 // c = A exp(i phi).
 __device__ __forceinline__ float2 mode_coef(float amp, float phase) {
     float s, c;

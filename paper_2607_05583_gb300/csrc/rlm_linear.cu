@@ -21,7 +21,9 @@
 // dz is rounded to bf16 once, the operand type of the two products that read it; dbias is
 // summed from the fp32 values.
 #include <algorithm>
+#include <atomic>
 #include <mutex>
+#include <type_traits>
 #include <vector>
 
 #include "rlm_device.cuh"
@@ -358,6 +360,93 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(2 * kBN));
 }
 
+// ---------------------------------------------------------------- few rows
+// R <= 8 kTok rows (serving): bound by reading w once.  A 128-row tile would do 128 / R
+// times the work on too few CTAs, so here 16 kRows rows of w are a CTA's: w is the 16-row
+// operand of mma.sync (m16n8k16), tokens its 8 columns.  Eight warps share the contraction
+// in 32-long blocks.  The order of the products within a block is free as long as both
+// operands agree, so a lane takes 8 consecutive k of its rows by one 16-byte load from
+// global memory, straight into the fragments: no shared memory, no shuffles.  The warps'
+// sums are added in order in shared memory.
+struct FewArgs {
+    const bf16 *x, *w, *residual;
+    const float *bias;
+    bf16 *y, *pre;
+    int64_t x_ld, w_ld, residual_ld, y_ld, pre_ld;
+    int R, N, K, act;
+};
+__device__ __forceinline__ uint4 load_w(const bf16 *p) {
+    uint4 v;
+    asm("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+constexpr int kFewWarps = 16;
+
+template <int kTok, int kRows>
+__global__ void __launch_bounds__(kFewWarps * 32) k_few(const FewArgs a) {
+    __shared__ float part[kFewWarps][16 * kRows][8 * kTok + 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+    const int n0 = blockIdx.x * 16 * kRows;
+    const bf16 *wp[2 * kRows], *xp[kTok];
+#pragma unroll
+    for (int i = 0; i < 2 * kRows; ++i) wp[i] = a.w + (int64_t)min(n0 + i * 8 + g, a.N - 1) * a.w_ld + q * 8;
+#pragma unroll
+    for (int i = 0; i < kTok; ++i) xp[i] = a.x + (int64_t)min(i * 8 + g, a.R - 1) * a.x_ld + q * 8;
+    float d[kRows][kTok][4] = {};
+    constexpr int kDeep = kRows + kTok > 4 ? 2 : 4;         // blocks in flight
+    auto blocks = [&](int k, auto whole) {
+        uint4 w[kDeep][2 * kRows], x[kDeep][kTok];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+            const int at = k + u * kFewWarps * 32;
+            const bool ok = decltype(whole)::value || at + q * 8 < a.K;
+#pragma unroll
+            for (int i = 0; i < 2 * kRows; ++i) w[u][i] = ok ? load_w(wp[i] + at) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < kTok; ++i)
+                x[u][i] = ok ? __ldg(reinterpret_cast<const uint4 *>(xp[i] + at)) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+#pragma unroll
+                for (int t = 0; t < kTok; ++t) {
+                    mma16816(d[r][t], w[u][2 * r].x, w[u][2 * r + 1].x, w[u][2 * r].y, w[u][2 * r + 1].y, x[u][t].x, x[u][t].y);
+                    mma16816(d[r][t], w[u][2 * r].z, w[u][2 * r + 1].z, w[u][2 * r].w, w[u][2 * r + 1].w, x[u][t].z, x[u][t].w);
+                }
+    };
+    int k = warp * 32;
+    for (; k + (kDeep - 1) * kFewWarps * 32 + 32 <= a.K; k += kDeep * kFewWarps * 32) blocks(k, std::true_type{});
+    if (k < a.K) blocks(k, std::false_type{});
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int t = 0; t < kTok; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[warp][r * 16 + (i >> 1) * 8 + g][t * 8 + q * 2 + (i & 1)] = d[r][t][i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * kRows * 8 * kTok; i += kFewWarps * 32) {
+        const int n = i % (16 * kRows), t = i / (16 * kRows), col = n0 + n;
+        if (t >= a.R || col >= a.N) continue;
+        float z = 0.f;
+#pragma unroll
+        for (int w = 0; w < kFewWarps; ++w) z += part[w][n][t];
+        if (a.bias) z += __ldg(a.bias + col);
+        if (a.pre) a.pre[t * a.pre_ld + col] = __float2bfloat16_rn(z);
+        z = act_of(a.act, z);
+        if (a.residual) z += __bfloat162float(a.residual[t * a.residual_ld + col]);
+        a.y[t * a.y_ld + col] = __float2bfloat16_rn(z);
+    }
+}
+
 // ------------------------------------------------- sums of split products
 // part [splits][M][N] fp32, added in order, then the epilogue; a thread per 4 columns.
 struct FinishArgs {
@@ -560,8 +649,15 @@ template <bool kAMn, bool kBMn, int kBN, bool kOutF32, int kAct>
 cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, const CUtensorMap &mp,
                         const GemmArgs &g, cudaStream_t st) {
     auto *fn = k_gemm<kAMn, kBMn, kBN, kOutF32, kAct>;
-    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<kBN>::kSmem);
-    if (e != cudaSuccess) return e;
+    static std::atomic<unsigned long long> set{0};          // devices that have the kernel's shared memory size
+    int dev = 0;
+    cudaGetDevice(&dev);
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (!(set.load(std::memory_order_relaxed) & bit)) {
+        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<kBN>::kSmem);
+        if (e != cudaSuccess) return e;
+        set.fetch_or(bit, std::memory_order_relaxed);
+    }
     const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits;
     fn<<<(unsigned)std::min<int64_t>(units, sm_count()), kGemmThreads, GemmCfg<kBN>::kSmem, st>>>(ma, mb, mc, mp, g);
     count_launches(1);
@@ -632,7 +728,23 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
 
 }  // namespace
 
-size_t linear_ws_bytes(int64_t R, int64_t K, int64_t N) { return gemm_ws(gemm_plan(R, N, K), R, N); }
+// Rows that k_few serves; see the table at linear_forward.
+constexpr int kFewRows = 32;
+constexpr bool kTwo = false;
+
+template <int kTok>
+void launch_few(const FewArgs &a, cudaStream_t st) {
+    // 32 rows of w a CTA where that still gives every SM one.
+    if (kTwo && a.N >= 32 * sm_count() * 3 / 4)
+        k_few<kTok, 2><<<(unsigned)((a.N + 31) / 32), kFewWarps * 32, 0, st>>>(a);
+    else
+        k_few<kTok, 1><<<(unsigned)((a.N + 15) / 16), kFewWarps * 32, 0, st>>>(a);
+    count_launches(1);
+}
+
+size_t linear_ws_bytes(int64_t R, int64_t K, int64_t N) {
+    return R <= kFewRows ? 0 : gemm_ws(gemm_plan(R, N, K), R, N);
+}
 
 size_t linear_backward_ws_bytes(int64_t R, int64_t K, int64_t N, int act) {
     const size_t dz = act == RLM_ACT_NONE ? 0 : round256((size_t)R * N * 2);
@@ -643,6 +755,24 @@ size_t linear_backward_ws_bytes(int64_t R, int64_t K, int64_t N, int act) {
 cudaError_t linear_forward(const rlm_matrix &x, const rlm_matrix &w, const float *bias, int act_kind,
                            const rlm_matrix *residual, const rlm_matrix *pre, const rlm_matrix &y, void *ws,
                            cudaStream_t st) {
+    if (x.rows <= kFewRows) {
+        FewArgs a = {};
+        a.x = static_cast<const bf16 *>(x.ptr), a.x_ld = x.ld;
+        a.w = static_cast<const bf16 *>(w.ptr), a.w_ld = w.ld;
+        a.y = static_cast<bf16 *>(y.ptr), a.y_ld = y.ld;
+        if (residual) a.residual = static_cast<const bf16 *>(residual->ptr), a.residual_ld = residual->ld;
+        if (pre) a.pre = static_cast<bf16 *>(pre->ptr), a.pre_ld = pre->ld;
+        a.bias = bias;
+        a.R = (int)x.rows, a.N = (int)w.rows, a.K = (int)x.cols;
+        a.act = act_kind;
+        if (a.R <= 8)
+            launch_few<1>(a, st);
+        else if (a.R <= 16)
+            launch_few<2>(a, st);
+        else
+            launch_few<4>(a, st);
+        return cudaGetLastError();
+    }
     Epilogue ep;
     ep.bias = bias;
     ep.act = act_kind;

@@ -91,33 +91,6 @@ struct ScanArgs {
     int L, D, groups, nseg, ntiles, nchunks;
 };
 
-// Two channels' values in one 64-bit register.
-using f32x2 = unsigned long long;
-__device__ __forceinline__ f32x2 pack(float2 v) {
-    f32x2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
-    return r;
-}
-__device__ __forceinline__ float2 unpack(f32x2 v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-    f32x2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 constexpr f32x2 kOne = 0x3f8000003f800000ull, kMinus = 0xbf800000bf800000ull;
 
 // (A, H) of two channels as (A.x, A.y, H.x, H.y); `later` o `earlier`.
@@ -807,9 +780,7 @@ cudaError_t launch_scan(bool backward, bool leak, ScanArgs<T> &a, int64_t B, cud
     a.nseg = p.nseg;
     a.ntiles = p.ntiles;
     a.nchunks = (a.L + kChunk - 1) / kChunk;
-    cudaError_t e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
+    cudaLaunchConfig_t cfg = {};                // resident() has set the kernel's shared memory size
     cfg.gridDim = dim3((unsigned)(p.chains * p.nseg));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = (size_t)k.smem;
