@@ -26,6 +26,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "rlm_device.cuh"
 #include "rlm_internal.h"
@@ -36,7 +37,10 @@ namespace {
 
 constexpr int kBlock = RLM_ADAMW_BLOCK;         // values that share a scale
 constexpr int kThreads = 256;
-constexpr int kChunk = 2048;                    // values of a block: 8 a thread
+// Values of a thread block: 8 a thread.  Several rounds a thread, the next round's loads issued
+// before this one's arithmetic, measured slower: 292 against 217 us for the 8-bit step at
+// 120 M values (four rounds), 491 against 478 us for the fp32 one.
+constexpr int kChunk = 8 * kThreads;
 constexpr int kMaxTensors = 400;
 
 struct Entry {
@@ -54,94 +58,98 @@ struct StepArgs {
 };
 static_assert(sizeof(StepArgs) <= 32764, "kernel parameter space");
 
+// Eight values as they lie in memory, so that a load can be issued long before its use.
 template <typename T>
-struct Eight;
-template <>
-struct Eight<float> {
-    static __device__ __forceinline__ void load(const float *p, float (&v)[8]) {
-        const float4 a = __ldcs(reinterpret_cast<const float4 *>(p)), b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+struct Eight {
+    static constexpr int kWords = 2 * (int)sizeof(T);
+    uint32_t w[kWords];
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
     }
-    static __device__ __forceinline__ void store(float *p, const float (&v)[8]) {
-        __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
-        __stcs(reinterpret_cast<float4 *>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
-    }
-};
-template <>
-struct Eight<__nv_bfloat16> {
-    static __device__ __forceinline__ void load(const __nv_bfloat16 *p, float (&v)[8]) {
-        const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p));
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+    __device__ __forceinline__ void set(const float (&v)[8]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < kWords; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                w[i] = __float_as_uint(v[i]);
+            } else {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t *>(&b);
+            }
         }
     }
-    static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float (&v)[8]) {
-        uint32_t w[4];
+};
+// Eight codes, as values of their block's scale.
+struct Codes {
+    static constexpr int kWords = 2;
+    uint32_t w[2];
+    __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t *>(&b);
+            const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> 16 * (i & 1)), __NV_E4M3);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
         }
-        __stcs(reinterpret_cast<uint4 *>(p), make_uint4(w[0], w[1], w[2], w[3]));
+    }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+        w[0] = w[1] = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v[2 * i], v[2 * i + 1]), __NV_SATFINITE, __NV_E4M3)
+                         << 16 * (i & 1);
     }
 };
-
-// The first `n` (at most 8) values at p; vec: 8 values by 16-byte accesses.
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, int n, bool vec, float (&v)[8]) {
-    if (vec) {
-        Eight<T>::load(p, v);
+// The first n (at most 8) values at p, the others zero: 16-byte (codes: 8-byte) accesses where
+// all eight are there and p allows it, else value by value.  E: bytes of a value.
+template <typename V, int E>
+__device__ __forceinline__ V load8(const void *p, int n) {
+    V v;
+    constexpr int kBytes = 4 * V::kWords, kWide = kBytes < 16 ? kBytes : 16;
+    if (n == 8 && (reinterpret_cast<uintptr_t>(p) & (kWide - 1)) == 0) {
+#pragma unroll
+        for (int i = 0; i < kBytes / kWide; ++i) {
+            if constexpr (kWide == 16) {
+                const uint4 q = __ldcs(static_cast<const uint4 *>(p) + i);
+                v.w[4 * i] = q.x, v.w[4 * i + 1] = q.y, v.w[4 * i + 2] = q.z, v.w[4 * i + 3] = q.w;
+            } else {
+                const uint2 q = __ldcs(static_cast<const uint2 *>(p));
+                v.w[0] = q.x, v.w[1] = q.y;
+            }
+        }
+        return v;
+    }
+#pragma unroll
+    for (int i = 0; i < V::kWords; ++i) v.w[i] = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i >= n) break;
+        if constexpr (E == 4) v.w[i] = static_cast<const uint32_t *>(p)[i];
+        if constexpr (E == 2) v.w[i >> 1] |= (uint32_t) static_cast<const uint16_t *>(p)[i] << 16 * (i & 1);
+        if constexpr (E == 1) v.w[i >> 2] |= (uint32_t) static_cast<const uint8_t *>(p)[i] << 8 * (i & 3);
+    }
+    return v;
+}
+template <typename V, int E>
+__device__ __forceinline__ void store8(void *p, int n, const V &v) {
+    constexpr int kBytes = 4 * V::kWords, kWide = kBytes < 16 ? kBytes : 16;
+    if (n == 8 && (reinterpret_cast<uintptr_t>(p) & (kWide - 1)) == 0) {
+#pragma unroll
+        for (int i = 0; i < kBytes / kWide; ++i) {
+            if constexpr (kWide == 16)
+                __stcs(static_cast<uint4 *>(p) + i, make_uint4(v.w[4 * i], v.w[4 * i + 1], v.w[4 * i + 2], v.w[4 * i + 3]));
+            else
+                __stcs(static_cast<uint2 *>(p), make_uint2(v.w[0], v.w[1]));
+        }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? ld_elem(p + i) : 0.f;
-}
-template <typename T>
-__device__ __forceinline__ void store8(T *p, int n, bool vec, const float (&v)[8]) {
-    if (vec) {
-        Eight<T>::store(p, v);
-        return;
+    for (int i = 0; i < 8; ++i) {
+        if (i >= n) break;
+        if constexpr (E == 4) static_cast<uint32_t *>(p)[i] = v.w[i];
+        if constexpr (E == 2) static_cast<uint16_t *>(p)[i] = (uint16_t)(v.w[i >> 1] >> 16 * (i & 1));
+        if constexpr (E == 1) static_cast<uint8_t *>(p)[i] = (uint8_t)(v.w[i >> 2] >> 8 * (i & 3));
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n) st_elem(p + i, v[i]);
-}
-
-// 8 codes, as values of their block's scale.
-__device__ __forceinline__ void load_codes(const uint8_t *p, int n, bool vec, float (&v)[8]) {
-    uint32_t w[2] = {0u, 0u};
-    if (vec) {
-        const uint2 a = __ldcs(reinterpret_cast<const uint2 *>(p));
-        w[0] = a.x, w[1] = a.y;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) w[i >> 2] |= (uint32_t)p[i] << 8 * (i & 3);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> 16 * (i & 1)), __NV_E4M3);
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
-    }
-}
-__device__ __forceinline__ void store_codes(uint8_t *p, int n, bool vec, const float (&v)[8]) {
-    uint32_t w[2] = {0u, 0u};
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        w[i >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v[2 * i], v[2 * i + 1]), __NV_SATFINITE, __NV_E4M3)
-                     << 16 * (i & 1);
-    if (vec) {
-        __stcs(reinterpret_cast<uint2 *>(p), make_uint2(w[0], w[1]));
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n) p[i] = (uint8_t)(w[i >> 2] >> 8 * (i & 3));
 }
 
 // The bits of the largest magnitude among the warp's values.
@@ -164,8 +172,22 @@ __device__ __forceinline__ void unpair(f32x2 p, float *v) {
     v[1] = f.y;
 }
 
+// What a thread reads of 8 values.
 template <typename P, typename G, bool kMaster, bool k8Bit>
-__global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ StepArgs a) {
+struct Reads {
+    using W = typename std::conditional<kMaster, Eight<float>, Eight<P>>::type;
+    using M = typename std::conditional<k8Bit, Codes, Eight<float>>::type;
+    Eight<G> g;
+    W w;
+    M m, v;
+    float ms, vs;
+};
+
+// The 8-bit step has more arithmetic to hide its loads behind, so its registers are held down
+// for more warps: 304 -> 274 us (fp32 weights) and 331 -> 308 us (masters) at 120 M values; the
+// 32-bit step loses by it.
+template <typename P, typename G, bool kMaster, bool k8Bit>
+__global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_adamw(const __grid_constant__ StepArgs a) {
     // The tensor whose chunks this block's index falls into.
     int lo = 0, hi = a.count - 1;
     while (lo < hi) {
@@ -174,42 +196,44 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Step
     }
     const Entry &e = a.t[lo];
     const int64_t at = (int64_t)(blockIdx.x - a.first[lo]) * kChunk + threadIdx.x * 8;
-    const int n = (int)min((int64_t)8, max((int64_t)0, e.n - at));
     float scale = 1.f;
     if (a.grad_scale) {
         scale = __ldg(a.grad_scale);
         if (!isfinite(scale)) return;           // an overflowed step: nothing changes
     }
-    P *p = static_cast<P *>(e.p) + at;
-    const G *g = static_cast<const G *>(e.g) + at;
-    const bool whole = n == 8;
-    auto wide = [&](const void *q, unsigned to) { return whole && (reinterpret_cast<uintptr_t>(q) & (to - 1)) == 0; };
-    float gv[8], m[8], v[8], w[8];
-    load8(g, n, wide(g, 16), gv);
-    float *master = kMaster ? e.master + at : nullptr;
-    if constexpr (kMaster) load8(master, n, wide(master, 16), w); else load8(p, n, wide(p, 16), w);
-    uint8_t *m8 = static_cast<uint8_t *>(e.m) + at, *v8 = static_cast<uint8_t *>(e.v) + at;
-    float *mf = static_cast<float *>(e.m) + at, *vf = static_cast<float *>(e.v) + at;
+    constexpr int kMoment = k8Bit ? 1 : 4;
+    using R = Reads<P, G, kMaster, k8Bit>;
+    auto bytes = [](void *p, int64_t at, int size) { return static_cast<char *>(p) + at * size; };
+    const int n = (int)min((int64_t)8, max((int64_t)0, e.n - at));
+    R cur;
+    cur.g = load8<Eight<G>, sizeof(G)>(bytes(e.g, at, sizeof(G)), n);
+    if constexpr (kMaster) cur.w = load8<typename R::W, 4>(e.master + at, n);
+    else cur.w = load8<typename R::W, sizeof(P)>(bytes(e.p, at, sizeof(P)), n);
+    cur.m = load8<typename R::M, kMoment>(bytes(e.m, at, kMoment), n);
+    cur.v = load8<typename R::M, kMoment>(bytes(e.v, at, kMoment), n);
     if constexpr (k8Bit) {
-        const int64_t blk = at / kBlock;
-        const float ms = n > 0 ? e.m_scale[blk] : 0.f, vs = n > 0 ? e.v_scale[blk] : 0.f;
-        load_codes(m8, n, wide(m8, 8), m);
-        load_codes(v8, n, wide(v8, 8), v);
+        cur.ms = n > 0 ? e.m_scale[at / kBlock] : 0.f;
+        cur.vs = n > 0 ? e.v_scale[at / kBlock] : 0.f;
+    }
+    const f32x2 b1 = twice(a.beta1), c1 = twice(a.one_minus_beta1), b2 = twice(a.beta2), c2 = twice(a.one_minus_beta2);
+    float m[8], v[8], w[8], root[8];
+    if constexpr (k8Bit) {
+        cur.m.get(m);
+        cur.v.get(v);
+        const f32x2 ms = twice(cur.ms), vs = twice(cur.vs);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            m[i] *= ms;
-            const float r = v[i] * vs;
-            v[i] = __fmul_rn(r, r);
+        for (int i = 0; i < 8; i += 2) {
+            const f32x2 r = mul2(pair(v + i), vs);
+            unpair(mul2(pair(m + i), ms), m + i);
+            unpair(mul2(r, r), v + i);
         }
     } else {
-        load8(mf, n, wide(mf, 16), m);
-        load8(vf, n, wide(vf, 16), v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[i] = cur.m[i], v[i] = cur.v[i];
     }
-    float root[8];
-    const f32x2 b1 = twice(a.beta1), c1 = twice(a.one_minus_beta1), b2 = twice(a.beta2), c2 = twice(a.one_minus_beta2);
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-        f32x2 gs = pair(gv + i);
+        f32x2 gs = pack(make_float2(cur.g[i], cur.g[i + 1]));
         if (a.grad_scale) gs = mul2(gs, twice(scale));
         const f32x2 m2 = add2(mul2(b1, pair(m + i)), mul2(c1, gs));
         const f32x2 v2 = add2(mul2(b2, pair(v + i)), mul2(c2, mul2(gs, gs)));
@@ -221,28 +245,41 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Step
         unpair(fma2(pair(root + i), twice(a.inv_sqrt_bc2), twice(a.eps)), r);
         asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r[0]));
         asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r[1]));
-        unpair(fma2(twice(-a.step_size), mul2(m2, pair(r)), mul2(pair(w + i), twice(a.decay))), w + i);
+        const f32x2 old = pack(make_float2(cur.w[i], cur.w[i + 1]));
+        unpair(fma2(twice(-a.step_size), mul2(m2, pair(r)), mul2(old, twice(a.decay))), w + i);
     }
-    store8(p, n, wide(p, 16), w);
-    if constexpr (kMaster) store8(master, n, wide(master, 16), w);
+    Eight<P> p;
+    p.set(w);
+    store8<Eight<P>, sizeof(P)>(bytes(e.p, at, sizeof(P)), n, p);
+    if constexpr (kMaster) {
+        Eight<float> q;
+        q.set(w);
+        store8<Eight<float>, 4>(e.master + at, n, q);
+    }
+    typename R::M mo, vo;
     if constexpr (k8Bit) {
         const int em = exponent(block_top(m)), ev = exponent(__float_as_uint(__fsqrt_rn(__uint_as_float(block_top(v)))));
-        const float im = power_of_two(8 - em), iv = power_of_two(8 - ev);
+        const f32x2 im = twice(power_of_two(8 - em)), iv = twice(power_of_two(8 - ev));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            m[i] *= im;
-            root[i] = root[i] > 0.f ? fmaxf(root[i] * iv, 0x1p-9f) : root[i] * iv;
+        for (int i = 0; i < 8; i += 2) {
+            float c[2];
+            unpair(mul2(pair(m + i), im), m + i);
+            unpair(mul2(pair(root + i), iv), c);
+            root[i] = root[i] > 0.f ? fmaxf(c[0], 0x1p-9f) : c[0];
+            root[i + 1] = root[i + 1] > 0.f ? fmaxf(c[1], 0x1p-9f) : c[1];
         }
-        store_codes(m8, n, wide(m8, 8), m);
-        store_codes(v8, n, wide(v8, 8), root);
+        mo.set(m);
+        vo.set(root);
         if ((threadIdx.x & 31) == 0 && n > 0) {
             e.m_scale[at / kBlock] = power_of_two(em - 8);
             e.v_scale[at / kBlock] = power_of_two(ev - 8);
         }
     } else {
-        store8(mf, n, wide(mf, 16), m);
-        store8(vf, n, wide(vf, 16), v);
+        mo.set(m);
+        vo.set(v);
     }
+    store8<typename R::M, kMoment>(bytes(e.m, at, kMoment), n, mo);
+    store8<typename R::M, kMoment>(bytes(e.v, at, kMoment), n, vo);
 }
 
 using StepKernel = void (*)(const StepArgs);

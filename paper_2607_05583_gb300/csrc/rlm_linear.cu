@@ -8,8 +8,8 @@
 // (MN-major): x w^T is K, K; dz w is K, MN; dz^T x is MN, MN.  TMA brings either form into
 // 128-byte swizzled shared memory and tcgen05.mma reads either, so nothing is transposed.
 //
-// k_gemm.  Persistent, one CTA per SM, 128 x kBN tiles (kBN = 256 or 128), contraction
-// steps of 64.  Warp 8 feeds a ring of operand stages, one thread of warp 9 issues the
+// k_gemm.  Persistent, one CTA per SM, contraction steps of 64; tiles of 256 x 256 or 256 x 128
+// by pairs of CTAs (cta_group::2), or 128 x 128 by single ones where pairs would be few.  Warp 8 feeds a ring of operand stages, one thread of warp 9 issues the
 // MMAs into one of two TMEM accumulators, warps 0-7 empty the other: warp w owns TMEM
 // lanes 32 (w mod 4) .. + 31 and half w / 4 of the columns, 64 bytes of output at a time,
 // from registers through its own 2 KB staging buffers (two, 64-byte swizzle) to TMA
@@ -72,10 +72,14 @@ constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = (kEpiWarps + 2) * 32;
 constexpr int kStageOut = 2048;                 // one warp's staging buffer: 32 rows of 64 bytes
 
-template <int kBN>
+// kPair: two CTAs share a 256-row tile (cta_group::2): each holds its 128 rows of A and half of
+// B's rows, so B is loaded once and read once for both.
+template <bool kPair, int kBN>
 struct GemmCfg {
-    static constexpr int kA = kBM * kBK * 2, kB = kBN * kBK * 2, kStage = kA + kB;
-    static constexpr int kStages = kBN == 256 ? 4 : 6;
+    static constexpr int kRowsB = kPair ? kBN / 2 : kBN;        // rows of B in this CTA's shared memory
+    static constexpr int kTileM = kPair ? 2 * kBM : kBM;
+    static constexpr int kA = kBM * kBK * 2, kB = kRowsB * kBK * 2, kStage = kA + kB;
+    static constexpr int kStages = 196608 / kStage;
     static constexpr int kOffOut = kStages * kStage;
     static constexpr int kOffBar = kOffOut + kEpiWarps * 2 * kStageOut;
     static constexpr int kBars = 2 * kStages + 4;
@@ -124,11 +128,11 @@ __device__ __forceinline__ uint32_t piece(int r, int p) { return r * 64 + ((p ^ 
 
 // kOutF32: the raw sums as fp32 (partial sums, or a gradient kept in fp32); otherwise the
 // epilogue act(sum + bias) + residual as bf16, and, if asked, sum + bias as bf16 (map_pre).
-template <bool kAMn, bool kBMn, int kBN, bool kOutF32, int kAct>
+template <bool kPair, bool kAMn, bool kBMn, int kBN, bool kOutF32, int kAct>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
            const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_pre, const GemmArgs g) {
-    using Cfg = GemmCfg<kBN>;
+    using Cfg = GemmCfg<kPair, kBN>;
     constexpr int ST = Cfg::kStages;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
@@ -138,6 +142,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const uint32_t full = bars, empty = bars + ST * 8, acc_full = bars + 2 * ST * 8, acc_empty = acc_full + 16;
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + Cfg::kOffMisc);
     uint32_t *tmem_at = reinterpret_cast<uint32_t *>(smem + Cfg::kOffMisc + 8);
+    // A pair: rank 0 issues the MMAs and holds the barriers that count both CTAs' copies (full)
+    // and both CTAs' readers (acc_empty); empty and acc_full are signalled in both.
+    const int rank = kPair ? (int)(blockIdx.x & 1) : 0;
+    const int unit0 = kPair ? blockIdx.x >> 1 : blockIdx.x, unit_step = kPair ? gridDim.x >> 1 : gridDim.x;
 
     if (tid == 0) {
         for (int i = 0; i < ST; ++i) {
@@ -146,16 +154,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(acc_full + i * 8, 1);
-            bar_init(acc_empty + i * 8, kEpiWarps);
+            bar_init(acc_empty + i * 8, (kPair ? 2 : 1) * kEpiWarps);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kEpiWarps) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_at)),
-                     "n"(2 * kBN)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        tmem_alloc<kPair>(smem_u32(tmem_at), 2 * kBN);
         if (lane == 0) {
             prefetch_map(&map_a);
             prefetch_map(&map_b);
@@ -164,6 +169,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     }
     fence_before();
     __syncthreads();
+    if (kPair) cluster_sync();
     fence_after();
     const uint32_t tmem = *tmem_at;
     const int units = g.tiles_m * g.tiles_n * g.splits;
@@ -172,42 +178,47 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         if (lane == 0) {
             int it = 0;
             bool ok = true;
-            for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+            for (int u = unit0; ok && u < units; u += unit_step) {
                 const int split = u % g.splits;
                 int tm, tn;
                 tile_of(u / g.splits, g, tm, tn);
                 const int s0 = split * g.steps_per_split, s1 = min(g.steps, s0 + g.steps_per_split);
+                const int ra = tm * Cfg::kTileM + rank * kBM, rb = tn * kBN + rank * Cfg::kRowsB;
                 for (int s = s0; s < s1; ++s, ++it) {
                     const int st = it % ST;
                     if (it >= ST && !(ok = wait_bar(empty + st * 8, (it / ST - 1) & 1, abort_flag, &g_linear_status))) break;
-                    const uint32_t a = base + st * Cfg::kStage, b = a + Cfg::kA, bar = full + st * 8;
-                    bar_expect_tx(bar, Cfg::kStage);
+                    const uint32_t a = base + st * Cfg::kStage, b = a + Cfg::kA;
+                    if (rank == 0) bar_expect_tx(full + st * 8, (kPair ? 2 : 1) * Cfg::kStage);
+                    const uint32_t bar = kPair ? map_rank(full + st * 8, 0) : full + st * 8;
+                    auto load = [&](uint32_t to, const CUtensorMap *map, int c0, int c1) {
+                        if constexpr (kPair) tma_load_2d_pair(to, map, c0, c1, bar);
+                        else tma_load_2d(to, map, c0, c1, bar);
+                    };
                     if (kAMn) {
 #pragma unroll
-                        for (int j = 0; j < kBM / 64; ++j)
-                            tma_load_2d(a + j * 8192, &map_a, tm * kBM + j * 64, s * kBK, bar);
+                        for (int j = 0; j < kBM / 64; ++j) load(a + j * 8192, &map_a, ra + j * 64, s * kBK);
                     } else {
-                        tma_load_2d(a, &map_a, s * kBK, tm * kBM, bar);
+                        load(a, &map_a, s * kBK, ra);
                     }
                     if (kBMn) {
 #pragma unroll
-                        for (int j = 0; j < kBN / 64; ++j)
-                            tma_load_2d(b + j * 8192, &map_b, tn * kBN + j * 64, s * kBK, bar);
+                        for (int j = 0; j < Cfg::kRowsB / 64; ++j) load(b + j * 8192, &map_b, rb + j * 64, s * kBK);
                     } else {
-                        tma_load_2d(b, &map_b, s * kBK, tn * kBN, bar);
+                        load(b, &map_b, s * kBK, rb);
                     }
                 }
             }
             // Copies in flight land before the CTA may end (after a timeout; otherwise they have).
-            for (int i = max(0, it - ST); i < it; ++i)
-                for (int n = 0; n < 1 << 22 && !bar_try(full + (i % ST) * 8, (i / ST) & 1); ++n) {}
+            if (*abort_flag && rank == 0)
+                for (int i = max(0, it - ST); i < it; ++i)
+                    for (int n = 0; n < 1 << 22 && !bar_try(full + (i % ST) * 8, (i / ST) & 1); ++n) {}
         }
     } else if (warp == kEpiWarps + 1) {
-        if (lane == 0) {
-            constexpr uint32_t id = idesc(kBM, kBN, kAMn, kBMn);
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t id = idesc(Cfg::kTileM, kBN, kAMn, kBMn);
             int it = 0, n = 0;
             bool ok = true;
-            for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++n) {
+            for (int u = unit0; ok && u < units; u += unit_step, ++n) {
                 const int split = u % g.splits;
                 const int s0 = split * g.steps_per_split, s1 = min(g.steps, s0 + g.steps_per_split);
                 const int buf = n & 1;
@@ -223,30 +234,22 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                     for (int k = 0; k < kBK / 16; ++k) {
                         const uint64_t da = kAMn ? desc(a + k * 2048, 8192, 1024) : desc(a + k * 32, 16, 1024);
                         const uint64_t db = kBMn ? desc(b + k * 2048, 8192, 1024) : desc(b + k * 32, 16, 1024);
-                        asm volatile(
-                            "{ .reg .pred p; setp.ne.b32 p, %4, 0;\n"
-                            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
-                            "l"(da), "l"(db), "r"(id), "r"((uint32_t)(s > s0 || k > 0))
-                            : "memory");
+                        mma<kPair>(d, da, db, id, (uint32_t)(s > s0 || k > 0));
                     }
-                    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                                     empty + st * 8)
-                                 : "memory");
+                    commit<kPair>(empty + st * 8);
                 }
-                asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(acc_full +
-                                                                                                                 buf * 8)
-                             : "memory");
+                commit<kPair>(acc_full + buf * 8);
             }
         }
     } else {
         constexpr int kCols = kOutF32 ? 16 : 32;            // output columns of one 64-byte chunk
         const uint32_t out = base + Cfg::kOffOut + warp * 2 * kStageOut;
         int n = 0, slot = 0;
-        for (int u = blockIdx.x; u < units; u += gridDim.x, ++n) {
+        for (int u = unit0; u < units; u += unit_step, ++n) {
             const int split = u % g.splits;
             int tm, tn;
             tile_of(u / g.splits, g, tm, tn);
-            const int row0 = tm * kBM + (warp & 3) * 32, col0 = tn * kBN + (warp >> 2) * (kBN / 2);
+            const int row0 = tm * Cfg::kTileM + rank * kBM + (warp & 3) * 32, col0 = tn * kBN + (warp >> 2) * (kBN / 2);
             const int buf = n & 1;
             if (!wait_bar(acc_full + buf * 8, (n / 2) & 1, abort_flag, &g_linear_status)) break;
             fence_after();
@@ -272,7 +275,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 if (c + kCols >= kBN / 2) {                 // the last read of this accumulator
                     fence_before();
                     __syncwarp();
-                    if (lane == 0) bar_arrive(acc_empty + buf * 8);
+                    if (lane == 0) {
+                        if constexpr (kPair) bar_arrive_cluster(map_rank(acc_empty + buf * 8, 0));
+                        else bar_arrive(acc_empty + buf * 8);
+                    }
                 }
                 if (!live) continue;
                 if constexpr (kOutF32) {
@@ -352,18 +358,18 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 }
             }
         }
-        if (lane == 0) store_wait_all();
+        if (lane == 0) store_wait_read<0>();        // the staging buffers are read; the writes need no waiting
     }
     fence_before();
     __syncthreads();
-    if (warp == kEpiWarps)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(2 * kBN));
+    if (kPair) cluster_sync();                      // neither CTA leaves while the other may still signal it
+    if (warp == kEpiWarps) tmem_free<kPair>(tmem, 2 * kBN);
 }
 
 // ---------------------------------------------------------------- few rows
 // R <= 8 kTok rows (serving): bound by reading w once.  A 128-row tile would do 128 / R
-// times the work on too few CTAs, so here 16 kRows rows of w are a CTA's: w is the 16-row
-// operand of mma.sync (m16n8k16), tokens its 8 columns.  Eight warps share the contraction
+// times the work on too few CTAs, so here 16 rows of w are a CTA's: w is the 16-row
+// operand of mma.sync (m16n8k16), tokens its 8 columns.  The warps share the contraction
 // in 32-long blocks.  The order of the products within a block is free as long as both
 // operands agree, so a lane takes 8 consecutive k of its rows by one 16-byte load from
 // global memory, straight into the fragments: no shared memory, no shuffles.  The warps'
@@ -387,28 +393,26 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-constexpr int kFewWarps = 16;
-
-template <int kTok, int kRows>
-__global__ void __launch_bounds__(kFewWarps * 32) k_few(const FewArgs a) {
-    __shared__ float part[kFewWarps][16 * kRows][8 * kTok + 1];
+template <int kTok, int kWarps>
+__global__ void __launch_bounds__(kWarps * 32) k_few(const FewArgs a) {
+    __shared__ float part[kWarps][16][8 * kTok + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
-    const int n0 = blockIdx.x * 16 * kRows;
-    const bf16 *wp[2 * kRows], *xp[kTok];
-#pragma unroll
-    for (int i = 0; i < 2 * kRows; ++i) wp[i] = a.w + (int64_t)min(n0 + i * 8 + g, a.N - 1) * a.w_ld + q * 8;
+    const int n0 = blockIdx.x * 16;
+    const bf16 *w0 = a.w + (int64_t)min(n0 + g, a.N - 1) * a.w_ld + q * 8;
+    const bf16 *w8 = a.w + (int64_t)min(n0 + 8 + g, a.N - 1) * a.w_ld + q * 8;
+    const bf16 *xp[kTok];
 #pragma unroll
     for (int i = 0; i < kTok; ++i) xp[i] = a.x + (int64_t)min(i * 8 + g, a.R - 1) * a.x_ld + q * 8;
-    float d[kRows][kTok][4] = {};
-    constexpr int kDeep = kRows + kTok > 4 ? 2 : 4;         // blocks in flight
+    float d[kTok][4] = {};
+    constexpr int kDeep = kTok > 2 ? 2 : 4;         // blocks in flight
     auto blocks = [&](int k, auto whole) {
-        uint4 w[kDeep][2 * kRows], x[kDeep][kTok];
+        uint4 w[kDeep][2], x[kDeep][kTok];
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) {
-            const int at = k + u * kFewWarps * 32;
+            const int at = k + u * kWarps * 32;
             const bool ok = decltype(whole)::value || at + q * 8 < a.K;
-#pragma unroll
-            for (int i = 0; i < 2 * kRows; ++i) w[u][i] = ok ? load_w(wp[i] + at) : make_uint4(0, 0, 0, 0);
+            w[u][0] = ok ? load_w(w0 + at) : make_uint4(0, 0, 0, 0);
+            w[u][1] = ok ? load_w(w8 + at) : make_uint4(0, 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < kTok; ++i)
                 x[u][i] = ok ? __ldg(reinterpret_cast<const uint4 *>(xp[i] + at)) : make_uint4(0, 0, 0, 0);
@@ -416,29 +420,25 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_few(const FewArgs a) {
 #pragma unroll
         for (int u = 0; u < kDeep; ++u)
 #pragma unroll
-            for (int r = 0; r < kRows; ++r)
-#pragma unroll
-                for (int t = 0; t < kTok; ++t) {
-                    mma16816(d[r][t], w[u][2 * r].x, w[u][2 * r + 1].x, w[u][2 * r].y, w[u][2 * r + 1].y, x[u][t].x, x[u][t].y);
-                    mma16816(d[r][t], w[u][2 * r].z, w[u][2 * r + 1].z, w[u][2 * r].w, w[u][2 * r + 1].w, x[u][t].z, x[u][t].w);
-                }
+            for (int t = 0; t < kTok; ++t) {
+                mma16816(d[t], w[u][0].x, w[u][1].x, w[u][0].y, w[u][1].y, x[u][t].x, x[u][t].y);
+                mma16816(d[t], w[u][0].z, w[u][1].z, w[u][0].w, w[u][1].w, x[u][t].z, x[u][t].w);
+            }
     };
     int k = warp * 32;
-    for (; k + (kDeep - 1) * kFewWarps * 32 + 32 <= a.K; k += kDeep * kFewWarps * 32) blocks(k, std::true_type{});
+    for (; k + (kDeep - 1) * kWarps * 32 + 32 <= a.K; k += kDeep * kWarps * 32) blocks(k, std::true_type{});
     if (k < a.K) blocks(k, std::false_type{});
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
+    for (int t = 0; t < kTok; ++t)
 #pragma unroll
-        for (int t = 0; t < kTok; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) part[warp][r * 16 + (i >> 1) * 8 + g][t * 8 + q * 2 + (i & 1)] = d[r][t][i];
+        for (int i = 0; i < 4; ++i) part[warp][(i >> 1) * 8 + g][t * 8 + q * 2 + (i & 1)] = d[t][i];
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * kRows * 8 * kTok; i += kFewWarps * 32) {
-        const int n = i % (16 * kRows), t = i / (16 * kRows), col = n0 + n;
+    for (int i = threadIdx.x; i < 16 * 8 * kTok; i += kWarps * 32) {
+        const int n = i % 16, t = i / 16, col = n0 + n;
         if (t >= a.R || col >= a.N) continue;
         float z = 0.f;
 #pragma unroll
-        for (int w = 0; w < kFewWarps; ++w) z += part[w][n][t];
+        for (int w = 0; w < kWarps; ++w) z += part[w][n][t];
         if (a.bias) z += __ldg(a.bias + col);
         if (a.pre) a.pre[t * a.pre_ld + col] = __float2bfloat16_rn(z);
         z = act_of(a.act, z);
@@ -594,30 +594,38 @@ bool output_map(CUtensorMap *map, void *ptr, bool f32, int64_t cols, int64_t row
 }
 
 struct GemmPlan {
+    bool pair;
     int bn, splits, steps_per_split, steps, tiles_m, tiles_n;
 };
 
-// Tile width and splits: the least of rounds of CTAs times a CTA's steps (with two steps'
-// worth for its start), 128-wide tiles costing 1.2 of their share of a 256-wide one, and
-// splits the bytes of their partial sums (a step of a 256-wide tile moves 48 KB).
+// Tile and splits: the least of rounds of work units times a unit's steps, with its start and
+// its epilogue, and for splits the bytes of their partial sums and a second launch; in
+// microseconds, measured (see kTiles).
+struct TileKind {
+    bool pair;
+    int bn;
+    double step, unit;      // one contraction step; what a unit costs beside its steps
+};
+constexpr TileKind kTiles[] = {{true, 256, 0.30, 0.9}, {true, 128, 0.20, 0.6}, {false, 128, 0.27, 0.6}};
+
 GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K) {
     GemmPlan best = {};
     double best_cost = 0;
     const int sms = sm_count();
-    for (int bn : {256, 128}) {
-        const int64_t tm = (M + kBM - 1) / kBM, tn = (N + bn - 1) / bn;
+    for (const TileKind &t : kTiles) {
+        const int64_t tm = (M + (t.pair ? 255 : 127)) / (t.pair ? 256 : 128), tn = (N + t.bn - 1) / t.bn;
+        const int64_t slots = t.pair ? sms / 2 : sms;
         const int steps = (int)((K + kBK - 1) / kBK);
-        for (int splits = 1; splits <= 16 && splits <= steps; ++splits) {
+        for (int splits = 1; splits <= 32 && splits <= steps; ++splits) {
             const int per = (steps + splits - 1) / splits;
             if ((steps + per - 1) / per != splits) continue;
-            if (splits > 1 && tm * tn * splits > sms) break;        // more work units than SMs: nothing to fill
-            const int64_t rounds = (tm * tn * splits + sms - 1) / sms;
-            const double step = bn == 256 ? 1.0 : 0.6;
-            double cost = (double)rounds * ((per + 2) * step + (bn == 256 ? 3.0 : 1.5));
-            if (splits > 1) cost += 8.0 + 8.0 * (double)splits * M * N / (6.0e12 * 0.3e-6);
+            if (splits > 1 && tm * tn * splits > slots) break;      // more work units than SMs: nothing to fill
+            const int64_t rounds = (tm * tn * splits + slots - 1) / slots;
+            double cost = (double)rounds * (per * t.step + t.unit);
+            if (splits > 1) cost += 3.0 + 8.0 * splits * (double)M * N / 6.0e6;
             if (best_cost == 0 || cost < best_cost) {
                 best_cost = cost;
-                best = {bn, splits, per, steps, (int)tm, (int)tn};
+                best = {t.pair, t.bn, splits, per, steps, (int)tm, (int)tn};
             }
         }
     }
@@ -645,38 +653,57 @@ struct Epilogue {
     int64_t pre_ld = 0;
 };
 
-template <bool kAMn, bool kBMn, int kBN, bool kOutF32, int kAct>
+template <bool kPair, bool kAMn, bool kBMn, int kBN, bool kOutF32, int kAct>
 cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, const CUtensorMap &mp,
                         const GemmArgs &g, cudaStream_t st) {
-    auto *fn = k_gemm<kAMn, kBMn, kBN, kOutF32, kAct>;
-    static std::atomic<unsigned long long> set{0};          // devices that have the kernel's shared memory size
+    using Cfg = GemmCfg<kPair, kBN>;
+    auto *fn = k_gemm<kPair, kAMn, kBMn, kBN, kOutF32, kAct>;
+    static std::atomic<int> ctas[64];               // per device: CTAs that fit, once the kernel is set up
     int dev = 0;
     cudaGetDevice(&dev);
-    const unsigned long long bit = 1ull << (dev & 63);
-    if (!(set.load(std::memory_order_relaxed) & bit)) {
-        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<kBN>::kSmem);
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kGemmThreads);
+    cfg.dynamicSmemBytes = Cfg::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kPair ? 2 : 1;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int room = ctas[dev & 63].load(std::memory_order_relaxed);
+    if (room == 0) {
+        cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
         if (e != cudaSuccess) return e;
-        set.fetch_or(bit, std::memory_order_relaxed);
+        room = sm_count();
+        if (kPair) {
+            // Pairs sit in one GPC: an odd SM of a GPC stays out.
+            int n = 0;
+            cfg.gridDim = dim3(2);
+            if ((e = cudaOccupancyMaxActiveClusters(&n, fn, &cfg)) != cudaSuccess) return e;
+            room = 2 * std::max(n, 1);
+        }
+        ctas[dev & 63].store(room, std::memory_order_relaxed);
     }
-    const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits;
-    fn<<<(unsigned)std::min<int64_t>(units, sm_count()), kGemmThreads, GemmCfg<kBN>::kSmem, st>>>(ma, mb, mc, mp, g);
+    const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits * (kPair ? 2 : 1);
+    cfg.gridDim = dim3((unsigned)std::min<int64_t>(units, room));
     count_launches(1);
-    return cudaGetLastError();
+    return cudaLaunchKernelEx(&cfg, fn, ma, mb, mc, mp, g);
 }
 
-template <bool kAMn, bool kBMn, int kBN>
+template <bool kPair, bool kAMn, bool kBMn, int kBN>
 cudaError_t pick_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, const CUtensorMap &mp,
                       const GemmArgs &g, bool f32, cudaStream_t st) {
-    if (f32) return launch_gemm<kAMn, kBMn, kBN, true, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
+    if (f32) return launch_gemm<kPair, kAMn, kBMn, kBN, true, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
     if constexpr (!kAMn && !kBMn) {         // only the forward product has an activation
         switch (g.act) {
-            case RLM_ACT_SILU: return launch_gemm<kAMn, kBMn, kBN, false, RLM_ACT_SILU>(ma, mb, mc, mp, g, st);
-            case RLM_ACT_GELU: return launch_gemm<kAMn, kBMn, kBN, false, RLM_ACT_GELU>(ma, mb, mc, mp, g, st);
-            case RLM_ACT_SIGMOID: return launch_gemm<kAMn, kBMn, kBN, false, RLM_ACT_SIGMOID>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_SILU: return launch_gemm<kPair, kAMn, kBMn, kBN, false, RLM_ACT_SILU>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_GELU: return launch_gemm<kPair, kAMn, kBMn, kBN, false, RLM_ACT_GELU>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_SIGMOID: return launch_gemm<kPair, kAMn, kBMn, kBN, false, RLM_ACT_SIGMOID>(ma, mb, mc, mp, g, st);
             default: break;
         }
     }
-    return launch_gemm<kAMn, kBMn, kBN, false, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
+    return launch_gemm<kPair, kAMn, kBMn, kBN, false, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
 }
 
 template <bool kAMn, bool kBMn>
@@ -684,7 +711,7 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
     const GemmPlan p = gemm_plan(M, N, K);
     CUtensorMap ma, mb, mc, mp;
     if (!(kAMn ? operand_map(&ma, a.ptr, M, K, a.ld, 64) : operand_map(&ma, a.ptr, K, M, a.ld, kBM)) ||
-        !(kBMn ? operand_map(&mb, b.ptr, N, K, b.ld, 64) : operand_map(&mb, b.ptr, K, N, b.ld, p.bn)))
+        !(kBMn ? operand_map(&mb, b.ptr, N, K, b.ld, 64) : operand_map(&mb, b.ptr, K, N, b.ld, p.pair ? p.bn / 2 : p.bn)))
         return cudaErrorInvalidValue;
     const bool split = p.splits > 1;
     if (!(split ? output_map(&mc, part, true, N, M, N, p.splits)
@@ -704,8 +731,9 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
         g.want_pre = ep.pre != nullptr;
     }
     const bool f32 = split || ep.out_f32;
-    cudaError_t e = p.bn == 256 ? pick_gemm<kAMn, kBMn, 256>(ma, mb, mc, mp, g, f32, st)
-                                : pick_gemm<kAMn, kBMn, 128>(ma, mb, mc, mp, g, f32, st);
+    const cudaError_t e = !p.pair        ? pick_gemm<false, kAMn, kBMn, 128>(ma, mb, mc, mp, g, f32, st)
+                          : p.bn == 256 ? pick_gemm<true, kAMn, kBMn, 256>(ma, mb, mc, mp, g, f32, st)
+                                        : pick_gemm<true, kAMn, kBMn, 128>(ma, mb, mc, mp, g, f32, st);
     if (e != cudaSuccess || !split) return e;
     FinishArgs f = {};
     f.part = part;
@@ -730,15 +758,16 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
 
 // Rows that k_few serves; see the table at linear_forward.
 constexpr int kFewRows = 32;
-constexpr bool kTwo = false;
 
 template <int kTok>
 void launch_few(const FewArgs &a, cudaStream_t st) {
-    // 32 rows of w a CTA where that still gives every SM one.
-    if (kTwo && a.N >= 32 * sm_count() * 3 / 4)
-        k_few<kTok, 2><<<(unsigned)((a.N + 31) / 32), kFewWarps * 32, 0, st>>>(a);
+    // Sixteen warps share the contraction, eight where there are three CTAs and more for each SM:
+    // 8.8 against 11.5 us (K = N = 4096, 8 rows), 21.1 against 18.2 us (K = 4096, N = 11008).
+    const unsigned ctas = (unsigned)((a.N + 15) / 16);
+    if (ctas >= 3u * (unsigned)sm_count())
+        k_few<kTok, 8><<<ctas, 8 * 32, 0, st>>>(a);
     else
-        k_few<kTok, 1><<<(unsigned)((a.N + 15) / 16), kFewWarps * 32, 0, st>>>(a);
+        k_few<kTok, 16><<<ctas, 16 * 32, 0, st>>>(a);
     count_launches(1);
 }
 
