@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
     const uint32_t base = smem_u32(smem);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     const uint32_t bars = base + Cfg::kOffBar;
     const uint32_t full = bars, empty = bars + ST * 8, acc_full = bars + 2 * ST * 8, acc_empty = acc_full + 16;
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + Cfg::kOffMisc);
@@ -175,21 +175,21 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const int units = g.tiles_m * g.tiles_n * g.splits;
 
     if (warp == kEpiWarps) {
-        if (lane == 0) {
-            int it = 0;
-            bool ok = true;
-            for (int u = unit0; ok && u < units; u += unit_step) {
-                const int split = u % g.splits;
-                int tm, tn;
-                tile_of(u / g.splits, g, tm, tn);
-                const int s0 = split * g.steps_per_split, s1 = min(g.steps, s0 + g.steps_per_split);
-                const int ra = tm * Cfg::kTileM + rank * kBM, rb = tn * kBN + rank * Cfg::kRowsB;
-                for (int s = s0; s < s1; ++s, ++it) {
-                    const int st = it % ST;
-                    if (it >= ST && !(ok = wait_bar(empty + st * 8, (it / ST - 1) & 1, abort_flag, &g_linear_status))) break;
-                    const uint32_t a = base + st * Cfg::kStage, b = a + Cfg::kA;
+        int it = 0;
+        bool ok = true;
+        for (int u = unit0; ok && u < units; u += unit_step) {
+            const int split = u % g.splits;
+            int tm, tn;
+            tile_of(u / g.splits, g, tm, tn);
+            const int s0 = split * g.steps_per_split, s1 = min(g.steps, s0 + g.steps_per_split);
+            const int ra = tm * Cfg::kTileM + rank * kBM, rb = tn * kBN + rank * Cfg::kRowsB;
+            for (int s = s0; s < s1; ++s, ++it) {
+                const int st = it % ST;
+                if (it >= ST && !(ok = wait_bar(empty + st * 8, (it / ST - 1) & 1, abort_flag, &g_linear_status))) break;
+                const uint32_t a = base + st * Cfg::kStage, b = a + Cfg::kA;
+                const uint32_t bar = kPair ? map_rank(full + st * 8, 0) : full + st * 8;
+                if (elect()) {
                     if (rank == 0) bar_expect_tx(full + st * 8, (kPair ? 2 : 1) * Cfg::kStage);
-                    const uint32_t bar = kPair ? map_rank(full + st * 8, 0) : full + st * 8;
                     auto load = [&](uint32_t to, const CUtensorMap *map, int c0, int c1) {
                         if constexpr (kPair) tma_load_2d_pair(to, map, c0, c1, bar);
                         else tma_load_2d(to, map, c0, c1, bar);
@@ -207,15 +207,18 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                         load(b, &map_b, s * kBK, rb);
                     }
                 }
+                __syncwarp();
             }
-            // Copies in flight land before the CTA may end (after a timeout; otherwise they have).
-            if (*abort_flag && rank == 0)
-                for (int i = max(0, it - ST); i < it; ++i)
-                    for (int n = 0; n < 1 << 22 && !bar_try(full + (i % ST) * 8, (i / ST) & 1); ++n) {}
         }
+        // Copies in flight land before the CTA may end (after a timeout; otherwise they have).
+        if (*abort_flag && rank == 0)
+            for (int i = max(0, it - ST); i < it; ++i)
+                for (int n = 0; n < 1 << 22 && !bar_try(full + (i % ST) * 8, (i / ST) & 1); ++n) {}
     } else if (warp == kEpiWarps + 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             constexpr uint32_t id = idesc(Cfg::kTileM, kBN, kAMn, kBMn);
+            constexpr uint32_t a_k = (kAMn ? 2048 : 32) >> 4, b_k = (kBMn ? 2048 : 32) >> 4;       // 16 contraction indexes on
+            const uint64_t da0 = desc(base, kAMn ? 8192 : 16, 1024), db0 = desc(base + Cfg::kA, kBMn ? 8192 : 16, 1024);
             int it = 0, n = 0;
             bool ok = true;
             for (int u = unit0; ok && u < units; u += unit_step, ++n) {
@@ -229,16 +232,17 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                     const int st = it % ST;
                     if (!(ok = wait_bar(full + st * 8, (it / ST) & 1, abort_flag, &g_linear_status))) break;
                     fence_after();
-                    const uint32_t a = base + st * Cfg::kStage, b = a + Cfg::kA;
+                    const uint64_t da = da0 + st * (Cfg::kStage >> 4), db = db0 + st * (Cfg::kStage >> 4);
+                    if (elect()) {
 #pragma unroll
-                    for (int k = 0; k < kBK / 16; ++k) {
-                        const uint64_t da = kAMn ? desc(a + k * 2048, 8192, 1024) : desc(a + k * 32, 16, 1024);
-                        const uint64_t db = kBMn ? desc(b + k * 2048, 8192, 1024) : desc(b + k * 32, 16, 1024);
-                        mma<kPair>(d, da, db, id, (uint32_t)(s > s0 || k > 0));
+                        for (int k = 0; k < kBK / 16; ++k)
+                            mma<kPair>(d, da + k * a_k, db + k * b_k, id, (uint32_t)(s > s0 || k > 0));
+                        commit<kPair>(empty + st * 8);
                     }
-                    commit<kPair>(empty + st * 8);
+                    __syncwarp();
                 }
-                commit<kPair>(acc_full + buf * 8);
+                if (elect()) commit<kPair>(acc_full + buf * 8);
+                __syncwarp();
             }
         }
     } else {

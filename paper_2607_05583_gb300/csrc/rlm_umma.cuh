@@ -27,6 +27,14 @@ __device__ __forceinline__ void bar_expect_tx(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
+// True in one lane of a converged warp.  Work for one thread is issued from warp-uniform code
+// under this predicate: operands then stay in uniform registers.
+__device__ __forceinline__ bool elect() {
+    uint32_t p;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(p));
+    return p != 0;
+}
+
 // Bounded wait on a barrier phase (about 2 s).  False once this CTA has given up: the
 // shared flag and the status word are set, and every role leaves its loop.
 __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status) {
