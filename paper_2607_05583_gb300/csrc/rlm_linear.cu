@@ -9,11 +9,12 @@
 // 128-byte swizzled shared memory and tcgen05.mma reads either, so nothing is transposed.
 //
 // k_gemm.  Persistent, one CTA per SM, contraction steps of 64; tiles of 256 x 256 or 256 x 128
-// by pairs of CTAs (cta_group::2), or 128 x 128 by single ones where pairs would be few.  Warp 8 feeds a ring of operand stages, one thread of warp 9 issues the
-// MMAs into one of two TMEM accumulators, warps 0-7 empty the other: warp w owns TMEM
-// lanes 32 (w mod 4) .. + 31 and half w / 4 of the columns, 64 bytes of output at a time,
-// from registers through its own 2 KB staging buffers (two, 64-byte swizzle) to TMA
-// stores, which clip at the matrix's edge.  A product of few tiles is cut along the
+// by pairs of CTAs (cta_group::2), or 128 x 128 by single ones where pairs would be few.  Warp 16 feeds a ring of operand stages, warp 17 issues the
+// MMAs into one of two TMEM accumulators, warps 0-15 empty the other: warp w owns TMEM
+// lanes 32 (w mod 4) .. + 31 and quarter w / 4 of the columns, 64 bytes of output at a time,
+// from registers through its own 4 KB of staging (swizzled) to TMA stores, which clip at the
+// matrix's edge.  Short contractions are bound by this path's latency: sixteen
+// warps where eight would do for long ones.  A product of few tiles is cut along the
 // contraction (splits): partial sums go to the workspace in fp32 and k_finish adds them in
 // order and applies the epilogue.  Accumulation is fp32 throughout; results repeat bit for
 // bit.
@@ -68,9 +69,9 @@ __device__ __forceinline__ float act_grad(int kind, float z) {
 
 // -------------------------------------------------------------------- gemm
 constexpr int kBM = 128, kBK = 64;
-constexpr int kEpiWarps = 8;
+constexpr int kEpiWarps = 16;
 constexpr int kGemmThreads = (kEpiWarps + 2) * 32;
-constexpr int kStageOut = 2048;                 // one warp's staging buffer: 32 rows of 64 bytes
+constexpr int kStageOut = 4096;                 // one epilogue warp's staging: 32 rows of 128 bytes, or two of 64 bytes
 
 // kPair: two CTAs share a 256-row tile (cta_group::2): each holds its 128 rows of A and half of
 // B's rows, so B is loaded once and read once for both.
@@ -79,9 +80,9 @@ struct GemmCfg {
     static constexpr int kRowsB = kPair ? kBN / 2 : kBN;        // rows of B in this CTA's shared memory
     static constexpr int kTileM = kPair ? 2 * kBM : kBM;
     static constexpr int kA = kBM * kBK * 2, kB = kRowsB * kBK * 2, kStage = kA + kB;
-    static constexpr int kStages = 196608 / kStage;
+    static constexpr int kStages = (229376 - kEpiWarps * kStageOut) / kStage;
     static constexpr int kOffOut = kStages * kStage;
-    static constexpr int kOffBar = kOffOut + kEpiWarps * 2 * kStageOut;
+    static constexpr int kOffBar = kOffOut + kEpiWarps * kStageOut;
     static constexpr int kBars = 2 * kStages + 4;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
     static constexpr int kSmem = kOffMisc + 16 + 1024;          // and room to align the ring
@@ -95,7 +96,6 @@ struct GemmArgs {
     const bf16 *residual;       // nullable [M][ld]
     int64_t residual_ld;
     int act;
-    int want_pre;
 };
 
 // Order of the tiles: columns of kGroup row tiles, so that the CTAs at work share operands in L2.
@@ -123,12 +123,23 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
 }
-// Byte offset of 16-byte piece p of row r in a staging buffer (64-byte TMA swizzle).
-__device__ __forceinline__ uint32_t piece(int r, int p) { return r * 64 + ((p ^ ((r >> 1) & 3)) << 4); }
+// Byte offset of 16-byte piece p of row r in a staging buffer, rows of kBytes (64- or
+// 128-byte TMA swizzle).
+template <int kBytes>
+__device__ __forceinline__ uint32_t piece(int r, int p) {
+    return kBytes == 128 ? r * 128 + ((p ^ (r & 7)) << 4) : r * 64 + ((p ^ ((r >> 1) & 3)) << 4);
+}
 
-// kOutF32: the raw sums as fp32 (partial sums, or a gradient kept in fp32); otherwise the
-// epilogue act(sum + bias) + residual as bf16, and, if asked, sum + bias as bf16 (map_pre).
-template <bool kPair, bool kAMn, bool kBMn, int kBN, bool kOutF32, int kAct>
+// What a product writes: the epilogue act(sum + bias) + residual as bf16; the raw sums as fp32
+// (partial sums, or a gradient kept in fp32); or the epilogue and sum + bias, both bf16.
+enum : int { kOutBf16 = 0, kOutF32 = 1, kOutPre = 2 };
+// Bytes of a row of one store: TMA moves a row a request, so 128 where a warp's columns allow
+// (with 64-byte rows 131072 x 256 x 512 took 55 us) and the staging need not hold two boxes.
+constexpr int store_bytes(int out, int bn) {
+    return out == kOutF32 ? 128 : out == kOutBf16 && bn == 256 ? 128 : 64;
+}
+
+template <bool kPair, bool kAMn, bool kBMn, int kBN, int kOut, int kAct>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
            const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_pre, const GemmArgs g) {
@@ -246,37 +257,67 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             }
         }
     } else {
-        constexpr int kCols = kOutF32 ? 16 : 32;            // output columns of one 64-byte chunk
-        const uint32_t out = base + Cfg::kOffOut + warp * 2 * kStageOut;
+        constexpr bool kF32 = kOut == kOutF32;
+        constexpr int kBytes = store_bytes(kOut, kBN), kSlots = kBytes == 128 ? 1 : 2;
+        constexpr int kCols = kF32 ? 16 : 32;               // output columns handled at a time, 64 bytes
+        constexpr int kWarpCols = kBN / (kEpiWarps / 4);    // a warp's columns of a tile
+        const uint32_t out = base + Cfg::kOffOut + warp * kStageOut;
         int n = 0, slot = 0;
+        // The next staging buffer, once the store that used it last has read it.
+        auto buffer = [&]() {
+            if (lane == 0) store_wait_read<kSlots - 1>();
+            __syncwarp();
+            const uint32_t to = out + slot * (kStageOut / kSlots);
+            slot = slot + 1 == kSlots ? 0 : slot + 1;
+            return to;
+        };
+        auto send = [&](const CUtensorMap *map, uint32_t from, int col, int row, int plane) {
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                tma_store_3d(map, from, col, row, plane);
+                store_commit();
+            }
+        };
+        auto stage = [&](uint32_t to, int half, const float (&z)[32]) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+                st_shared16(to + piece<kBytes>(lane, 4 * half + p),
+                            make_uint4(pack2(z[8 * p], z[8 * p + 1]), pack2(z[8 * p + 2], z[8 * p + 3]),
+                                       pack2(z[8 * p + 4], z[8 * p + 5]), pack2(z[8 * p + 6], z[8 * p + 7])));
+        };
         for (int u = unit0; u < units; u += unit_step, ++n) {
             const int split = u % g.splits;
             int tm, tn;
             tile_of(u / g.splits, g, tm, tn);
-            const int row0 = tm * Cfg::kTileM + rank * kBM + (warp & 3) * 32, col0 = tn * kBN + (warp >> 2) * (kBN / 2);
+            const int row0 = tm * Cfg::kTileM + rank * kBM + (warp & 3) * 32, col0 = tn * kBN + (warp >> 2) * kWarpCols;
             const int buf = n & 1;
+            // The residual's chunk, eight rows of 64 bytes a request; handed to the rows' lanes through
+            // the staging buffer.  Asked for ahead of the accumulator.
+            uint4 res[4];
+            auto ask = [&](int col) {
+                if (kF32 || !g.residual) return;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = row0 + i * 8 + (lane >> 2), cc = col + (lane & 3) * 8;
+                    res[i] = r < g.M && cc < g.N
+                                 ? __ldg(reinterpret_cast<const uint4 *>(g.residual + (int64_t)r * g.residual_ld + cc))
+                                 : make_uint4(0, 0, 0, 0);
+                }
+            };
+            ask(col0);
             if (!wait_bar(acc_full + buf * 8, (n / 2) & 1, abort_flag, &g_linear_status)) break;
             fence_after();
-            const uint32_t acc = tmem + buf * kBN + (warp >> 2) * (kBN / 2) + ((uint32_t)(warp & 3) << 21);
-            for (int c = 0; c < kBN / 2; c += kCols) {
-                const int col = col0 + c;
-                const bool live = row0 < g.M && col < g.N;
-                uint32_t v[32];
-                uint4 res[4];
-                if (!kOutF32 && g.residual && live) {
-                    // Eight rows of 64 bytes a request; handed to the rows' lanes through the staging buffer.
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = row0 + i * 8 + (lane >> 2), cc = col + (lane & 3) * 8;
-                        res[i] = r < g.M && cc < g.N
-                                     ? __ldg(reinterpret_cast<const uint4 *>(g.residual + (int64_t)r * g.residual_ld + cc))
-                                     : make_uint4(0, 0, 0, 0);
-                    }
-                }
+            const uint32_t acc = tmem + buf * kBN + (warp >> 2) * kWarpCols + ((uint32_t)(warp & 3) << 21);
+            uint32_t to = 0;
+#pragma unroll 1
+            for (int c = 0; c < kWarpCols; c += kCols) {
+                const int col = col0 + c, half = kBytes == 128 ? (c / kCols) & 1 : 0;
+                uint32_t v[kCols];
                 tmem_ld16(acc + c, v);
-                if (!kOutF32) tmem_ld16(acc + c + 16, v + 16);
+                if constexpr (!kF32) tmem_ld16(acc + c + 16, v + 16);
                 tmem_wait_ld();
-                if (c + kCols >= kBN / 2) {                 // the last read of this accumulator
+                if (c + kCols >= kWarpCols) {               // the last read of this accumulator
                     fence_before();
                     __syncwarp();
                     if (lane == 0) {
@@ -284,81 +325,54 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                         else bar_arrive(acc_empty + buf * 8);
                     }
                 }
-                if (!live) continue;
-                if constexpr (kOutF32) {
-                    if (lane == 0) store_wait_read<1>();
-                    __syncwarp();
-                    const uint32_t to = out + slot * kStageOut;
+                // A box that starts past the edge is left out; a half past it is clipped.
+                if (row0 >= g.M || col - half * kCols >= g.N) continue;
+                if constexpr (kF32) {
+                    if (half == 0) to = buffer();
 #pragma unroll
                     for (int p = 0; p < 4; ++p)
-                        st_shared16(to + piece(lane, p), make_uint4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]));
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        tma_store_3d(&map_c, to, col, row0, split);
-                        store_commit();
-                    }
-                    slot ^= 1;
+                        st_shared16(to + piece<kBytes>(lane, 4 * half + p),
+                                    make_uint4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]));
+                    if (half == 1) send(&map_c, to, col - kCols, row0, split);
                 } else {
-                float z[32];
+                    float z[32];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(v[i]);
-                if (g.bias) {
+                    for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(v[i]);
+                    if (g.bias) {
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        if (col + q * 4 < g.N) {
-                            const float4 b = __ldg(reinterpret_cast<const float4 *>(g.bias + col + q * 4));
-                            z[4 * q] += b.x;
-                            z[4 * q + 1] += b.y;
-                            z[4 * q + 2] += b.z;
-                            z[4 * q + 3] += b.w;
+                        for (int q = 0; q < 8; ++q) {
+                            if (col + q * 4 < g.N) {
+                                const float4 b = __ldg(reinterpret_cast<const float4 *>(g.bias + col + q * 4));
+                                z[4 * q] += b.x;
+                                z[4 * q + 1] += b.y;
+                                z[4 * q + 2] += b.z;
+                                z[4 * q + 3] += b.w;
+                            }
                         }
                     }
-                }
-                if (g.want_pre) {
-                    if (lane == 0) store_wait_read<1>();
-                    __syncwarp();
-                    const uint32_t to = out + slot * kStageOut;
-#pragma unroll
-                    for (int p = 0; p < 4; ++p)
-                        st_shared16(to + piece(lane, p), make_uint4(pack2(z[8 * p], z[8 * p + 1]), pack2(z[8 * p + 2], z[8 * p + 3]),
-                                                                    pack2(z[8 * p + 4], z[8 * p + 5]), pack2(z[8 * p + 6], z[8 * p + 7])));
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        tma_store_3d(&map_pre, to, col, row0, 0);
-                        store_commit();
+                    if constexpr (kOut == kOutPre) {
+                        to = buffer();
+                        stage(to, 0, z);
+                        send(&map_pre, to, col, row0, 0);
                     }
-                    slot ^= 1;
-                }
 #pragma unroll
-                for (int i = 0; i < 32; ++i) z[i] = act<kAct>(z[i]);
-                if (lane == 0) store_wait_read<1>();
-                __syncwarp();
-                const uint32_t to = out + slot * kStageOut;
-                if (g.residual) {
+                    for (int i = 0; i < 32; ++i) z[i] = act<kAct>(z[i]);
+                    if (half == 0) to = buffer();
+                    if (g.residual) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) st_shared16(to + piece(i * 8 + (lane >> 2), lane & 3), res[i]);
-                    __syncwarp();
+                        for (int i = 0; i < 4; ++i) st_shared16(to + piece<kBytes>(i * 8 + (lane >> 2), 4 * half + (lane & 3)), res[i]);
+                        __syncwarp();
+                        if (c + kCols < kWarpCols) ask(col + kCols);
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        const uint4 r = ld_shared16(to + piece(lane, p));
-                        z[8 * p] += lo16(r.x), z[8 * p + 1] += hi16(r.x), z[8 * p + 2] += lo16(r.y), z[8 * p + 3] += hi16(r.y);
-                        z[8 * p + 4] += lo16(r.z), z[8 * p + 5] += hi16(r.z), z[8 * p + 6] += lo16(r.w), z[8 * p + 7] += hi16(r.w);
+                        for (int p = 0; p < 4; ++p) {
+                            const uint4 r = ld_shared16(to + piece<kBytes>(lane, 4 * half + p));
+                            z[8 * p] += lo16(r.x), z[8 * p + 1] += hi16(r.x), z[8 * p + 2] += lo16(r.y), z[8 * p + 3] += hi16(r.y);
+                            z[8 * p + 4] += lo16(r.z), z[8 * p + 5] += hi16(r.z), z[8 * p + 6] += lo16(r.w), z[8 * p + 7] += hi16(r.w);
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
-                }
-#pragma unroll
-                for (int p = 0; p < 4; ++p)
-                    st_shared16(to + piece(lane, p), make_uint4(pack2(z[8 * p], z[8 * p + 1]), pack2(z[8 * p + 2], z[8 * p + 3]),
-                                                                pack2(z[8 * p + 4], z[8 * p + 5]), pack2(z[8 * p + 6], z[8 * p + 7])));
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    tma_store_3d(&map_c, to, col, row0, 0);
-                    store_commit();
-                }
-                slot ^= 1;
+                    stage(to, half, z);
+                    if (kBytes == 64 || half == 1) send(&map_c, to, col - half * kCols, row0, 0);
                 }
             }
         }
@@ -583,17 +597,18 @@ bool operand_map(CUtensorMap *map, const void *ptr, int64_t inner, int64_t outer
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// An output [planes][rows][cols]: boxes of 64 bytes by 32 rows.
-bool output_map(CUtensorMap *map, void *ptr, bool f32, int64_t cols, int64_t rows, int64_t ld, int planes) {
+// An output [planes][rows][cols]: boxes of `bytes` (64 or 128) by 32 rows.
+bool output_map(CUtensorMap *map, void *ptr, bool f32, int64_t cols, int64_t rows, int64_t ld, int planes, int bytes) {
     EncodeFn fn = encode_fn();
     if (!fn) return false;
     const int es = f32 ? 4 : 2;
     cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
     cuuint64_t strides[2] = {(cuuint64_t)ld * es, (cuuint64_t)ld * rows * es};
-    cuuint32_t box[3] = {(cuuint32_t)(64 / es), 32, 1};
+    cuuint32_t box[3] = {(cuuint32_t)(bytes / es), 32, 1};
     cuuint32_t one[3] = {1, 1, 1};
     return fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, ptr, dims, strides, box, one,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+              CU_TENSOR_MAP_L2_PROMOTION_NONE,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -657,11 +672,11 @@ struct Epilogue {
     int64_t pre_ld = 0;
 };
 
-template <bool kPair, bool kAMn, bool kBMn, int kBN, bool kOutF32, int kAct>
+template <bool kPair, bool kAMn, bool kBMn, int kBN, int kOut, int kAct>
 cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, const CUtensorMap &mp,
                         const GemmArgs &g, cudaStream_t st) {
     using Cfg = GemmCfg<kPair, kBN>;
-    auto *fn = k_gemm<kPair, kAMn, kBMn, kBN, kOutF32, kAct>;
+    auto *fn = k_gemm<kPair, kAMn, kBMn, kBN, kOut, kAct>;
     static std::atomic<int> ctas[64];               // per device: CTAs that fit, once the kernel is set up
     int dev = 0;
     cudaGetDevice(&dev);
@@ -697,17 +712,23 @@ cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUte
 
 template <bool kPair, bool kAMn, bool kBMn, int kBN>
 cudaError_t pick_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, const CUtensorMap &mp,
-                      const GemmArgs &g, bool f32, cudaStream_t st) {
-    if (f32) return launch_gemm<kPair, kAMn, kBMn, kBN, true, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
-    if constexpr (!kAMn && !kBMn) {         // only the forward product has an activation
-        switch (g.act) {
-            case RLM_ACT_SILU: return launch_gemm<kPair, kAMn, kBMn, kBN, false, RLM_ACT_SILU>(ma, mb, mc, mp, g, st);
-            case RLM_ACT_GELU: return launch_gemm<kPair, kAMn, kBMn, kBN, false, RLM_ACT_GELU>(ma, mb, mc, mp, g, st);
-            case RLM_ACT_SIGMOID: return launch_gemm<kPair, kAMn, kBMn, kBN, false, RLM_ACT_SIGMOID>(ma, mb, mc, mp, g, st);
+                      const GemmArgs &g, int out, cudaStream_t st) {
+    if (out == kOutF32) return launch_gemm<kPair, kAMn, kBMn, kBN, kOutF32, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
+    if constexpr (!kAMn && !kBMn) {         // only the forward product has an activation, or keeps z
+        switch (g.act * 2 + (out == kOutPre)) {
+            case RLM_ACT_NONE * 2 + 1: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_SILU * 2: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_SILU>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_SILU * 2 + 1: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_SILU>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_GELU * 2: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_GELU>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_GELU * 2 + 1: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_GELU>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_SIGMOID * 2:
+                return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_SIGMOID>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_SIGMOID * 2 + 1:
+                return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_SIGMOID>(ma, mb, mc, mp, g, st);
             default: break;
         }
     }
-    return launch_gemm<kPair, kAMn, kBMn, kBN, false, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
+    return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
 }
 
 template <bool kAMn, bool kBMn>
@@ -718,11 +739,12 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
         !(kBMn ? operand_map(&mb, b.ptr, N, K, b.ld, 64) : operand_map(&mb, b.ptr, K, N, b.ld, p.pair ? p.bn / 2 : p.bn)))
         return cudaErrorInvalidValue;
     const bool split = p.splits > 1;
-    if (!(split ? output_map(&mc, part, true, N, M, N, p.splits)
-                : output_map(&mc, ep.out, ep.out_f32, N, M, ep.out_ld, 1)))
+    const int out = split || ep.out_f32 ? kOutF32 : ep.pre ? kOutPre : kOutBf16, bytes = store_bytes(out, p.bn);
+    if (!(split ? output_map(&mc, part, true, N, M, N, p.splits, bytes)
+                : output_map(&mc, ep.out, ep.out_f32, N, M, ep.out_ld, 1, bytes)))
         return cudaErrorInvalidValue;
     mp = mc;
-    if (!split && ep.pre && !output_map(&mp, ep.pre, false, N, M, ep.pre_ld, 1)) return cudaErrorInvalidValue;
+    if (out == kOutPre && !output_map(&mp, ep.pre, false, N, M, ep.pre_ld, 1, bytes)) return cudaErrorInvalidValue;
     GemmArgs g = {};
     g.M = (int)M, g.N = (int)N, g.K = (int)K;
     g.tiles_m = p.tiles_m, g.tiles_n = p.tiles_n;
@@ -732,12 +754,10 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
         g.residual = ep.residual;
         g.residual_ld = ep.residual_ld;
         g.act = ep.act;
-        g.want_pre = ep.pre != nullptr;
     }
-    const bool f32 = split || ep.out_f32;
-    const cudaError_t e = !p.pair        ? pick_gemm<false, kAMn, kBMn, 128>(ma, mb, mc, mp, g, f32, st)
-                          : p.bn == 256 ? pick_gemm<true, kAMn, kBMn, 256>(ma, mb, mc, mp, g, f32, st)
-                                        : pick_gemm<true, kAMn, kBMn, 128>(ma, mb, mc, mp, g, f32, st);
+    const cudaError_t e = !p.pair        ? pick_gemm<false, kAMn, kBMn, 128>(ma, mb, mc, mp, g, out, st)
+                          : p.bn == 256 ? pick_gemm<true, kAMn, kBMn, 256>(ma, mb, mc, mp, g, out, st)
+                                        : pick_gemm<true, kAMn, kBMn, 128>(ma, mb, mc, mp, g, out, st);
     if (e != cudaSuccess || !split) return e;
     FinishArgs f = {};
     f.part = part;
