@@ -12,8 +12,9 @@
 // by pairs of CTAs (cta_group::2), or 128 x 128 by single ones where pairs would be few.  Warp 16 feeds a ring of operand stages, warp 17 issues the
 // MMAs into one of two TMEM accumulators, warps 0-15 empty the other: warp w owns TMEM
 // lanes 32 (w mod 4) .. + 31 and quarter w / 4 of the columns, 64 bytes of output at a time,
-// from registers through its own 4 KB of staging (swizzled) to TMA stores, which clip at the
-// matrix's edge.  Short contractions are bound by this path's latency: sixteen
+// from registers through its own 2 KB of shared memory to 64-byte row pieces.  (TMA
+// stores share the copy engine with the operands, a row a request: 48 against 36 us at
+// 131072 x 256 x 512.)  Short contractions are bound by this path's latency: sixteen
 // warps where eight would do for long ones.  A product of few tiles is cut along the
 // contraction (splits): partial sums go to the workspace in fp32 and k_finish adds them in
 // order and applies the epilogue.  Accumulation is fp32 throughout; results repeat bit for
@@ -59,6 +60,27 @@ __device__ __forceinline__ float act_of(int kind, float z) {
         default: return z;
     }
 }
+// The same on two values.  sigma's exponential and reciprocal are the approximate instructions
+// (2^-22 each); e^-u past fp32's range gives 1 / inf = 0.
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 minus_u_log2e) {
+    float2 e = unpack(minus_u_log2e);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+    e = unpack(add2(pack(e), 0x3f8000003f800000ull));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+    return pack(e);
+}
+__device__ __forceinline__ f32x2 twice(float v) { return pack(make_float2(v, v)); }
+template <int kAct>
+__device__ __forceinline__ f32x2 act2(f32x2 z) {
+    constexpr float l2e = 1.44269504f;
+    if (kAct == RLM_ACT_SILU) return mul2(z, sigmoid2(mul2(z, twice(-l2e))));
+    if (kAct == RLM_ACT_SIGMOID) return sigmoid2(mul2(z, twice(-l2e)));
+    if (kAct == RLM_ACT_GELU)
+        return mul2(z, sigmoid2(mul2(z, fma2(mul2(z, z), twice(-l2e * kBend3), twice(-l2e * kBend1)))));
+    return z;
+}
 // act'(z).  1 - sigma is formed as sigma(-z): the difference would lose it for large z.
 __device__ __forceinline__ float act_grad(int kind, float z) {
     if (kind == RLM_ACT_SIGMOID) return sigmoidf(z) * sigmoidf(-z);
@@ -71,7 +93,7 @@ __device__ __forceinline__ float act_grad(int kind, float z) {
 constexpr int kBM = 128, kBK = 64;
 constexpr int kEpiWarps = 16;
 constexpr int kGemmThreads = (kEpiWarps + 2) * 32;
-constexpr int kStageOut = 4096;                 // one epilogue warp's staging: 32 rows of 128 bytes, or two of 64 bytes
+constexpr int kStageOut = 2048;                 // one epilogue warp's staging: 32 rows of 64 bytes
 
 // kPair: two CTAs share a 256-row tile (cta_group::2): each holds its 128 rows of A and half of
 // B's rows, so B is loaded once and read once for both.
@@ -96,6 +118,9 @@ struct GemmArgs {
     const bf16 *residual;       // nullable [M][ld]
     int64_t residual_ld;
     int act;
+    void *out;                  // bf16, or fp32 [splits][M][ld]
+    bf16 *pre;
+    int64_t out_ld, pre_ld;
 };
 
 // Order of the tiles: columns of kGroup row tiles, so that the CTAs at work share operands in L2.
@@ -123,26 +148,17 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
 }
-// Byte offset of 16-byte piece p of row r in a staging buffer, rows of kBytes (64- or
-// 128-byte TMA swizzle).
-template <int kBytes>
-__device__ __forceinline__ uint32_t piece(int r, int p) {
-    return kBytes == 128 ? r * 128 + ((p ^ (r & 7)) << 4) : r * 64 + ((p ^ ((r >> 1) & 3)) << 4);
-}
+// Byte offset of 16-byte piece p of row r in a staging buffer: neither eight lanes of a row
+// each nor those of two rows meet in a bank.
+__device__ __forceinline__ uint32_t piece(int r, int p) { return r * 64 + ((p ^ ((r >> 1) & 3)) << 4); }
 
 // What a product writes: the epilogue act(sum + bias) + residual as bf16; the raw sums as fp32
 // (partial sums, or a gradient kept in fp32); or the epilogue and sum + bias, both bf16.
 enum : int { kOutBf16 = 0, kOutF32 = 1, kOutPre = 2 };
-// Bytes of a row of one store: TMA moves a row a request, so 128 where a warp's columns allow
-// (with 64-byte rows 131072 x 256 x 512 took 55 us) and the staging need not hold two boxes.
-constexpr int store_bytes(int out, int bn) {
-    return out == kOutF32 ? 128 : out == kOutBf16 && bn == 256 ? 128 : 64;
-}
-
 template <bool kPair, bool kAMn, bool kBMn, int kBN, int kOut, int kAct>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-           const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_pre, const GemmArgs g) {
+           const GemmArgs g) {
     using Cfg = GemmCfg<kPair, kBN>;
     constexpr int ST = Cfg::kStages;
     extern __shared__ unsigned char smem_raw[];
@@ -175,7 +191,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         if (lane == 0) {
             prefetch_map(&map_a);
             prefetch_map(&map_b);
-            prefetch_map(&map_c);
         }
     }
     fence_before();
@@ -258,33 +273,34 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
     } else {
         constexpr bool kF32 = kOut == kOutF32;
-        constexpr int kBytes = store_bytes(kOut, kBN), kSlots = kBytes == 128 ? 1 : 2;
         constexpr int kCols = kF32 ? 16 : 32;               // output columns handled at a time, 64 bytes
         constexpr int kWarpCols = kBN / (kEpiWarps / 4);    // a warp's columns of a tile
-        const uint32_t out = base + Cfg::kOffOut + warp * kStageOut;
-        int n = 0, slot = 0;
-        // The next staging buffer, once the store that used it last has read it.
-        auto buffer = [&]() {
-            if (lane == 0) store_wait_read<kSlots - 1>();
+        const uint32_t staging = base + Cfg::kOffOut + warp * kStageOut;
+        int n = 0;
+        // The staged rows to memory, eight rows of 64 bytes a request; to: (row0, col), `cols` columns there.
+        auto send = [&](char *to, int64_t pitch, int row0, int cols) {
             __syncwarp();
-            const uint32_t to = out + slot * (kStageOut / kSlots);
-            slot = slot + 1 == kSlots ? 0 : slot + 1;
-            return to;
-        };
-        auto send = [&](const CUtensorMap *map, uint32_t from, int col, int row, int plane) {
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                tma_store_3d(map, from, col, row, plane);
-                store_commit();
-            }
-        };
-        auto stage = [&](uint32_t to, int half, const float (&z)[32]) {
+            const int p = lane & 3, r0 = lane >> 2;
 #pragma unroll
-            for (int p = 0; p < 4; ++p)
-                st_shared16(to + piece<kBytes>(lane, 4 * half + p),
-                            make_uint4(pack2(z[8 * p], z[8 * p + 1]), pack2(z[8 * p + 2], z[8 * p + 3]),
-                                       pack2(z[8 * p + 4], z[8 * p + 5]), pack2(z[8 * p + 6], z[8 * p + 7])));
+            for (int i = 0; i < 4; ++i) {
+                const int r = r0 + i * 8;
+                const uint4 v = ld_shared16(staging + piece(r, p));
+                if (row0 + r < g.M && p * (kF32 ? 4 : 8) < cols) *reinterpret_cast<uint4 *>(to + r * pitch + p * 16) = v;
+            }
+            __syncwarp();
+        };
+        auto send_bf16 = [&](const f32x2 (&z)[16], bf16 *to, int64_t ld, int row0, int cols) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = unpack(z[4 * p + i]);
+                    w[i] = pack2(f.x, f.y);
+                }
+                st_shared16(staging + piece(lane, p), make_uint4(w[0], w[1], w[2], w[3]));
+            }
+            send(reinterpret_cast<char *>(to), ld * 2, row0, cols);
         };
         for (int u = unit0; u < units; u += unit_step, ++n) {
             const int split = u % g.splits;
@@ -292,8 +308,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             tile_of(u / g.splits, g, tm, tn);
             const int row0 = tm * Cfg::kTileM + rank * kBM + (warp & 3) * 32, col0 = tn * kBN + (warp >> 2) * kWarpCols;
             const int buf = n & 1;
-            // The residual's chunk, eight rows of 64 bytes a request; handed to the rows' lanes through
-            // the staging buffer.  Asked for ahead of the accumulator.
+            // The residual's chunk and a lane's bias, asked for ahead of the accumulator; both are handed
+            // to the lanes that need them through the staging buffer.
             uint4 res[4];
             auto ask = [&](int col) {
                 if (kF32 || !g.residual) return;
@@ -306,16 +322,20 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 }
             };
             ask(col0);
+            float bias0 = 0.f, bias1 = 0.f;
+            if (!kF32 && g.bias) {
+                if (col0 + lane < g.N) bias0 = __ldg(g.bias + col0 + lane);
+                if (kWarpCols == 64 && col0 + 32 + lane < g.N) bias1 = __ldg(g.bias + col0 + 32 + lane);
+            }
             if (!wait_bar(acc_full + buf * 8, (n / 2) & 1, abort_flag, &g_linear_status)) break;
             fence_after();
             const uint32_t acc = tmem + buf * kBN + (warp >> 2) * kWarpCols + ((uint32_t)(warp & 3) << 21);
-            uint32_t to = 0;
 #pragma unroll 1
             for (int c = 0; c < kWarpCols; c += kCols) {
-                const int col = col0 + c, half = kBytes == 128 ? (c / kCols) & 1 : 0;
+                const int col = col0 + c;
                 uint32_t v[kCols];
-                tmem_ld16(acc + c, v);
-                if constexpr (!kF32) tmem_ld16(acc + c + 16, v + 16);
+#pragma unroll
+                for (int i = 0; i < kCols; i += 16) tmem_ld16(acc + c + i, v + i);
                 tmem_wait_ld();
                 if (c + kCols >= kWarpCols) {               // the last read of this accumulator
                     fence_before();
@@ -325,58 +345,50 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                         else bar_arrive(acc_empty + buf * 8);
                     }
                 }
-                // A box that starts past the edge is left out; a half past it is clipped.
-                if (row0 >= g.M || col - half * kCols >= g.N) continue;
+                if (row0 >= g.M || col >= g.N) continue;
                 if constexpr (kF32) {
-                    if (half == 0) to = buffer();
 #pragma unroll
                     for (int p = 0; p < 4; ++p)
-                        st_shared16(to + piece<kBytes>(lane, 4 * half + p),
-                                    make_uint4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]));
-                    if (half == 1) send(&map_c, to, col - kCols, row0, split);
+                        st_shared16(staging + piece(lane, p), make_uint4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]));
+                    send(reinterpret_cast<char *>(static_cast<float *>(g.out) + ((int64_t)split * g.M + row0) * g.out_ld + col),
+                         g.out_ld * 4, row0, g.N - col);
                 } else {
-                    float z[32];
+                    f32x2 z[16];
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(v[i]);
+                    for (int i = 0; i < 16; ++i) z[i] = pack(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])));
                     if (g.bias) {
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(staging + lane * 4), "f"(c == 0 ? bias0 : bias1) : "memory");
+                        __syncwarp();
 #pragma unroll
                         for (int q = 0; q < 8; ++q) {
-                            if (col + q * 4 < g.N) {
-                                const float4 b = __ldg(reinterpret_cast<const float4 *>(g.bias + col + q * 4));
-                                z[4 * q] += b.x;
-                                z[4 * q + 1] += b.y;
-                                z[4 * q + 2] += b.z;
-                                z[4 * q + 3] += b.w;
-                            }
+                            const uint4 b = ld_shared16(staging + q * 16);
+                            z[2 * q] = add2(z[2 * q], pack(make_float2(__uint_as_float(b.x), __uint_as_float(b.y))));
+                            z[2 * q + 1] = add2(z[2 * q + 1], pack(make_float2(__uint_as_float(b.z), __uint_as_float(b.w))));
                         }
+                        __syncwarp();
                     }
-                    if constexpr (kOut == kOutPre) {
-                        to = buffer();
-                        stage(to, 0, z);
-                        send(&map_pre, to, col, row0, 0);
-                    }
+                    if constexpr (kOut == kOutPre) send_bf16(z, g.pre + (int64_t)row0 * g.pre_ld + col, g.pre_ld, row0, g.N - col);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) z[i] = act<kAct>(z[i]);
-                    if (half == 0) to = buffer();
+                    for (int i = 0; i < 16; ++i) z[i] = act2<kAct>(z[i]);
                     if (g.residual) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) st_shared16(to + piece<kBytes>(i * 8 + (lane >> 2), 4 * half + (lane & 3)), res[i]);
+                        for (int i = 0; i < 4; ++i) st_shared16(staging + piece(i * 8 + (lane >> 2), lane & 3), res[i]);
                         __syncwarp();
                         if (c + kCols < kWarpCols) ask(col + kCols);
 #pragma unroll
                         for (int p = 0; p < 4; ++p) {
-                            const uint4 r = ld_shared16(to + piece<kBytes>(lane, 4 * half + p));
-                            z[8 * p] += lo16(r.x), z[8 * p + 1] += hi16(r.x), z[8 * p + 2] += lo16(r.y), z[8 * p + 3] += hi16(r.y);
-                            z[8 * p + 4] += lo16(r.z), z[8 * p + 5] += hi16(r.z), z[8 * p + 6] += lo16(r.w), z[8 * p + 7] += hi16(r.w);
+                            const uint4 r = ld_shared16(staging + piece(lane, p));
+                            z[4 * p] = add2(z[4 * p], pack(make_float2(lo16(r.x), hi16(r.x))));
+                            z[4 * p + 1] = add2(z[4 * p + 1], pack(make_float2(lo16(r.y), hi16(r.y))));
+                            z[4 * p + 2] = add2(z[4 * p + 2], pack(make_float2(lo16(r.z), hi16(r.z))));
+                            z[4 * p + 3] = add2(z[4 * p + 3], pack(make_float2(lo16(r.w), hi16(r.w))));
                         }
                         __syncwarp();
                     }
-                    stage(to, half, z);
-                    if (kBytes == 64 || half == 1) send(&map_c, to, col - half * kCols, row0, 0);
+                    send_bf16(z, static_cast<bf16 *>(g.out) + (int64_t)row0 * g.out_ld + col, g.out_ld, row0, g.N - col);
                 }
             }
         }
-        if (lane == 0) store_wait_read<0>();        // the staging buffers are read; the writes need no waiting
     }
     fence_before();
     __syncthreads();
@@ -597,21 +609,6 @@ bool operand_map(CUtensorMap *map, const void *ptr, int64_t inner, int64_t outer
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// An output [planes][rows][cols]: boxes of `bytes` (64 or 128) by 32 rows.
-bool output_map(CUtensorMap *map, void *ptr, bool f32, int64_t cols, int64_t rows, int64_t ld, int planes, int bytes) {
-    EncodeFn fn = encode_fn();
-    if (!fn) return false;
-    const int es = f32 ? 4 : 2;
-    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
-    cuuint64_t strides[2] = {(cuuint64_t)ld * es, (cuuint64_t)ld * rows * es};
-    cuuint32_t box[3] = {(cuuint32_t)(bytes / es), 32, 1};
-    cuuint32_t one[3] = {1, 1, 1};
-    return fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, ptr, dims, strides, box, one,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-              CU_TENSOR_MAP_L2_PROMOTION_NONE,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 struct GemmPlan {
     bool pair;
     int bn, splits, steps_per_split, steps, tiles_m, tiles_n;
@@ -673,8 +670,7 @@ struct Epilogue {
 };
 
 template <bool kPair, bool kAMn, bool kBMn, int kBN, int kOut, int kAct>
-cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, const CUtensorMap &mp,
-                        const GemmArgs &g, cudaStream_t st) {
+cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const GemmArgs &g, cudaStream_t st) {
     using Cfg = GemmCfg<kPair, kBN>;
     auto *fn = k_gemm<kPair, kAMn, kBMn, kBN, kOut, kAct>;
     static std::atomic<int> ctas[64];               // per device: CTAs that fit, once the kernel is set up
@@ -707,57 +703,55 @@ cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUte
     const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits * (kPair ? 2 : 1);
     cfg.gridDim = dim3((unsigned)std::min<int64_t>(units, room));
     count_launches(1);
-    return cudaLaunchKernelEx(&cfg, fn, ma, mb, mc, mp, g);
+    return cudaLaunchKernelEx(&cfg, fn, ma, mb, g);
 }
 
 template <bool kPair, bool kAMn, bool kBMn, int kBN>
-cudaError_t pick_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, const CUtensorMap &mp,
-                      const GemmArgs &g, int out, cudaStream_t st) {
-    if (out == kOutF32) return launch_gemm<kPair, kAMn, kBMn, kBN, kOutF32, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
+cudaError_t pick_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const GemmArgs &g, int out, cudaStream_t st) {
+    if (out == kOutF32) return launch_gemm<kPair, kAMn, kBMn, kBN, kOutF32, RLM_ACT_NONE>(ma, mb, g, st);
     if constexpr (!kAMn && !kBMn) {         // only the forward product has an activation, or keeps z
         switch (g.act * 2 + (out == kOutPre)) {
-            case RLM_ACT_NONE * 2 + 1: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
-            case RLM_ACT_SILU * 2: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_SILU>(ma, mb, mc, mp, g, st);
-            case RLM_ACT_SILU * 2 + 1: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_SILU>(ma, mb, mc, mp, g, st);
-            case RLM_ACT_GELU * 2: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_GELU>(ma, mb, mc, mp, g, st);
-            case RLM_ACT_GELU * 2 + 1: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_GELU>(ma, mb, mc, mp, g, st);
+            case RLM_ACT_NONE * 2 + 1: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_NONE>(ma, mb, g, st);
+            case RLM_ACT_SILU * 2: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_SILU>(ma, mb, g, st);
+            case RLM_ACT_SILU * 2 + 1: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_SILU>(ma, mb, g, st);
+            case RLM_ACT_GELU * 2: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_GELU>(ma, mb, g, st);
+            case RLM_ACT_GELU * 2 + 1: return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_GELU>(ma, mb, g, st);
             case RLM_ACT_SIGMOID * 2:
-                return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_SIGMOID>(ma, mb, mc, mp, g, st);
+                return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_SIGMOID>(ma, mb, g, st);
             case RLM_ACT_SIGMOID * 2 + 1:
-                return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_SIGMOID>(ma, mb, mc, mp, g, st);
+                return launch_gemm<kPair, kAMn, kBMn, kBN, kOutPre, RLM_ACT_SIGMOID>(ma, mb, g, st);
             default: break;
         }
     }
-    return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_NONE>(ma, mb, mc, mp, g, st);
+    return launch_gemm<kPair, kAMn, kBMn, kBN, kOutBf16, RLM_ACT_NONE>(ma, mb, g, st);
 }
 
 template <bool kAMn, bool kBMn>
 cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Epilogue &ep, float *part, cudaStream_t st) {
     const GemmPlan p = gemm_plan(M, N, K);
-    CUtensorMap ma, mb, mc, mp;
+    CUtensorMap ma, mb;
     if (!(kAMn ? operand_map(&ma, a.ptr, M, K, a.ld, 64) : operand_map(&ma, a.ptr, K, M, a.ld, kBM)) ||
         !(kBMn ? operand_map(&mb, b.ptr, N, K, b.ld, 64) : operand_map(&mb, b.ptr, K, N, b.ld, p.pair ? p.bn / 2 : p.bn)))
         return cudaErrorInvalidValue;
     const bool split = p.splits > 1;
-    const int out = split || ep.out_f32 ? kOutF32 : ep.pre ? kOutPre : kOutBf16, bytes = store_bytes(out, p.bn);
-    if (!(split ? output_map(&mc, part, true, N, M, N, p.splits, bytes)
-                : output_map(&mc, ep.out, ep.out_f32, N, M, ep.out_ld, 1, bytes)))
-        return cudaErrorInvalidValue;
-    mp = mc;
-    if (out == kOutPre && !output_map(&mp, ep.pre, false, N, M, ep.pre_ld, 1, bytes)) return cudaErrorInvalidValue;
+    const int out = split || ep.out_f32 ? kOutF32 : ep.pre ? kOutPre : kOutBf16;
     GemmArgs g = {};
     g.M = (int)M, g.N = (int)N, g.K = (int)K;
     g.tiles_m = p.tiles_m, g.tiles_n = p.tiles_n;
     g.splits = p.splits, g.steps_per_split = p.steps_per_split, g.steps = p.steps;
+    g.out = split ? part : ep.out;
+    g.out_ld = split ? N : ep.out_ld;
     if (!split) {
+        g.pre = static_cast<bf16 *>(ep.pre);
+        g.pre_ld = ep.pre_ld;
         g.bias = ep.bias;
         g.residual = ep.residual;
         g.residual_ld = ep.residual_ld;
         g.act = ep.act;
     }
-    const cudaError_t e = !p.pair        ? pick_gemm<false, kAMn, kBMn, 128>(ma, mb, mc, mp, g, out, st)
-                          : p.bn == 256 ? pick_gemm<true, kAMn, kBMn, 256>(ma, mb, mc, mp, g, out, st)
-                                        : pick_gemm<true, kAMn, kBMn, 128>(ma, mb, mc, mp, g, out, st);
+    const cudaError_t e = !p.pair        ? pick_gemm<false, kAMn, kBMn, 128>(ma, mb, g, out, st)
+                          : p.bn == 256 ? pick_gemm<true, kAMn, kBMn, 256>(ma, mb, g, out, st)
+                                        : pick_gemm<true, kAMn, kBMn, 128>(ma, mb, g, out, st);
     if (e != cudaSuccess || !split) return e;
     FinishArgs f = {};
     f.part = part;
