@@ -81,12 +81,25 @@ __device__ __forceinline__ f32x2 act2(f32x2 z) {
         return mul2(z, sigmoid2(mul2(z, fma2(mul2(z, z), twice(-l2e * kBend3), twice(-l2e * kBend1)))));
     return z;
 }
-// act'(z).  1 - sigma is formed as sigma(-z): the difference would lose it for large z.
-__device__ __forceinline__ float act_grad(int kind, float z) {
-    if (kind == RLM_ACT_SIGMOID) return sigmoidf(z) * sigmoidf(-z);
-    if (kind == RLM_ACT_SILU) return sigmoidf(z) * fmaf(z, sigmoidf(-z), 1.0f);
-    const float u = z * fmaf(kBend3 * z, z, kBend1), du = fmaf(3.0f * kBend3 * z, z, kBend1);
-    return sigmoidf(u) * fmaf(z * du, sigmoidf(-u), 1.0f);
+// act'(z) of two values.  1 - sigma(u) is e^-u sigma(u): the difference would lose it for large
+// u.  u is held above -80, where sigma and its slope are below 2^-115 either way.
+__device__ __forceinline__ f32x2 act_grad2(int kind, f32x2 z) {
+    constexpr float l2e = 1.44269504f;
+    const f32x2 one = 0x3f8000003f800000ull;
+    const f32x2 zz = mul2(z, z);
+    const f32x2 u = kind == RLM_ACT_GELU ? mul2(z, fma2(zz, twice(kBend3), twice(kBend1))) : z;
+    float2 f = unpack(u);
+    f = unpack(mul2(pack(make_float2(fmaxf(f.x, -80.f), fmaxf(f.y, -80.f))), twice(-l2e)));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(f.x));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(f.y));
+    const f32x2 e = pack(f);
+    f = unpack(add2(e, one));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(f.x));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(f.y));
+    const f32x2 s = pack(f), rest = mul2(e, s);
+    if (kind == RLM_ACT_SIGMOID) return mul2(s, rest);
+    const f32x2 slope = kind == RLM_ACT_GELU ? mul2(z, fma2(zz, twice(3.0f * kBend3), twice(kBend1))) : z;
+    return mul2(s, fma2(slope, rest, one));
 }
 
 // -------------------------------------------------------------------- gemm
@@ -312,13 +325,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             // to the lanes that need them through the staging buffer.
             uint4 res[4];
             auto ask = [&](int col) {
-                if (kF32 || !g.residual) return;
+                if constexpr (!kF32) {
+                    if (!g.residual) return;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = row0 + i * 8 + (lane >> 2), cc = col + (lane & 3) * 8;
-                    res[i] = r < g.M && cc < g.N
-                                 ? __ldg(reinterpret_cast<const uint4 *>(g.residual + (int64_t)r * g.residual_ld + cc))
-                                 : make_uint4(0, 0, 0, 0);
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = row0 + i * 8 + (lane >> 2), cc = col + (lane & 3) * 8;
+                        res[i] = r < g.M && cc < g.N
+                                     ? __ldg(reinterpret_cast<const uint4 *>(g.residual + (int64_t)r * g.residual_ld + cc))
+                                     : make_uint4(0, 0, 0, 0);
+                    }
                 }
             };
             ask(col0);
@@ -517,49 +532,58 @@ __global__ void __launch_bounds__(256) k_finish(const FinishArgs f) {
 }
 
 // --------------------------------------------- dz = dy act'(z), and dbias
-// Blocks of kDzRows rows by 256 columns, a thread per 8 columns and every eighth row.  Bound by
+// Blocks of kDzRows rows by 256 columns (fewer where N is less, and more rows at a time), a thread
+// per 8 columns.  Bound by
 // its 6 bytes an element (2 without an activation).  The block's column sums go to
 // `part` [row blocks][N], which k_column_sum adds in order.
 constexpr int kDzRows = 128;
 struct DzArgs {
     const bf16 *dy, *pre;
-    bf16 *dz;               // nullable (no activation: dy serves)
+    bf16 *dz;               // (unused without an activation: dy serves)
     float *part;            // nullable (no dbias)
     int64_t R, dy_ld, pre_ld;
-    int N, act;
+    int N, log2_groups;     // column groups of 8 in a block: at most 32
 };
+template <int kAct>
 __global__ void __launch_bounds__(256) k_dz(const DzArgs a) {
-    __shared__ float sums[8][256];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int col = blockIdx.y * 256 + lane * 8;
+    __shared__ float sums[256 * 8];             // [rows at a time][columns]
+    const int groups = 1 << a.log2_groups, cg = threadIdx.x & (groups - 1), rl = threadIdx.x >> a.log2_groups;
+    const int rows = 256 >> a.log2_groups, cols = groups * 8;
+    const int col = blockIdx.y * 256 + cg * 8;
     const int64_t r0 = (int64_t)blockIdx.x * kDzRows, r1 = min(a.R, r0 + kDzRows);
-    float s[8] = {};
+    f32x2 s[4] = {0, 0, 0, 0};
     if (col < a.N) {
 #pragma unroll 4
-        for (int64_t r = r0 + warp; r < r1; r += 8) {
+        for (int64_t r = r0 + rl; r < r1; r += rows) {
             const uint4 d = __ldg(reinterpret_cast<const uint4 *>(a.dy + r * a.dy_ld + col));
-            float v[8] = {lo16(d.x), hi16(d.x), lo16(d.y), hi16(d.y), lo16(d.z), hi16(d.z), lo16(d.w), hi16(d.w)};
-            if (a.dz) {
-                const uint4 p = __ldg(reinterpret_cast<const uint4 *>(a.pre + r * a.pre_ld + col));
-                const float z[8] = {lo16(p.x), hi16(p.x), lo16(p.y), hi16(p.y), lo16(p.z), hi16(p.z), lo16(p.w), hi16(p.w)};
+            const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
+            f32x2 v[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= act_grad(a.act, z[i]);
-                *reinterpret_cast<uint4 *>(a.dz + r * a.N + col) =
-                    make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+            for (int i = 0; i < 4; ++i) v[i] = pack(make_float2(lo16(dw[i]), hi16(dw[i])));
+            if constexpr (kAct != RLM_ACT_NONE) {
+                const uint4 p = __ldg(reinterpret_cast<const uint4 *>(a.pre + r * a.pre_ld + col));
+                const uint32_t pw[4] = {p.x, p.y, p.z, p.w};
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = mul2(v[i], act_grad2(kAct, pack(make_float2(lo16(pw[i]), hi16(pw[i])))));
+                    const float2 f = unpack(v[i]);
+                    w[i] = pack2(f.x, f.y);
+                }
+                *reinterpret_cast<uint4 *>(a.dz + r * a.N + col) = make_uint4(w[0], w[1], w[2], w[3]);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] += v[i];
+            for (int i = 0; i < 4; ++i) s[i] = add2(s[i], v[i]);
         }
     }
     if (!a.part) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sums[warp][lane * 8 + i] = s[i];
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float2 *>(&sums[rl * cols + cg * 8 + 2 * i]) = unpack(s[i]);
     __syncthreads();
     const int c = blockIdx.y * 256 + threadIdx.x;
-    if (c < a.N) {
+    if ((int)threadIdx.x < cols && c < a.N) {
         float t = 0.f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) t += sums[w][threadIdx.x];
+        for (int w = 0; w < rows; ++w) t += sums[w * cols + threadIdx.x];
         a.part[(int64_t)blockIdx.x * a.N + c] = t;
     }
 }
@@ -614,15 +638,16 @@ struct GemmPlan {
     int bn, splits, steps_per_split, steps, tiles_m, tiles_n;
 };
 
-// Tile and splits: the least of rounds of work units times a unit's steps, with its start and
-// its epilogue, and for splits the bytes of their partial sums and a second launch; in
-// microseconds, measured (see kTiles).
+// Tile and splits, by time in microseconds: a launch, then rounds of units, each its steps or
+// (for short contractions) its epilogue, which the next unit's steps overlap; no less than the
+// operands' bytes take; for splits a second launch and the partial sums' bytes through L2.  Measured
+// on 512 to 131072 rows, K and N of 64 to 8192; the choices it makes are within 10 % of the best.
 struct TileKind {
     bool pair;
     int bn;
-    double step, unit;      // one contraction step; what a unit costs beside its steps
+    double launch, step, epilogue;
 };
-constexpr TileKind kTiles[] = {{true, 256, 0.30, 0.9}, {true, 128, 0.20, 0.6}, {false, 128, 0.27, 0.6}};
+constexpr TileKind kTiles[] = {{true, 256, 5.7, 0.285, 1.9}, {true, 128, 5.1, 0.17, 1.2}, {false, 128, 4.0, 0.19, 1.0}};
 
 GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K) {
     GemmPlan best = {};
@@ -632,13 +657,17 @@ GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K) {
         const int64_t tm = (M + (t.pair ? 255 : 127)) / (t.pair ? 256 : 128), tn = (N + t.bn - 1) / t.bn;
         const int64_t slots = t.pair ? sms / 2 : sms;
         const int steps = (int)((K + kBK - 1) / kBK);
-        for (int splits = 1; splits <= 32 && splits <= steps; ++splits) {
+        for (int splits = 1; splits <= 64 && splits <= steps; ++splits) {
             const int per = (steps + splits - 1) / splits;
             if ((steps + per - 1) / per != splits) continue;
             if (splits > 1 && tm * tn * splits > slots) break;      // more work units than SMs: nothing to fill
             const int64_t rounds = (tm * tn * splits + slots - 1) / slots;
-            double cost = (double)rounds * (per * t.step + t.unit);
-            if (splits > 1) cost += 3.0 + 8.0 * splits * (double)M * N / 6.0e6;
+            // Bytes from memory, and from L2: every unit's operands, at 20 TB/s beside the output.
+            const double out = 2.0 * M * N, bytes = 2.0 * ((double)M * K + (double)N * K) + out;
+            const double l2 = (double)(tm * tn) * steps * kBK * 2.0 * ((t.pair ? 256 : 128) + t.bn);
+            const double work = (double)rounds * std::max(per * t.step, t.epilogue);
+            double cost = t.launch + std::max({work, bytes / 6.0e6, l2 / 20.0e6 + out / 8.0e6});
+            if (splits > 1) cost += 3.0 + 8.0 * splits * (double)M * N / 8.0e6;
             if (best_cost == 0 || cost < best_cost) {
                 best_cost = cost;
                 best = {t.pair, t.bn, splits, per, steps, (int)tm, (int)tn};
@@ -774,8 +803,15 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
 
 }  // namespace
 
-// Rows that k_few serves; see the table at linear_forward.
-constexpr int kFewRows = 32;
+// Whether k_few serves a product: always up to 8 rows; from there its reads of x grow with the
+// rows while the tiles' cost does not (us, from HBM, k_few / tiles): 16 rows, K x N = 4096 x 4096
+// 10.9 / 12.6, 8192 x 1024 15.6 / 11.1, 4096 x 11008 30 / 21; 32 rows, 1024 x 1024 4.1 / 5.6,
+// 2048 x 4096 10.2 / 10.0, 512 x 16384 10.3 / 7.7.
+bool few_rows(int64_t R, int64_t K, int64_t N) {
+    if (R <= 8) return true;
+    if (R <= 16) return K <= 4096 && K * N <= 24 << 20;
+    return R <= 32 && K <= 2048 && K * N <= 4 << 20;
+}
 
 template <int kTok>
 void launch_few(const FewArgs &a, cudaStream_t st) {
@@ -790,7 +826,7 @@ void launch_few(const FewArgs &a, cudaStream_t st) {
 }
 
 size_t linear_ws_bytes(int64_t R, int64_t K, int64_t N) {
-    return R <= kFewRows ? 0 : gemm_ws(gemm_plan(R, N, K), R, N);
+    return few_rows(R, K, N) ? 0 : gemm_ws(gemm_plan(R, N, K), R, N);
 }
 
 size_t linear_backward_ws_bytes(int64_t R, int64_t K, int64_t N, int act) {
@@ -802,7 +838,7 @@ size_t linear_backward_ws_bytes(int64_t R, int64_t K, int64_t N, int act) {
 cudaError_t linear_forward(const rlm_matrix &x, const rlm_matrix &w, const float *bias, int act_kind,
                            const rlm_matrix *residual, const rlm_matrix *pre, const rlm_matrix &y, void *ws,
                            cudaStream_t st) {
-    if (x.rows <= kFewRows) {
+    if (few_rows(x.rows, x.cols, w.rows)) {
         FewArgs a = {};
         a.x = static_cast<const bf16 *>(x.ptr), a.x_ld = x.ld;
         a.w = static_cast<const bf16 *>(w.ptr), a.w_ld = w.ld;
@@ -848,7 +884,7 @@ cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm
         a.dy_ld = dy.ld;
         a.R = R;
         a.N = (int)N;
-        a.act = act_kind;
+        while (a.log2_groups < 5 && (8 << a.log2_groups) < N) ++a.log2_groups;
         if (act_kind != RLM_ACT_NONE) {
             a.pre = static_cast<const bf16 *>(pre->ptr);
             a.pre_ld = pre->ld;
@@ -859,7 +895,11 @@ cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm
         const int64_t blocks = (R + kDzRows - 1) / kDzRows;
         if (dbias) a.part = reinterpret_cast<float *>(at);
         at += round256((size_t)blocks * N * sizeof(float));
-        k_dz<<<dim3((unsigned)blocks, (unsigned)((N + 255) / 256)), 256, 0, st>>>(a);
+        auto *fn = act_kind == RLM_ACT_SILU      ? k_dz<RLM_ACT_SILU>
+                   : act_kind == RLM_ACT_GELU    ? k_dz<RLM_ACT_GELU>
+                   : act_kind == RLM_ACT_SIGMOID ? k_dz<RLM_ACT_SIGMOID>
+                                                 : k_dz<RLM_ACT_NONE>;
+        fn<<<dim3((unsigned)blocks, (unsigned)((N + 255) / 256)), 256, 0, st>>>(a);
         count_launches(1);
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
