@@ -24,11 +24,13 @@
 // A thread composes its run (first pass), keeps -b in registers, and once it knows the
 // state at the run's start walks the run again for the outputs (second pass).
 //
-// A ninth warp turns runs into states.  Its lane holds one channel pair of 8
-// consecutive runs (64 tokens, one saved chunk): it composes them, scans across lanes,
-// adds the carry and hands every run its start state.  The data warps work on the next
-// tile's first pass meanwhile: the second pass of tile w follows the first pass of
-// tile w + 1, so the hand-over, and the exchange below, are off their path.
+// Two more warps turn runs into states, a tile each in turn.  A lane holds one channel
+// pair of 8 consecutive runs (64 tokens, one saved chunk): it composes them, scans across
+// lanes, adds the carry (which one warp hands the other) and gives every run its start
+// state.  The data warps work on the next tile's first pass meanwhile: the second pass of
+// tile w follows the first pass of tile w + 1.  (One such warp took 3100 cycles a tile where
+// a cluster shares a chain, half of them the exchange, and bounded the kernel: 54 us at
+// B = 4, L = 32768, D = 256.)
 //
 // Segments.  Few channels would leave SMs idle, so a cluster of nseg CTAs (2, 4 or 8)
 // shares a chain of tiles: in wave w CTA s takes tile w nseg + s and sends the tile's
@@ -52,9 +54,10 @@ __device__ int g_scan_status = 0;
 namespace {
 
 constexpr int kDataThreads = 256;
-constexpr int kThreads = kDataThreads + 32;         // and the warp that turns runs into states
+constexpr int kThreads = kDataThreads + 64;         // and the two warps that turn runs into states
 constexpr int kS = 8;                               // tokens of a run
-constexpr int kBarRuns = 1, kBarStates = 3;         // named barriers, two of each by tile parity
+constexpr int kBarRuns = 1, kBarStates = 3, kBarCarry = 5;      // named barriers, two of each by tile parity
+constexpr int kHandOver = kDataThreads + 32;        // threads of the first two: the data warps and one state warp
 constexpr int kChunk = RLM_SCAN_CHUNK;              // tokens between saved states
 constexpr long long kWaitLimit = 4000000000ll;      // SM cycles: about 2 s
 
@@ -93,41 +96,42 @@ struct ScanArgs {
 
 constexpr f32x2 kOne = 0x3f8000003f800000ull, kMinus = 0xbf800000bf800000ull;
 
-// (A, H) of two channels as (A.x, A.y, H.x, H.y); `later` o `earlier`.
-__device__ __forceinline__ float4 compose(float4 earlier, float4 later) {
-    return make_float4(later.x * earlier.x, later.y * earlier.y, fmaf(later.x, earlier.z, later.z),
-                       fmaf(later.y, earlier.w, later.w));
-}
-__device__ __forceinline__ float4 shfl4(float4 v, int src) {
-    return make_float4(__shfl_sync(~0u, v.x, src), __shfl_sync(~0u, v.y, src), __shfl_sync(~0u, v.z, src),
-                       __shfl_sync(~0u, v.w, src));
-}
-__device__ __forceinline__ float4 identity4() { return make_float4(1.f, 1.f, 0.f, 0.f); }
-__device__ __forceinline__ float2 apply(float4 f, float2 h) {
-    return make_float2(fmaf(f.x, h.x, f.z), fmaf(f.y, h.y, f.w));
-}
+// A run of two channels: h -> A h + H.
+struct alignas(16) Run {
+    f32x2 A, H;
+};
+__device__ __forceinline__ Run identity() { return {kOne, 0}; }
+__device__ __forceinline__ f32x2 apply(Run f, f32x2 h) { return fma2(f.A, h, f.H); }
+__device__ __forceinline__ Run compose(Run earlier, Run later) { return {mul2(later.A, earlier.A), apply(later, earlier.H)}; }
+__device__ __forceinline__ Run shuffle(Run v, int src) { return {__shfl_sync(~0u, v.A, src), __shfl_sync(~0u, v.H, src)}; }
 
 // Inclusive scan over the lanes of one channel pair (P apart); kRev: over those after.
-template <bool kRev>
-__device__ __forceinline__ float4 lane_scan(float4 v, int P, int lane) {
+template <bool kRev, int P>
+__device__ __forceinline__ Run lane_scan(Run v, int lane) {
+#pragma unroll
     for (int d = P; d < 32; d <<= 1) {
         const int src = kRev ? lane + d : lane - d;
-        const float4 o = shfl4(v, src & 31);
+        const Run o = shuffle(v, src & 31);
         if (kRev ? src < 32 : src >= 0) v = compose(o, v);
     }
     return v;
 }
 // The same, without this lane's own run.
-template <bool kRev>
-__device__ __forceinline__ float4 lane_exclusive(float4 incl, int P, int lane) {
+template <bool kRev, int P>
+__device__ __forceinline__ Run lane_exclusive(Run incl, int lane) {
+    if (P == 32) return identity();
     const int src = kRev ? lane + P : lane - P;
-    const float4 o = shfl4(incl, src & 31);
-    return (kRev ? src < 32 : src >= 0) ? o : identity4();
+    const Run o = shuffle(incl, src & 31);
+    return (kRev ? src < 32 : src >= 0) ? o : identity();
 }
 
-__device__ __forceinline__ void bar_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kThreads) : "memory"); }
+template <int kCount = kHandOver>
+__device__ __forceinline__ void bar_sync(int id) {
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kCount) : "memory");
+}
+template <int kCount = kHandOver>
 __device__ __forceinline__ void bar_arrive(int id) {
-    asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kThreads) : "memory");
+    asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kCount) : "memory");
 }
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -137,10 +141,12 @@ __device__ __forceinline__ void cluster_sync() {
 
 constexpr int kMaxSeg = 8;      // portable cluster size
 
-// What a cluster's members send one another: tile runs by wave parity.
+// What a cluster's members send one another: tile runs, four waves' worth (see exchange()).
+constexpr int kWaves = 4;
+template <int P>
 struct Peers {
-    float4 run[2][kMaxSeg][32];
-    unsigned long long full[2];     // mbarriers: one arrival (this CTA's) and the entries' bytes
+    Run run[kWaves][kMaxSeg][P];
+    unsigned long long full[kWaves];    // mbarriers: one arrival (this CTA's) and the entries' bytes
 };
 
 // Bounded wait; after a timeout (now or earlier) the kernel runs on with what is there.
@@ -166,46 +172,68 @@ __device__ __forceinline__ void wait_full(uint32_t bar, uint32_t parity, bool &g
     }
 }
 
-// One wave's exchange by the ninth warp: sends this tile's run `mine` (held by every lane
-// of a pair) to all members and returns the composition of the tiles before it (*pre) and
-// of the whole wave.  A member sends wave w + 2 only after it has received this one's wave
-// w + 1, which this warp sent after it had read wave w: the two buffers suffice.
-__device__ __forceinline__ void exchange(float4 mine, Peers &peers, int wave, int seg, int nseg, int P, int cp,
-                                         bool &gave_up, float4 *pre, float4 *all) {
-    const int lane = threadIdx.x & 31, par = wave & 1;
-    const uint32_t bar = smem_u32(&peers.full[par]), slot = smem_u32(&peers.run[par][seg][cp]);
+// One wave's exchange by its state warp: sends this tile's run `mine` (held by every lane of a
+// pair) to all members and returns the composition of the tiles before it (*pre) and of the
+// whole wave.  A member sends wave w + 4 into the place of wave w once its data warps have
+// passed wave w + 2, which took this CTA's run of wave w + 2, sent by the warp that read wave w
+// just before.
+template <int P>
+__device__ __forceinline__ void exchange(Run mine, Peers<P> &peers, int wave, int seg, int nseg, int cp, bool &gave_up,
+                                         Run *pre, Run *all) {
+    const int lane = threadIdx.x & 31, at = wave % kWaves;
+    const uint32_t bar = smem_u32(&peers.full[at]), slot = smem_u32(&peers.run[at][seg][cp]);
     if (lane == 0)
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(nseg * P * 16) : "memory");
     for (int s = lane / P; s < nseg; s += 32 / P) {
         uint32_t to, tb;
         asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(slot), "r"(s));
         asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(tb) : "r"(bar), "r"(s));
-        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
-                         to),
-                     "r"(__float_as_uint(mine.x)), "r"(__float_as_uint(mine.y)), "r"(__float_as_uint(mine.z)),
-                     "r"(__float_as_uint(mine.w)), "r"(tb)
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(to),
+                     "l"(mine.A), "l"(mine.H), "r"(tb)
                      : "memory");
     }
-    wait_full(bar, (wave >> 1) & 1, gave_up);
-    float4 fa = identity4();
-    *pre = fa;
+    wait_full(bar, (wave / kWaves) & 1, gave_up);
+    Run v[kMaxSeg];
+#pragma unroll
+    for (int s = 0; s < kMaxSeg; ++s) v[s] = s < nseg ? peers.run[at][s][cp] : identity();
+    Run f = identity();
+    *pre = f;
 #pragma unroll
     for (int s = 0; s < kMaxSeg; ++s) {
-        if (s < nseg) {
-            if (s == seg) *pre = fa;
-            fa = compose(fa, peers.run[par][s][cp]);
-        }
+        if (s == seg) *pre = f;
+        f = compose(f, v[s]);
     }
-    *all = fa;
+    *all = f;
     __syncwarp();
+}
+
+// A state warp's share of a wave once its tile's run is known: exchange, the carry from the
+// other state warp, the next wave's carry to it.  Returns the state before the tile.
+template <int P>
+__device__ __forceinline__ f32x2 carry_over(Run total, Peers<P> &peers, f32x2 (&carries)[2][32], f32x2 &carry, int wave, int n,
+                                            int seg, int nseg, int cp, bool &gave_up) {
+    Run pre = identity(), all = total;
+    if (nseg > 1) exchange<P>(total, peers, wave, seg, nseg, cp, gave_up, &pre, &all);
+    if (wave > 0) {
+        bar_sync<64>(kBarCarry + ((wave - 1) & 1));
+        carry = carries[(wave - 1) & 1][cp];
+    }
+    const f32x2 h = apply(pre, carry);
+    carry = apply(all, carry);
+    if (wave + 1 < n) {
+        if ((threadIdx.x & 31) < P) carries[wave & 1][cp] = carry;
+        bar_arrive<64>(kBarCarry + (wave & 1));
+    }
+    return h;
 }
 
 // Set-up and end of a cluster: no member sends before all have their barriers, none
 // leaves while another may still send to it.
-__device__ __forceinline__ void open_peers(Peers &peers, int nseg) {
+template <int P>
+__device__ __forceinline__ void open_peers(Peers<P> &peers, int nseg) {
     if (nseg < 2) return;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kWaves; ++i)
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&peers.full[i])) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -247,7 +275,7 @@ template <typename T, int kFields, int kStages, int kLog2P>
 struct Ring {
     static constexpr int kRowBytes = 2 * (int)sizeof(T) << kLog2P;
     static constexpr int kRunBytes = (kS + 1) * kRowBytes;
-    static constexpr int kFieldBytes = (32 >> kLog2P) * kRunBytes;
+    static constexpr int kFieldBytes = (32 >> kLog2P) * kRunBytes - kRowBytes;      // (no row after the last run)
     static constexpr int kStageBytes = kFields * kFieldBytes;
     static constexpr int kWarpBytes = kStages * kStageBytes;
     static constexpr int kBytes = kWarpBytes * (kDataThreads / 32);
@@ -367,52 +395,44 @@ using FwdRing = Ring<T, 2, kFwdStages<T>, kLog2P>;          // fields: x, g
 template <typename T, bool kLeak, int kLog2P>
 __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_forward(const ScanArgs<T> a) {
     extern __shared__ __align__(16) unsigned char ring_mem[];
-    __shared__ Peers peers;
-    __shared__ float4 runs[2][kDataThreads];
-    __shared__ float2 states[2][kDataThreads];
+    __shared__ Peers<1 << kLog2P> peers;
+    __shared__ Run runs[2][kDataThreads];
+    __shared__ f32x2 states[2][kDataThreads], carries[2][32];
+    constexpr int P = 1 << kLog2P;
     const Where w = where<kLog2P>(a);
     constexpr int ST = kFwdStages<T>;
     open_peers(peers, a.nseg);
 
-    if (w.warp == kDataThreads / 32) {
-        // Runs to states: lane (part, cp) holds runs 8 part .. 8 part + 7.
-        const int first = (w.lane / w.P) * 8 * w.P + w.cp;
-        float2 carry = make_float2(0.f, 0.f);
-        if (a.state_in && w.on) carry = *reinterpret_cast<const float2 *>(a.state_in + (int64_t)w.row * a.D + w.c);
+    if (w.warp >= kDataThreads / 32) {
+        // Runs to states, the two warps in turn: lane (part, cp) holds runs 8 part .. 8 part + 7.
+        const int first = (w.lane / P) * 8 * P + w.cp, me = w.warp - kDataThreads / 32;
+        f32x2 carry = 0;
+        if (a.state_in && w.on) carry = pack(*reinterpret_cast<const float2 *>(a.state_in + (int64_t)w.row * a.D + w.c));
         bool gave_up = false;
-        for (int k = 0; k < w.n; ++k) {
+        for (int k = me; k < w.n; k += 2) {
             const int par = k & 1, tile = k * a.nseg + w.seg;
             bar_sync(kBarRuns + par);
-            float4 f = identity4();
+            Run f = identity();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f = compose(f, runs[par][first + j * w.P]);
-            const float4 incl = lane_scan<false>(f, w.P, w.lane);
-            const float4 excl = lane_exclusive<false>(incl, w.P, w.lane);
-            const float4 total = shfl4(incl, 32 - w.P + w.cp);
-            float2 h = carry;
-            if (a.nseg > 1) {
-                float4 pre, all;
-                exchange(total, peers, k, w.seg, a.nseg, w.P, w.cp, gave_up, &pre, &all);
-                h = apply(pre, carry);
-                carry = apply(all, carry);
-            } else {
-                carry = apply(total, carry);
-            }
+            for (int j = 0; j < 8; ++j) f = compose(f, runs[par][first + j * P]);
+            const Run incl = lane_scan<false, P>(f, w.lane), excl = lane_exclusive<false, P>(incl, w.lane);
+            const Run total = P == 32 ? incl : shuffle(incl, 32 - P + w.cp);
+            f32x2 h = carry_over<P>(total, peers, carries, carry, k, w.n, w.seg, a.nseg, w.cp, gave_up);
             h = apply(excl, h);
-            const int t0 = tile * w.tile_tokens + (w.lane / w.P) * kChunk;
+            const int t0 = tile * w.tile_tokens + (w.lane / P) * kChunk;
             if (a.saved && w.on && t0 < a.L)
-                *reinterpret_cast<float2 *>(a.saved + ((int64_t)w.row * a.nchunks + t0 / kChunk) * a.D + w.c) = h;
+                *reinterpret_cast<float2 *>(a.saved + ((int64_t)w.row * a.nchunks + t0 / kChunk) * a.D + w.c) = unpack(h);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                states[par][first + j * w.P] = h;
-                h = apply(runs[par][first + j * w.P], h);
+                states[par][first + j * P] = h;
+                h = apply(runs[par][first + j * P], h);
             }
             bar_arrive(kBarStates + par);
         }
         // Every member holds the same carry.  state_out may be state_in: all members have read it.
         close_peers(a.nseg);
-        if (a.state_out && w.on && w.lane < w.P && w.seg == 0)
-            *reinterpret_cast<float2 *>(a.state_out + (int64_t)w.row * a.D + w.c) = carry;
+        if (a.state_out && w.on && w.lane < P && w.seg == 0 && me == ((w.n - 1) & 1))
+            *reinterpret_cast<float2 *>(a.state_out + (int64_t)w.row * a.D + w.c) = unpack(carry);
         return;
     }
 
@@ -447,14 +467,13 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_forward(const Scan
             A = fma2(nb[i], A, A);
             H = advance<kLeak>(H, nb[i], ring.value(st, 0, i));
         }
-        const float2 fa = unpack(A), fh = unpack(H);
-        runs[k & 1][threadIdx.x] = make_float4(fa.x, fa.y, fh.x, fh.y);
+        runs[k & 1][threadIdx.x] = {A, H};
         bar_arrive(kBarRuns + (k & 1));
     };
     auto second = [&](int k, const f32x2 (&nb)[kS]) {
         const int st = k % ST, t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
         bar_sync(kBarStates + (k & 1));
-        f32x2 h = pack(states[k & 1][threadIdx.x]);
+        f32x2 h = states[k & 1][threadIdx.x];
         T *out = yp + (int64_t)t0 * a.y_l;
         if (w.on && t0 + kS <= w.len) {
 #pragma unroll
@@ -488,71 +507,57 @@ template <typename T, bool kLeak, int kLog2P>
 __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_backward(const ScanArgs<T> a) {
     extern __shared__ __align__(16) unsigned char ring_mem[];
     // Gradients are carried negated: with -b at hand, b G = (-b)(-G) needs no sign.
-    __shared__ Peers peers;
-    __shared__ float4 runs[2][kDataThreads];        // (A, H) of a run
-    __shared__ float2 ends[2][kDataThreads];        // its -C from a zero C after it; then its -C
-    __shared__ float2 states[2][kDataThreads];
+    __shared__ Peers<1 << kLog2P> peers;
+    __shared__ Run runs[2][kDataThreads];
+    __shared__ f32x2 ends[2][kDataThreads];         // a run's -C from a zero C after it; then its -C
+    __shared__ f32x2 states[2][kDataThreads], carries[2][32];
+    constexpr int P = 1 << kLog2P;
     const Where w = where<kLog2P>(a);
     constexpr int ST = kBwdStages<T>;
     open_peers(peers, a.nseg);
 
-    if (w.warp == kDataThreads / 32) {
+    if (w.warp >= kDataThreads / 32) {
         // A lane's 8 runs are one chunk: their states follow from the chunk's saved state.
-        const int part = w.lane / w.P, first = part * 8 * w.P + w.cp;
-        float2 carry = make_float2(0.f, 0.f);       // -C after the wave
-        if (a.state_in && w.on) {
-            carry = *reinterpret_cast<const float2 *>(a.state_in + (int64_t)w.row * a.D + w.c);
-            carry = make_float2(-carry.x, -carry.y);
-        }
+        const int part = w.lane / P, first = part * 8 * P + w.cp, me = w.warp - kDataThreads / 32;
+        f32x2 carry = 0;                            // -C after the wave
+        if (a.state_in && w.on)
+            carry = mul2(pack(*reinterpret_cast<const float2 *>(a.state_in + (int64_t)w.row * a.D + w.c)), kMinus);
         auto saved_at = [&](int k) {
             const int t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens + part * kChunk;
             if (k >= w.n || !w.on || t0 < 0 || t0 >= w.len) return make_float2(0.f, 0.f);
             return __ldg(reinterpret_cast<const float2 *>(a.saved + ((int64_t)w.row * a.nchunks + t0 / kChunk) * a.D + w.c));
         };
         bool gave_up = false;
-        float2 next = saved_at(0);
-        for (int k = 0; k < w.n; ++k) {
+        float2 next = saved_at(me);
+        for (int k = me; k < w.n; k += 2) {
             const int par = k & 1;
-            float2 h = next;
-            next = saved_at(k + 1);
+            f32x2 h = pack(next);
+            next = saved_at(k + 2);
             bar_sync(kBarRuns + par);
-            auto reverse_run = [&](int j) {
-                const float2 A = *reinterpret_cast<const float2 *>(&runs[par][first + j * w.P]);
-                const float2 e = ends[par][first + j * w.P];
-                return make_float4(A.x, A.y, e.x, e.y);
-            };
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                states[par][first + j * w.P] = h;
-                h = apply(runs[par][first + j * w.P], h);
-            }
-            float4 f = identity4();
+            auto reverse_run = [&](int j) { return Run{runs[par][first + j * P].A, ends[par][first + j * P]}; };
+            Run f = identity();
 #pragma unroll
             for (int j = 7; j >= 0; --j) f = compose(f, reverse_run(j));
-            const float4 incl = lane_scan<true>(f, w.P, w.lane);
-            const float4 excl = lane_exclusive<true>(incl, w.P, w.lane);
-            const float4 total = shfl4(incl, w.cp);
-            float2 C = carry;
-            if (a.nseg > 1) {
-                float4 pre, all;
-                exchange(total, peers, k, w.seg, a.nseg, w.P, w.cp, gave_up, &pre, &all);
-                C = apply(pre, carry);
-                carry = apply(all, carry);
-            } else {
-                carry = apply(total, carry);
-            }
+            const Run incl = lane_scan<true, P>(f, w.lane), excl = lane_exclusive<true, P>(incl, w.lane);
+            const Run total = P == 32 ? incl : shuffle(incl, w.cp);
+            f32x2 C = carry_over<P>(total, peers, carries, carry, k, w.n, w.seg, a.nseg, w.cp, gave_up);
             C = apply(excl, C);
 #pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                states[par][first + j * P] = h;
+                h = apply(runs[par][first + j * P], h);
+            }
+#pragma unroll
             for (int j = 7; j >= 0; --j) {
-                const float4 r = reverse_run(j);
-                ends[par][first + j * w.P] = C;
+                const Run r = reverse_run(j);
+                ends[par][first + j * P] = C;
                 C = apply(r, C);
             }
             bar_arrive(kBarStates + par);
         }
         close_peers(a.nseg);
-        if (a.state_out && w.on && w.lane < w.P && w.seg == 0)
-            *reinterpret_cast<float2 *>(a.state_out + (int64_t)w.row * a.D + w.c) = make_float2(-carry.x, -carry.y);
+        if (a.state_out && w.on && w.lane < P && w.seg == 0 && me == ((w.n - 1) & 1))
+            *reinterpret_cast<float2 *>(a.state_out + (int64_t)w.row * a.D + w.c) = unpack(mul2(carry, kMinus));
         return;
     }
 
@@ -593,15 +598,14 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_backward(const Sca
             const f32x2 G = fma2(ring.value(st, 2, i), kMinus, R);
             R = fma2(nb[i], G, G);
         }
-        const float2 fa = unpack(A), fh = unpack(H);
-        runs[k & 1][threadIdx.x] = make_float4(fa.x, fa.y, fh.x, fh.y);
-        ends[k & 1][threadIdx.x] = unpack(R);
+        runs[k & 1][threadIdx.x] = {A, H};
+        ends[k & 1][threadIdx.x] = R;
         bar_arrive(kBarRuns + (k & 1));
     };
     auto second = [&](int k, const f32x2 (&nb)[kS]) {
         const int st = k % ST, t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens + w.sc * kS;
         bar_sync(kBarStates + (k & 1));
-        f32x2 h = pack(states[k & 1][threadIdx.x]), C = pack(ends[k & 1][threadIdx.x]);
+        f32x2 h = states[k & 1][threadIdx.x], C = ends[k & 1][threadIdx.x];
         f32x2 v[kS];                                    // h_{t-1} - x or h_{t-1}
 #pragma unroll
         for (int i = 0; i < kS; ++i) {
