@@ -18,8 +18,10 @@
 // to m / eps.  The step itself uses the moments before they are rounded.  A warp's 32 x 8
 // values are one block.
 //
-// The products and sums of m and v are rounded one by one (no contraction), so scales do
-// not depend on how a compiler fuses them.  sqrt and the quotient of the step are the
+// The products and sums of m and v are rounded one by one: an 8-bit m and a bf16 gradient have
+// few bits, so 0.9 m + 0.1 g meets the ties of the 4-bit codes about once in 500 values, and a
+// fused product would decide them (and with them whole steps) otherwise than its definition.
+// Scalar instructions, because mul and add on packed pairs were fused.  sqrt and the quotient of the step are the
 // approximate instructions (2^-22): with the exact sequences the 8-bit step was bound by
 // its instructions (379 us at 120 M values, against 178 us for its bytes).
 #include <cuda_fp8.h>
@@ -215,7 +217,6 @@ __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_ada
         cur.ms = n > 0 ? e.m_scale[at / kBlock] : 0.f;
         cur.vs = n > 0 ? e.v_scale[at / kBlock] : 0.f;
     }
-    const f32x2 b1 = twice(a.beta1), c1 = twice(a.one_minus_beta1), b2 = twice(a.beta2), c2 = twice(a.one_minus_beta2);
     float m[8], v[8], w[8], root[8];
     if constexpr (k8Bit) {
         cur.m.get(m);
@@ -233,12 +234,12 @@ __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_ada
     }
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-        f32x2 gs = pack(make_float2(cur.g[i], cur.g[i + 1]));
-        if (a.grad_scale) gs = mul2(gs, twice(scale));
-        const f32x2 m2 = add2(mul2(b1, pair(m + i)), mul2(c1, gs));
-        const f32x2 v2 = add2(mul2(b2, pair(v + i)), mul2(c2, mul2(gs, gs)));
-        unpair(m2, m + i);
-        unpair(v2, v + i);
+#pragma unroll
+        for (int j = i; j < i + 2; ++j) {
+            const float gs = a.grad_scale ? cur.g[j] * scale : cur.g[j];
+            m[j] = __fadd_rn(__fmul_rn(a.beta1, m[j]), __fmul_rn(a.one_minus_beta1, gs));
+            v[j] = __fadd_rn(__fmul_rn(a.beta2, v[j]), __fmul_rn(a.one_minus_beta2, __fmul_rn(gs, gs)));
+        }
         float r[2];
         asm("sqrt.approx.f32 %0, %1;" : "=f"(root[i]) : "f"(v[i]));
         asm("sqrt.approx.f32 %0, %1;" : "=f"(root[i + 1]) : "f"(v[i + 1]));
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_ada
         asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r[0]));
         asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r[1]));
         const f32x2 old = pack(make_float2(cur.w[i], cur.w[i + 1]));
-        unpair(fma2(twice(-a.step_size), mul2(m2, pair(r)), mul2(old, twice(a.decay))), w + i);
+        unpair(fma2(twice(-a.step_size), mul2(pair(m + i), pair(r)), mul2(old, twice(a.decay))), w + i);
     }
     Eight<P> p;
     p.set(w);
