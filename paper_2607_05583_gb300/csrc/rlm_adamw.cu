@@ -190,6 +190,7 @@ struct Reads {
 // 32-bit step loses by it.
 template <typename P, typename G, bool kMaster, bool k8Bit>
 __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_adamw(const __grid_constant__ StepArgs a) {
+    wait_for_previous();
     // The tensor whose chunks this block's index falls into.
     int lo = 0, hi = a.count - 1;
     while (lo < hi) {
@@ -326,9 +327,7 @@ cudaError_t adamw_step(const rlm_adamw_tensor *tensors, int count, rlm_dtype par
             chunks += (unsigned)c;
         }
         a.first[a.count] = chunks;
-        fn<<<chunks, kThreads, 0, st>>>(a);
-        count_launches(1);
-        const cudaError_t e = cudaGetLastError();
+        const cudaError_t e = launch_dependent(fn, dim3(chunks), kThreads, 0, st, 1, a);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

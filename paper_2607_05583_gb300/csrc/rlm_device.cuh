@@ -50,6 +50,14 @@ __device__ __forceinline__ float2 lambda_pow(float gamma, float omega, float n) 
     return make_float2(r * fmaf(-pe, sp, cp), r * fmaf(pe, cp, sp));
 }
 
+// Programmatic dependent launch: returns once the kernels before this one in the stream have
+// finished, and lets the next one start its own set-up (it waits here in turn).  For kernels
+// launched with launch_dependent().
+__device__ __forceinline__ void wait_for_previous() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // Two fp32 values in one 64-bit register, and the packed arithmetic on them (each half
 // rounded as the scalar operation rounds it).
 using f32x2 = unsigned long long;

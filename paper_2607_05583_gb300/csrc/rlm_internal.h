@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <utility>
+
 #include "../../include/rlm.h"
 
 namespace rlm {
@@ -18,6 +20,28 @@ int sm_count();
 
 // Adds n to the process-wide count of kernels this library has launched.
 void count_launches(int n);
+
+// Launches a kernel that begins with wait_for_previous(): its blocks may start, and set
+// themselves up, while the kernel before it in the stream ends.  cluster > 1: in clusters.
+template <typename... Params, typename... Args>
+cudaError_t launch_dependent(void (*fn)(Params...), dim3 grid, int block, size_t smem, cudaStream_t st, int cluster,
+                             Args &&...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    count_launches(1);
+    return cudaLaunchKernelEx(&cfg, fn, std::forward<Args>(args)...);
+}
 
 // ---- SIMT chunked scan (rlm_simt.cu) --------------------------------------
 // Chunk length the SIMT path uses for a problem; workspace and launch agree.

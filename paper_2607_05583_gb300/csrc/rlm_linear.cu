@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     __syncthreads();
     if (kPair) cluster_sync();
     fence_after();
+    wait_for_previous();
     const uint32_t tmem = *tmem_at;
     const int units = g.tiles_m * g.tiles_n * g.splits;
 
@@ -441,6 +442,7 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
 template <int kTok, int kWarps>
 __global__ void __launch_bounds__(kWarps * 32) k_few(const FewArgs a) {
     __shared__ float part[kWarps][16][8 * kTok + 1];
+    wait_for_previous();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
     const int n0 = blockIdx.x * 16;
     const bf16 *w0 = a.w + (int64_t)min(n0 + g, a.N - 1) * a.w_ld + q * 8;
@@ -505,6 +507,7 @@ struct FinishArgs {
     bf16 *pre;
 };
 __global__ void __launch_bounds__(256) k_finish(const FinishArgs f) {
+    wait_for_previous();
     const int64_t q = f.N / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= f.M * q) return;
     const int64_t row = i / q;
@@ -547,6 +550,7 @@ struct DzArgs {
 template <int kAct>
 __global__ void __launch_bounds__(256) k_dz(const DzArgs a) {
     __shared__ float sums[256 * 8];             // [rows at a time][columns]
+    wait_for_previous();
     const int groups = 1 << a.log2_groups, cg = threadIdx.x & (groups - 1), rl = threadIdx.x >> a.log2_groups;
     const int rows = 256 >> a.log2_groups, cols = groups * 8;
     const int col = blockIdx.y * 256 + cg * 8;
@@ -590,10 +594,13 @@ __global__ void __launch_bounds__(256) k_dz(const DzArgs a) {
 // Column sums of part [n][N]: 32 columns a block, 32 row strides, then a fixed-order sum.
 __global__ void __launch_bounds__(1024) k_column_sum(const float *part, int64_t n, int N, float *out) {
     __shared__ float sums[32][33];
+    wait_for_previous();
     const int c = threadIdx.x & 31, w = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
     float s = 0.f;
-    if (col < N)
+    if (col < N) {
+#pragma unroll 8
         for (int64_t r = w; r < n; r += 32) s += part[r * N + col];
+    }
     sums[w][c] = s;
     __syncthreads();
     if (w == 0 && col < N) {
@@ -705,16 +712,6 @@ cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const Gemm
     static std::atomic<int> ctas[64];               // per device: CTAs that fit, once the kernel is set up
     int dev = 0;
     cudaGetDevice(&dev);
-    cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(kGemmThreads);
-    cfg.dynamicSmemBytes = Cfg::kSmem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kPair ? 2 : 1;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
     int room = ctas[dev & 63].load(std::memory_order_relaxed);
     if (room == 0) {
         cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
@@ -722,17 +719,25 @@ cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const Gemm
         room = sm_count();
         if (kPair) {
             // Pairs sit in one GPC: an odd SM of a GPC stays out.
-            int n = 0;
+            cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(2);
+            cfg.blockDim = dim3(kGemmThreads);
+            cfg.dynamicSmemBytes = Cfg::kSmem;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = 2;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            int n = 0;
             if ((e = cudaOccupancyMaxActiveClusters(&n, fn, &cfg)) != cudaSuccess) return e;
             room = 2 * std::max(n, 1);
         }
         ctas[dev & 63].store(room, std::memory_order_relaxed);
     }
     const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits * (kPair ? 2 : 1);
-    cfg.gridDim = dim3((unsigned)std::min<int64_t>(units, room));
-    count_launches(1);
-    return cudaLaunchKernelEx(&cfg, fn, ma, mb, g);
+    return launch_dependent(fn, dim3((unsigned)std::min<int64_t>(units, room)), kGemmThreads, Cfg::kSmem, st, kPair ? 2 : 1,
+                            ma, mb, g);
 }
 
 template <bool kPair, bool kAMn, bool kBMn, int kBN>
@@ -796,9 +801,7 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
     f.out_ld = ep.out_ld;
     f.pre = static_cast<bf16 *>(ep.pre);
     f.pre_ld = ep.pre_ld;
-    k_finish<<<(unsigned)((M * (N / 4) + 255) / 256), 256, 0, st>>>(f);
-    count_launches(1);
-    return cudaGetLastError();
+    return launch_dependent(k_finish, dim3((unsigned)((M * (N / 4) + 255) / 256)), 256, 0, st, 1, f);
 }
 
 }  // namespace
@@ -814,15 +817,13 @@ bool few_rows(int64_t R, int64_t K, int64_t N) {
 }
 
 template <int kTok>
-void launch_few(const FewArgs &a, cudaStream_t st) {
+cudaError_t launch_few(const FewArgs &a, cudaStream_t st) {
     // Sixteen warps share the contraction, eight where there are three CTAs and more for each SM:
     // 8.8 against 11.5 us (K = N = 4096, 8 rows), 21.1 against 18.2 us (K = 4096, N = 11008).
     const unsigned ctas = (unsigned)((a.N + 15) / 16);
     if (ctas >= 3u * (unsigned)sm_count())
-        k_few<kTok, 8><<<ctas, 8 * 32, 0, st>>>(a);
-    else
-        k_few<kTok, 16><<<ctas, 16 * 32, 0, st>>>(a);
-    count_launches(1);
+        return launch_dependent(k_few<kTok, 8>, dim3(ctas), 8 * 32, 0, st, 1, a);
+    return launch_dependent(k_few<kTok, 16>, dim3(ctas), 16 * 32, 0, st, 1, a);
 }
 
 size_t linear_ws_bytes(int64_t R, int64_t K, int64_t N) {
@@ -848,13 +849,7 @@ cudaError_t linear_forward(const rlm_matrix &x, const rlm_matrix &w, const float
         a.bias = bias;
         a.R = (int)x.rows, a.N = (int)w.rows, a.K = (int)x.cols;
         a.act = act_kind;
-        if (a.R <= 8)
-            launch_few<1>(a, st);
-        else if (a.R <= 16)
-            launch_few<2>(a, st);
-        else
-            launch_few<4>(a, st);
-        return cudaGetLastError();
+        return a.R <= 8 ? launch_few<1>(a, st) : a.R <= 16 ? launch_few<2>(a, st) : launch_few<4>(a, st);
     }
     Epilogue ep;
     ep.bias = bias;
@@ -899,14 +894,12 @@ cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm
                    : act_kind == RLM_ACT_GELU    ? k_dz<RLM_ACT_GELU>
                    : act_kind == RLM_ACT_SIGMOID ? k_dz<RLM_ACT_SIGMOID>
                                                  : k_dz<RLM_ACT_NONE>;
-        fn<<<dim3((unsigned)blocks, (unsigned)((N + 255) / 256)), 256, 0, st>>>(a);
-        count_launches(1);
-        cudaError_t e = cudaGetLastError();
+        cudaError_t e = launch_dependent(fn, dim3((unsigned)blocks, (unsigned)((N + 255) / 256)), 256, 0, st, 1, a);
         if (e != cudaSuccess) return e;
         if (dbias) {
-            k_column_sum<<<(unsigned)((N + 31) / 32), 1024, 0, st>>>(a.part, blocks, (int)N, dbias);
-            count_launches(1);
-            if ((e = cudaGetLastError()) != cudaSuccess) return e;
+            e = launch_dependent(k_column_sum, dim3((unsigned)((N + 31) / 32)), 1024, 0, st, 1,
+                                 static_cast<const float *>(a.part), blocks, (int)N, dbias);
+            if (e != cudaSuccess) return e;
         }
     }
     float *part = reinterpret_cast<float *>(at);

@@ -264,7 +264,6 @@ __device__ __forceinline__ Where where(const ScanArgs<T> &a) {
     w.c = (chain - w.row * a.groups) * 2 * w.P + 2 * w.cp;
     w.on = w.c < a.D;
     w.tile_tokens = (kDataThreads >> kLog2P) * kS;
-    w.len = a.lengths ? min(max(__ldg(a.lengths + w.row), 0), a.L) : a.L;
     w.n = (a.ntiles + a.nseg - 1) / a.nseg;         // waves (in the last one, tiles past the end do nothing)
     return w;
 }
@@ -399,9 +398,11 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_forward(const Scan
     __shared__ Run runs[2][kDataThreads];
     __shared__ f32x2 states[2][kDataThreads], carries[2][32];
     constexpr int P = 1 << kLog2P;
-    const Where w = where<kLog2P>(a);
+    Where w = where<kLog2P>(a);
     constexpr int ST = kFwdStages<T>;
     open_peers(peers, a.nseg);
+    wait_for_previous();
+    w.len = a.lengths ? min(max(__ldg(a.lengths + w.row), 0), a.L) : a.L;
 
     if (w.warp >= kDataThreads / 32) {
         // Runs to states, the two warps in turn: lane (part, cp) holds runs 8 part .. 8 part + 7.
@@ -512,9 +513,11 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_backward(const Sca
     __shared__ f32x2 ends[2][kDataThreads];         // a run's -C from a zero C after it; then its -C
     __shared__ f32x2 states[2][kDataThreads], carries[2][32];
     constexpr int P = 1 << kLog2P;
-    const Where w = where<kLog2P>(a);
+    Where w = where<kLog2P>(a);
     constexpr int ST = kBwdStages<T>;
     open_peers(peers, a.nseg);
+    wait_for_previous();
+    w.len = a.lengths ? min(max(__ldg(a.lengths + w.row), 0), a.L) : a.L;
 
     if (w.warp >= kDataThreads / 32) {
         // A lane's 8 runs are one chunk: their states follow from the chunk's saved state.
@@ -657,7 +660,7 @@ template <typename T, bool kLeak>
 __global__ void __launch_bounds__(256) k_scan_step(const T *x, const T *g, T *y, int64_t x_b, int64_t g_b, int64_t y_b,
                                                    float *state, int half, int64_t n) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_for_previous();
     if (i < n) {
         int64_t row;
         int c;
@@ -677,7 +680,6 @@ __global__ void __launch_bounds__(256) k_scan_step(const T *x, const T *g, T *y,
         *sp = h;
         Pair<T>::store(y + row * y_b + c, h);
     }
-    asm volatile("griddepcontrol.launch_dependents;" :::);
 }
 
 template <typename T>
@@ -784,19 +786,8 @@ cudaError_t launch_scan(bool backward, bool leak, ScanArgs<T> &a, int64_t B, cud
     a.nseg = p.nseg;
     a.ntiles = p.ntiles;
     a.nchunks = (a.L + kChunk - 1) / kChunk;
-    cudaLaunchConfig_t cfg = {};                // resident() has set the kernel's shared memory size
-    cfg.gridDim = dim3((unsigned)(p.chains * p.nseg));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)k.smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.nseg;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    count_launches(1);
-    return cudaLaunchKernelEx(&cfg, k.fn, a);
+    // (resident() has set the kernel's shared memory size.)
+    return launch_dependent(k.fn, dim3((unsigned)(p.chains * p.nseg)), kThreads, (size_t)k.smem, st, p.nseg, a);
 }
 
 template <typename T>
@@ -844,19 +835,9 @@ cudaError_t step_t(const rlm_strided &x, const rlm_strided &g, const rlm_strided
                    cudaStream_t st) {
     const int half = (int)(x.D / 2);
     const int64_t n = x.B * half;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((n + 255) / 256));
-    cfg.blockDim = dim3(256);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    count_launches(1);
-    return cudaLaunchKernelEx(&cfg, leak ? k_scan_step<T, true> : k_scan_step<T, false>, static_cast<const T *>(x.ptr),
-                              static_cast<const T *>(g.ptr), static_cast<T *>(y.ptr), x.stride_b, g.stride_b,
-                              y.stride_b, state, half, n);
+    return launch_dependent(leak ? k_scan_step<T, true> : k_scan_step<T, false>, dim3((unsigned)((n + 255) / 256)), 256, 0, st, 1,
+                            static_cast<const T *>(x.ptr), static_cast<const T *>(g.ptr), static_cast<T *>(y.ptr), x.stride_b,
+                            g.stride_b, y.stride_b, state, half, n);
 }
 
 }  // namespace
