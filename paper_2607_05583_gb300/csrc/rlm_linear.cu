@@ -535,30 +535,29 @@ __global__ void __launch_bounds__(256) k_finish(const FinishArgs f) {
 }
 
 // --------------------------------------------- dz = dy act'(z), and dbias
-// Blocks of kDzRows rows by 256 columns (fewer where N is less, and more rows at a time), a thread
+// Blocks of 128 rows (fewer where that leaves SMs idle) by 256 columns (fewer where N is less, and more rows at a time), a thread
 // per 8 columns.  Bound by
 // its 6 bytes an element (2 without an activation).  The block's column sums go to
 // `part` [row blocks][N], which k_column_sum adds in order.
-constexpr int kDzRows = 128;
 struct DzArgs {
     const bf16 *dy, *pre;
     bf16 *dz;               // (unused without an activation: dy serves)
     float *part;            // nullable (no dbias)
     int64_t R, dy_ld, pre_ld;
-    int N, log2_groups;     // column groups of 8 in a block: at most 32
+    int N, rows, log2_groups;       // rows of a block; column groups of 8 in a block, at most 32
 };
 template <int kAct>
 __global__ void __launch_bounds__(256) k_dz(const DzArgs a) {
     __shared__ float sums[256 * 8];             // [rows at a time][columns]
     wait_for_previous();
     const int groups = 1 << a.log2_groups, cg = threadIdx.x & (groups - 1), rl = threadIdx.x >> a.log2_groups;
-    const int rows = 256 >> a.log2_groups, cols = groups * 8;
+    const int at_once = 256 >> a.log2_groups, cols = groups * 8;
     const int col = blockIdx.y * 256 + cg * 8;
-    const int64_t r0 = (int64_t)blockIdx.x * kDzRows, r1 = min(a.R, r0 + kDzRows);
+    const int64_t r0 = (int64_t)blockIdx.x * a.rows, r1 = min(a.R, r0 + a.rows);
     f32x2 s[4] = {0, 0, 0, 0};
     if (col < a.N) {
 #pragma unroll 4
-        for (int64_t r = r0 + rl; r < r1; r += rows) {
+        for (int64_t r = r0 + rl; r < r1; r += at_once) {
             const uint4 d = __ldg(reinterpret_cast<const uint4 *>(a.dy + r * a.dy_ld + col));
             const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
             f32x2 v[4];
@@ -587,7 +586,7 @@ __global__ void __launch_bounds__(256) k_dz(const DzArgs a) {
     const int c = blockIdx.y * 256 + threadIdx.x;
     if ((int)threadIdx.x < cols && c < a.N) {
         float t = 0.f;
-        for (int w = 0; w < rows; ++w) t += sums[w * cols + threadIdx.x];
+        for (int w = 0; w < at_once; ++w) t += sums[w * cols + threadIdx.x];
         a.part[(int64_t)blockIdx.x * a.N + c] = t;
     }
 }
@@ -830,9 +829,18 @@ size_t linear_ws_bytes(int64_t R, int64_t K, int64_t N) {
     return few_rows(R, K, N) ? 0 : gemm_ws(gemm_plan(R, N, K), R, N);
 }
 
+namespace {
+int dz_rows(int64_t R, int64_t N) {
+    int rows = 128;
+    while (rows > 16 && ((R + rows - 1) / rows) * ((N + 255) / 256) < 4 * sm_count()) rows /= 2;
+    return rows;
+}
+}  // namespace
+
 size_t linear_backward_ws_bytes(int64_t R, int64_t K, int64_t N, int act) {
     const size_t dz = act == RLM_ACT_NONE ? 0 : round256((size_t)R * N * 2);
-    const size_t sums = round256((size_t)((R + kDzRows - 1) / kDzRows) * N * sizeof(float));
+    const int rows = dz_rows(R, N);
+    const size_t sums = round256((size_t)((R + rows - 1) / rows) * N * sizeof(float));
     return dz + sums + std::max(gemm_ws(gemm_plan(R, K, N), R, K), gemm_ws(gemm_plan(N, K, R), N, K));
 }
 
@@ -873,12 +881,16 @@ cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm
     const int64_t R = x.rows, K = x.cols, N = w.rows;
     char *at = static_cast<char *>(ws);
     Operand dz = {dy.ptr, dy.ld};
+    const int rows = dz_rows(R, N);
+    const int64_t blocks = (R + rows - 1) / rows;
+    const float *sums = nullptr;
     if (act_kind != RLM_ACT_NONE || dbias) {
         DzArgs a = {};
         a.dy = static_cast<const bf16 *>(dy.ptr);
         a.dy_ld = dy.ld;
         a.R = R;
         a.N = (int)N;
+        a.rows = rows;
         while (a.log2_groups < 5 && (8 << a.log2_groups) < N) ++a.log2_groups;
         if (act_kind != RLM_ACT_NONE) {
             a.pre = static_cast<const bf16 *>(pre->ptr);
@@ -887,20 +899,14 @@ cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm
             at += round256((size_t)R * N * 2);
             dz = {a.dz, N};
         }
-        const int64_t blocks = (R + kDzRows - 1) / kDzRows;
-        if (dbias) a.part = reinterpret_cast<float *>(at);
+        if (dbias) sums = a.part = reinterpret_cast<float *>(at);
         at += round256((size_t)blocks * N * sizeof(float));
         auto *fn = act_kind == RLM_ACT_SILU      ? k_dz<RLM_ACT_SILU>
                    : act_kind == RLM_ACT_GELU    ? k_dz<RLM_ACT_GELU>
                    : act_kind == RLM_ACT_SIGMOID ? k_dz<RLM_ACT_SIGMOID>
                                                  : k_dz<RLM_ACT_NONE>;
-        cudaError_t e = launch_dependent(fn, dim3((unsigned)blocks, (unsigned)((N + 255) / 256)), 256, 0, st, 1, a);
+        const cudaError_t e = launch_dependent(fn, dim3((unsigned)blocks, (unsigned)((N + 255) / 256)), 256, 0, st, 1, a);
         if (e != cudaSuccess) return e;
-        if (dbias) {
-            e = launch_dependent(k_column_sum, dim3((unsigned)((N + 31) / 32)), 1024, 0, st, 1,
-                                 static_cast<const float *>(a.part), blocks, (int)N, dbias);
-            if (e != cudaSuccess) return e;
-        }
     }
     float *part = reinterpret_cast<float *>(at);
     if (dx) {
@@ -915,8 +921,11 @@ cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm
         ep.out = dw->ptr;
         ep.out_ld = dw->ld;
         ep.out_f32 = dw->dtype == RLM_F32;
-        return gemm<true, true>(dz, {x.ptr, x.ld}, N, K, R, ep, part, st);
+        const cudaError_t e = gemm<true, true>(dz, {x.ptr, x.ld}, N, K, R, ep, part, st);
+        if (e != cudaSuccess) return e;
     }
+    // Last: ahead of the products its few large blocks would hold up the first of them.
+    if (dbias) return launch_dependent(k_column_sum, dim3((unsigned)((N + 31) / 32)), 1024, 0, st, 1, sums, blocks, (int)N, dbias);
     return cudaSuccess;
 }
 
