@@ -40,8 +40,9 @@ namespace {
 constexpr int kBlock = RLM_ADAMW_BLOCK;         // values that share a scale
 constexpr int kThreads = 256;
 // Values of a thread block: 8 a thread.  Several rounds a thread, the next round's loads issued
-// before this one's arithmetic, measured slower: 292 against 217 us for the 8-bit step at
-// 120 M values (four rounds), 491 against 478 us for the fp32 one.
+// before this one's arithmetic or not, measured slower (the blocks at work then spread over more
+// of each buffer): 276 against 227 us for the 8-bit step at 120 M values with two rounds, 491
+// against 478 us for the fp32 one with four.
 constexpr int kChunk = 8 * kThreads;
 constexpr int kMaxTensors = 400;
 
@@ -156,10 +157,10 @@ __device__ __forceinline__ void store8(void *p, int n, const V &v) {
 
 // The bits of the largest magnitude among the warp's values.
 __device__ __forceinline__ unsigned block_top(const float (&v)[8]) {
-    unsigned top = 0;
+    float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-    return __reduce_max_sync(~0u, top);
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[i]));
+    return __reduce_max_sync(~0u, __float_as_uint(top));
 }
 // e of the block scale 2^(e - 8): the least e with top < 2^e, at least -100 (so both
 // 2^(e - 8) and its inverse are normal).
@@ -186,7 +187,7 @@ struct Reads {
 };
 
 // The 8-bit step has more arithmetic to hide its loads behind, so its registers are held down
-// for more warps: 304 -> 274 us (fp32 weights) and 331 -> 308 us (masters) at 120 M values; the
+// for more warps: 304 -> 276 us (fp32 weights) and 331 -> 290 us (masters) at 120 M values; the
 // 32-bit step loses by it.
 template <typename P, typename G, bool kMaster, bool k8Bit>
 __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_adamw(const __grid_constant__ StepArgs a) {

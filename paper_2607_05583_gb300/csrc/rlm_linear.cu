@@ -844,7 +844,7 @@ size_t linear_ws_bytes(int64_t R, int64_t K, int64_t N) {
 namespace {
 int dz_rows(int64_t R, int64_t N) {
     int rows = 128;
-    while (rows > 16 && ((R + rows - 1) / rows) * ((N + 255) / 256) < 4 * sm_count()) rows /= 2;
+    while (rows > 16 && ((R + rows - 1) / rows) * ((N + 255) / 256) < 8 * sm_count()) rows /= 2;
     return rows;
 }
 }  // namespace
