@@ -369,7 +369,7 @@ def _opt(t: torch.Tensor | None, dtype, shape, name: str):
     """Pointer of an optional contiguous CUDA tensor of a fixed shape (None: NULL)."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of shape {tuple(shape)}, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")
     return t.data_ptr()

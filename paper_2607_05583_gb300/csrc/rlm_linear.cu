@@ -667,7 +667,7 @@ struct TileKind {
 };
 constexpr TileKind kTiles[] = {{true, 256, 5.7, 0.285, 1.9}, {true, 128, 5.1, 0.17, 1.2}, {false, 128, 4.0, 0.19, 1.0}};
 
-GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K) {
+GemmPlan find_plan(int64_t M, int64_t N, int64_t K) {
     GemmPlan best = {};
     double best_cost = 0;
     const int sms = sm_count();
@@ -693,6 +693,21 @@ GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K) {
         }
     }
     return best;
+}
+
+// A program's few shapes come again and again: their plans are kept (they depend on the shape and
+// the device's SM count alone).
+GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K) {
+    struct Kept {
+        int64_t M, N, K;
+        int sms;
+        GemmPlan plan;
+    };
+    static thread_local Kept kept[32] = {};
+    const int sms = sm_count();
+    Kept &k = kept[(unsigned)(M * 31 + N * 17 + K / 8 * 5 + M / 64) % 32];
+    if (k.M != M || k.N != N || k.K != K || k.sms != sms) k = {M, N, K, sms, find_plan(M, N, K)};
+    return k.plan;
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }

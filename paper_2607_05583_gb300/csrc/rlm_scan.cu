@@ -41,8 +41,7 @@
 // no field is read twice.  Every wait is bounded.  The order of all products and sums is
 // fixed by the shape: results repeat bit for bit.
 #include <algorithm>
-#include <mutex>
-#include <vector>
+#include <atomic>
 
 #include "rlm_device.cuh"
 #include "rlm_internal.h"
@@ -711,22 +710,12 @@ struct ScanPlan {
 };
 
 // Resident CTAs of a kernel on the current device in clusters of nseg (a cluster's CTAs
-// sit in one GPC, so large ones do not fill every SM).  Asked once for each kernel.
+// sit in one GPC, so large ones do not fill every SM).  Asked once for each kernel, whose shared
+// memory size it sets.
 template <typename T>
-int64_t resident(const ScanKernel<T> &k, int nseg) {
-    struct Key {
-        const void *fn;
-        int dev, nseg;
-        int64_t ctas;
-    };
-    static std::mutex mu;
-    static std::vector<Key> known;
-    int dev = 0;
-    cudaGetDevice(&dev);
-    const void *fn = reinterpret_cast<const void *>(k.fn);
-    std::lock_guard<std::mutex> lock(mu);
-    for (const Key &e : known)
-        if (e.fn == fn && e.dev == dev && e.nseg == nseg) return e.ctas;
+int64_t resident(const ScanKernel<T> &k, int nseg, std::atomic<int> &known) {
+    const int ctas = known.load(std::memory_order_relaxed);
+    if (ctas > 0) return ctas;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)nseg);
     cfg.blockDim = dim3(kThreads);
@@ -741,9 +730,9 @@ int64_t resident(const ScanKernel<T> &k, int nseg) {
     if (cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) != cudaSuccess ||
         cudaOccupancyMaxActiveClusters(&n, k.fn, &cfg) != cudaSuccess) {
         cudaGetLastError();
-        n = 0;
+        return 0;
     }
-    known.push_back({fn, dev, nseg, (int64_t)n * nseg});
+    known.store(n * nseg, std::memory_order_relaxed);
     return (int64_t)n * nseg;
 }
 
@@ -751,6 +740,9 @@ int64_t resident(const ScanKernel<T> &k, int nseg) {
 // a CTA's waves, with a few waves' worth for its start and end.
 template <typename T>
 ScanPlan scan_plan(int64_t B, int64_t L, int D, bool backward, bool leak) {
+    static std::atomic<int> known[64][2][2][4][4];          // resident CTAs: device, direction, leak, pairs, segments
+    int dev = 0;
+    cudaGetDevice(&dev);
     ScanPlan best = {};
     double best_cost = 0;
     for (int lp = 5; lp >= 2; --lp) {
@@ -762,8 +754,9 @@ ScanPlan scan_plan(int64_t B, int64_t L, int D, bool backward, bool leak) {
         p.chains = B * p.groups;
         const int tile = (kDataThreads >> lp) * kS;
         p.ntiles = (int)((L + tile - 1) / tile);
-        for (p.nseg = 1; p.nseg <= kMaxSeg && p.nseg <= p.ntiles; p.nseg *= 2) {
-            const int64_t room = resident(k, p.nseg);
+        int at = 0;
+        for (p.nseg = 1; p.nseg <= kMaxSeg && p.nseg <= p.ntiles; p.nseg *= 2, ++at) {
+            const int64_t room = resident(k, p.nseg, known[dev & 63][backward][leak][lp - 2][at]);
             if (room < 1) continue;
             const int64_t rounds = (p.chains * p.nseg + room - 1) / room;
             const int waves = (p.ntiles + p.nseg - 1) / p.nseg;
