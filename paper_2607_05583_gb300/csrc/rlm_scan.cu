@@ -388,23 +388,29 @@ __device__ __forceinline__ void two_passes(int n, First first, Second second) {
 
 // Resident CTAs per SM: what the rings leave room for.
 template <typename T>
-constexpr int kPerSm = sizeof(T) == 2 ? 2 : 1;
+constexpr int kBwdPerSm = sizeof(T) == 2 ? 2 : 1;
 
 // ----------------------------------------------------------------- forward
+// Tiles of x (needed until the second pass) and of g (until the first) in the ring.
 template <typename T>
-constexpr int kFwdStages = sizeof(T) == 2 ? 4 : 5;
+constexpr int kXStages = sizeof(T) == 2 ? 4 : 3;
+template <typename T>
+constexpr int kGStages = sizeof(T) == 2 ? 4 : 2;
 template <typename T, int kLog2P>
-using FwdRing = Ring<T, 2, kFwdStages<T>, kLog2P>;          // fields: x, g
+using XRing = Ring<T, 1, kXStages<T>, kLog2P>;
+template <typename T, int kLog2P>
+using GRing = Ring<T, 1, kGStages<T>, kLog2P>;
 
 template <typename T, bool kLeak, int kLog2P>
-__global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_forward(const ScanArgs<T> a) {
+__global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> a) {
     extern __shared__ __align__(16) unsigned char ring_mem[];
     __shared__ Peers<1 << kLog2P> peers;
     __shared__ Run runs[2][kDataThreads];
     __shared__ f32x2 states[2][kDataThreads], carries[2][32];
     constexpr int P = 1 << kLog2P;
     Where w = where<kLog2P>(a);
-    constexpr int ST = kFwdStages<T>;
+    constexpr int X = kXStages<T>, G = kGStages<T>;
+    static_assert(G <= X, "g leaves the ring first");
     open_peers(peers, a.nseg);
     wait_for_previous();
     w.len = a.lengths ? min(max(__ldg(a.lengths + w.row), 0), a.L) : a.L;
@@ -442,26 +448,28 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_forward(const Scan
         return;
     }
 
-    const FwdRing<T, kLog2P> ring(w, ring_mem);
-    const bool on = ring.c < a.D;
-    const T *xp = a.x + w.row * a.x_b + (on ? ring.c : 0), *gp = a.g + w.row * a.g_b + (on ? ring.c : 0);
+    const XRing<T, kLog2P> xs(w, ring_mem);
+    const GRing<T, kLog2P> gs(w, ring_mem + XRing<T, kLog2P>::kBytes);
+    const bool on = xs.c < a.D;
+    const T *xp = a.x + w.row * a.x_b + (on ? xs.c : 0), *gp = a.g + w.row * a.g_b + (on ? xs.c : 0);
     T *yp = a.y + w.row * a.y_b + w.c;
     auto copy = [&](int k) {
         if (k < w.n) {
             const int t0 = (k * a.nseg + w.seg) * w.tile_tokens;
-            ring.copy(k % ST, 0, xp, a.x_l, t0, w.tile_tokens, w.len, on);
-            ring.copy(k % ST, 1, gp, a.g_l, t0, w.tile_tokens, w.len, on);
+            xs.copy(k % X, 0, xp, a.x_l, t0, w.tile_tokens, w.len, on);
+            gs.copy(k % G, 0, gp, a.g_l, t0, w.tile_tokens, w.len, on);
         }
         copies_commit();
     };
 #pragma unroll
-    for (int k = 0; k < ST; ++k) copy(k);
+    for (int k = 0; k < G; ++k) copy(k);
     auto first = [&](int k, f32x2 (&nb)[kS]) {
-        // Copies are one group a tile: tile k is in once at most the groups after it are open.
-        if (k == 0) copies_wait<ST - 1>(); else copies_wait<ST - 2>();
-        const int st = k % ST, t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
+        // Copies are one group a tile: tile k is in once at most the groups after it are open.  Tile q + X
+        // is asked for after second(q); G tiles at the start and, where G < X, one more after first(0).
+        if (k == 0) copies_wait<G - 1>(); else if (k == 1) copies_wait<G + (G < X) - 2>(); else copies_wait<X - 2>();
+        const int t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
 #pragma unroll
-        for (int i = 0; i < kS; ++i) nb[i] = minus_rest<T>(ring.value(st, 1, i));
+        for (int i = 0; i < kS; ++i) nb[i] = minus_rest<T>(gs.value(k % G, 0, i));
         if (t0 + kS > w.len) {                          // past the end: the identity (x is 0 there)
 #pragma unroll
             for (int i = 0; i < kS; ++i)
@@ -471,33 +479,37 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_forward(const Scan
 #pragma unroll
         for (int i = 0; i < kS; ++i) {
             A = fma2(nb[i], A, A);
-            H = advance<kLeak>(H, nb[i], ring.value(st, 0, i));
+            H = advance<kLeak>(H, nb[i], xs.value(k % X, 0, i));
         }
         runs[k & 1][threadIdx.x] = {A, H};
         bar_arrive(kBarRuns + (k & 1));
+        if (G < X && k == 0) {
+            __syncwarp();
+            copy(G);
+        }
     };
     auto second = [&](int k, const f32x2 (&nb)[kS]) {
-        const int st = k % ST, t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
+        const int t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
         bar_sync(kBarStates + (k & 1));
         f32x2 h = states[k & 1][threadIdx.x];
         T *out = yp + (int64_t)t0 * a.y_l;
         if (w.on && t0 + kS <= w.len) {
 #pragma unroll
             for (int i = 0; i < kS; ++i) {
-                h = advance<kLeak>(h, nb[i], ring.value(st, 0, i));
+                h = advance<kLeak>(h, nb[i], xs.value(k % X, 0, i));
                 Pair<T>::store(out, unpack(h));
                 out += a.y_l;
             }
         } else if (w.on) {
 #pragma unroll
             for (int i = 0; i < kS; ++i) {
-                h = advance<kLeak>(h, nb[i], ring.value(st, 0, i));
+                h = advance<kLeak>(h, nb[i], xs.value(k % X, 0, i));
                 if (t0 + i < a.L) Pair<T>::store(out, t0 + i < w.len ? unpack(h) : make_float2(0.f, 0.f));
                 out += a.y_l;
             }
         }
         __syncwarp();
-        copy(k + ST);           // into the stage that this pass has just left
+        copy(k + X);            // x into the stage that this pass has just left
     };
     two_passes(w.n, first, second);
     close_peers(a.nseg);
@@ -510,7 +522,7 @@ template <typename T, int kLog2P>
 using BwdRing = Ring<T, 3, kBwdStages<T>, kLog2P>;          // fields: x, g, dy
 
 template <typename T, bool kLeak, int kLog2P>
-__global__ void __launch_bounds__(kThreads, kPerSm<T>) k_scan_backward(const ScanArgs<T> a) {
+__global__ void __launch_bounds__(kThreads, kBwdPerSm<T>) k_scan_backward(const ScanArgs<T> a) {
     extern __shared__ __align__(16) unsigned char ring_mem[];
     // Gradients are carried negated: with -b at hand, b G = (-b)(-G) needs no sign.
     __shared__ Peers<1 << kLog2P> peers;
@@ -695,7 +707,7 @@ struct ScanKernel {
 template <typename T, bool kLeak, int kLog2P>
 ScanKernel<T> kernel_of(bool backward) {
     if (backward) return {k_scan_backward<T, kLeak, kLog2P>, BwdRing<T, kLog2P>::kBytes};
-    return {k_scan_forward<T, kLeak, kLog2P>, FwdRing<T, kLog2P>::kBytes};
+    return {k_scan_forward<T, kLeak, kLog2P>, XRing<T, kLog2P>::kBytes + GRing<T, kLog2P>::kBytes};
 }
 template <typename T, bool kLeak>
 ScanKernel<T> kernel_of(bool backward, int log2p) {
