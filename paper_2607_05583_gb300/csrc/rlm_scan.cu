@@ -61,7 +61,7 @@ namespace {
 constexpr int kDataThreads = 256;
 constexpr int kThreads = kDataThreads + 64;         // and the two warps that turn runs into states
 constexpr int kS = 8;                               // tokens of a run
-constexpr int kBarRuns = 1, kBarStates = 3, kBarCarry = 5;      // named barriers, two of each by tile parity
+constexpr int kBarRuns = 1, kBarStates = 4, kBarCarry = 7;      // named barriers: up to three by tile, three, two by parity
 constexpr int kHandOver = kDataThreads + 32;        // threads of the first two: the data warps and one state warp
 constexpr int kChunk = RLM_SCAN_CHUNK;              // tokens between saved states
 constexpr long long kWaitLimit = 4000000000ll;      // SM cycles: about 2 s
@@ -386,16 +386,39 @@ __device__ __forceinline__ void two_passes(int n, First first, Second second) {
     }
 }
 
+// The same with a lag of two tiles, for the forward pass in bf16 (its registers and ring have room;
+// 3 to 5 % where a cluster shares a chain).
+template <typename First, typename Second>
+__device__ __forceinline__ void three_passes(int n, First first, Second second) {
+    f32x2 n0[kS], n1[kS], n2[kS];
+    first(0, n0);
+    if (n > 1) first(1, n1);
+    for (int k = 2;; k += 3) {
+        if (k < n) first(k, n2);
+        second(k - 2, n0);
+        if (k - 1 >= n) return;
+        if (k + 1 < n) first(k + 1, n0);
+        second(k - 1, n1);
+        if (k >= n) return;
+        if (k + 2 < n) first(k + 2, n1);
+        second(k, n2);
+        if (k + 1 >= n) return;
+    }
+}
+
 // Resident CTAs per SM: what the rings leave room for.
 template <typename T>
 constexpr int kBwdPerSm = sizeof(T) == 2 ? 2 : 1;
 
 // ----------------------------------------------------------------- forward
-// Tiles of x (needed until the second pass) and of g (until the first) in the ring.
+// Tiles between a tile's first and second pass, and tiles of g (needed until the first) and of x
+// (until the second) in the ring.
 template <typename T>
-constexpr int kXStages = sizeof(T) == 2 ? 4 : 3;
+constexpr int kLag = sizeof(T) == 2 ? 2 : 1;
 template <typename T>
-constexpr int kGStages = sizeof(T) == 2 ? 4 : 2;
+constexpr int kGStages = sizeof(T) == 2 ? 3 : 2;
+template <typename T>
+constexpr int kXStages = kGStages<T> + kLag<T>;
 template <typename T, int kLog2P>
 using XRing = Ring<T, 1, kXStages<T>, kLog2P>;
 template <typename T, int kLog2P>
@@ -405,12 +428,11 @@ template <typename T, bool kLeak, int kLog2P>
 __global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> a) {
     extern __shared__ __align__(16) unsigned char ring_mem[];
     __shared__ Peers<1 << kLog2P> peers;
-    __shared__ Run runs[2][kDataThreads];
-    __shared__ f32x2 states[2][kDataThreads], carries[2][32];
+    constexpr int X = kXStages<T>, G = kGStages<T>, NB = kLag<T> + 1;
+    __shared__ Run runs[NB][kDataThreads];
+    __shared__ f32x2 states[NB][kDataThreads], carries[2][32];
     constexpr int P = 1 << kLog2P;
     Where w = where<kLog2P>(a);
-    constexpr int X = kXStages<T>, G = kGStages<T>;
-    static_assert(G <= X, "g leaves the ring first");
     open_peers(peers, a.nseg);
     wait_for_previous();
     w.len = a.lengths ? min(max(__ldg(a.lengths + w.row), 0), a.L) : a.L;
@@ -422,7 +444,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> 
         if (a.state_in && w.on) carry = pack(*reinterpret_cast<const float2 *>(a.state_in + (int64_t)w.row * a.D + w.c));
         bool gave_up = false;
         for (int k = me; k < w.n; k += 2) {
-            const int par = k & 1, tile = k * a.nseg + w.seg;
+            const int par = k % NB, tile = k * a.nseg + w.seg;
             bar_sync(kBarRuns + par);
             Run f = identity();
 #pragma unroll
@@ -464,9 +486,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> 
 #pragma unroll
     for (int k = 0; k < G; ++k) copy(k);
     auto first = [&](int k, f32x2 (&nb)[kS]) {
-        // Copies are one group a tile: tile k is in once at most the groups after it are open.  Tile q + X
-        // is asked for after second(q); G tiles at the start and, where G < X, one more after first(0).
-        if (k == 0) copies_wait<G - 1>(); else if (k == 1) copies_wait<G + (G < X) - 2>(); else copies_wait<X - 2>();
+        // Copies are one group a tile, asked for G at the start, one after each of the first kLag first
+        // passes and then one after each second pass: always G are open or to come, tile k the first.
+        copies_wait<G - 1>();
         const int t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
 #pragma unroll
         for (int i = 0; i < kS; ++i) nb[i] = minus_rest<T>(gs.value(k % G, 0, i));
@@ -481,17 +503,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> 
             A = fma2(nb[i], A, A);
             H = advance<kLeak>(H, nb[i], xs.value(k % X, 0, i));
         }
-        runs[k & 1][threadIdx.x] = {A, H};
-        bar_arrive(kBarRuns + (k & 1));
-        if (G < X && k == 0) {
+        runs[k % NB][threadIdx.x] = {A, H};
+        bar_arrive(kBarRuns + k % NB);
+        if (k < kLag<T>) {
             __syncwarp();
-            copy(G);
+            copy(G + k);
         }
     };
     auto second = [&](int k, const f32x2 (&nb)[kS]) {
         const int t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
-        bar_sync(kBarStates + (k & 1));
-        f32x2 h = states[k & 1][threadIdx.x];
+        bar_sync(kBarStates + k % NB);
+        f32x2 h = states[k % NB][threadIdx.x];
         T *out = yp + (int64_t)t0 * a.y_l;
         if (w.on && t0 + kS <= w.len) {
 #pragma unroll
@@ -511,7 +533,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> 
         __syncwarp();
         copy(k + X);            // x into the stage that this pass has just left
     };
-    two_passes(w.n, first, second);
+    if constexpr (kLag<T> == 2) three_passes(w.n, first, second); else two_passes(w.n, first, second);
     close_peers(a.nseg);
 }
 
