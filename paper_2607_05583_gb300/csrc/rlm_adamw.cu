@@ -8,7 +8,7 @@
 // values; a block takes one chunk, found by bisection in the tensors' running chunk counts.
 // The tensors' pointers travel in the kernel's parameters (up to kMaxTensors a launch), so
 // a step copies nothing to the device first.  A thread holds 8 values in registers, moved
-// by 16-byte accesses; tensors whose pointers or ends do not allow that go value by value.
+// by 16-byte accesses; tensors whose pointers do not allow that, and ends, go value by value.
 //
 // 8-bit moments.  Blocks of 256 values share a power-of-two scale 2^(e - 8), 2^e the first
 // power of two above the block's largest magnitude, so scaling is exact; the values are
@@ -24,7 +24,7 @@
 // Scalar instructions, because mul and add on packed pairs were fused.  sqrt and the
 // quotient of the step are the approximate instructions (2^-22): with the exact sequences
 // the 8-bit step, which its instructions bound (78 % of issue slots), took 379 us at 120 M
-// values against 227 us now and 178 us for its bytes.  The 32-bit steps run at the copy
+// values against 211 us now and 178 us for its bytes.  The 32-bit steps run at the copy
 // rate: 478 us for 3.36 GB (fp32, and bf16 with masters), 7.0 TB/s.
 #include <cuda_fp8.h>
 
@@ -43,7 +43,7 @@ constexpr int kBlock = RLM_ADAMW_BLOCK;         // values that share a scale
 constexpr int kThreads = 256;
 // Values of a thread block: 8 a thread.  Several rounds a thread, the next round's loads issued
 // before this one's arithmetic or not, measured slower (the blocks at work then spread over more
-// of each buffer): 276 against 227 us for the 8-bit step at 120 M values with two rounds, 491
+// of each buffer): 276 against 227 us for the 8-bit step (as it was then) at 120 M values with two rounds, 491
 // against 478 us for the fp32 one with four.
 constexpr int kChunk = 8 * kThreads;
 constexpr int kMaxTensors = 400;
@@ -53,6 +53,7 @@ struct Entry {
     float *master;          // nullable
     float *m_scale, *v_scale;
     int64_t n;
+    int wide;               // every buffer allows 16-byte (codes: 8-byte) accesses
 };
 struct StepArgs {
     const float *grad_scale;        // nullable
@@ -106,12 +107,12 @@ struct Codes {
     }
 };
 // The first n (at most 8) values at p, the others zero: 16-byte (codes: 8-byte) accesses where
-// all eight are there and p allows it, else value by value.  E: bytes of a value.
+// `wide`, else value by value.  E: bytes of a value.
 template <typename V, int E>
-__device__ __forceinline__ V load8(const void *p, int n) {
+__device__ __forceinline__ V load8(const void *p, int n, bool wide) {
     V v;
     constexpr int kBytes = 4 * V::kWords, kWide = kBytes < 16 ? kBytes : 16;
-    if (n == 8 && (reinterpret_cast<uintptr_t>(p) & (kWide - 1)) == 0) {
+    if (wide) {
 #pragma unroll
         for (int i = 0; i < kBytes / kWide; ++i) {
             if constexpr (kWide == 16) {
@@ -136,9 +137,9 @@ __device__ __forceinline__ V load8(const void *p, int n) {
     return v;
 }
 template <typename V, int E>
-__device__ __forceinline__ void store8(void *p, int n, const V &v) {
+__device__ __forceinline__ void store8(void *p, int n, bool wide, const V &v) {
     constexpr int kBytes = 4 * V::kWords, kWide = kBytes < 16 ? kBytes : 16;
-    if (n == 8 && (reinterpret_cast<uintptr_t>(p) & (kWide - 1)) == 0) {
+    if (wide) {
 #pragma unroll
         for (int i = 0; i < kBytes / kWide; ++i) {
             if constexpr (kWide == 16)
@@ -189,17 +190,23 @@ struct Reads {
 };
 
 // The 8-bit step has more arithmetic to hide its loads behind, so its registers are held down
-// for more warps: 304 -> 276 us (fp32 weights) and 331 -> 290 us (masters) at 120 M values; the
-// 32-bit step loses by it.
+// for more warps: 246 -> 211 us (bf16 weights), 291 -> 276 us (fp32) and 297 -> 281 us (masters) at 120 M
+// values; the 32-bit step loses by it.
 template <typename P, typename G, bool kMaster, bool k8Bit>
 __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_adamw(const __grid_constant__ StepArgs a) {
     wait_for_previous();
-    // The tensor whose chunks this block's index falls into.
-    int lo = 0, hi = a.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.first[mid] <= blockIdx.x) lo = mid; else hi = mid - 1;
+    // The tensor whose chunks this block's index falls into: found by one warp for all.
+    __shared__ int tensor;
+    if (threadIdx.x < 32) {
+        int lo = 0, hi = a.count - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (a.first[mid] <= blockIdx.x) lo = mid; else hi = mid - 1;
+        }
+        if (threadIdx.x == 0) tensor = lo;
     }
+    __syncthreads();
+    const int lo = __shfl_sync(~0u, tensor, 0);
     const Entry &e = a.t[lo];
     const int64_t at = (int64_t)(blockIdx.x - a.first[lo]) * kChunk + threadIdx.x * 8;
     float scale = 1.f;
@@ -211,12 +218,13 @@ __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_ada
     using R = Reads<P, G, kMaster, k8Bit>;
     auto bytes = [](void *p, int64_t at, int size) { return static_cast<char *>(p) + at * size; };
     const int n = (int)min((int64_t)8, max((int64_t)0, e.n - at));
+    const bool wide = e.wide && n == 8;
     R cur;
-    cur.g = load8<Eight<G>, sizeof(G)>(bytes(e.g, at, sizeof(G)), n);
-    if constexpr (kMaster) cur.w = load8<typename R::W, 4>(e.master + at, n);
-    else cur.w = load8<typename R::W, sizeof(P)>(bytes(e.p, at, sizeof(P)), n);
-    cur.m = load8<typename R::M, kMoment>(bytes(e.m, at, kMoment), n);
-    cur.v = load8<typename R::M, kMoment>(bytes(e.v, at, kMoment), n);
+    cur.g = load8<Eight<G>, sizeof(G)>(bytes(e.g, at, sizeof(G)), n, wide);
+    if constexpr (kMaster) cur.w = load8<typename R::W, 4>(e.master + at, n, wide);
+    else cur.w = load8<typename R::W, sizeof(P)>(bytes(e.p, at, sizeof(P)), n, wide);
+    cur.m = load8<typename R::M, kMoment>(bytes(e.m, at, kMoment), n, wide);
+    cur.v = load8<typename R::M, kMoment>(bytes(e.v, at, kMoment), n, wide);
     if constexpr (k8Bit) {
         cur.ms = n > 0 ? e.m_scale[at / kBlock] : 0.f;
         cur.vs = n > 0 ? e.v_scale[at / kBlock] : 0.f;
@@ -255,11 +263,11 @@ __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_ada
     }
     Eight<P> p;
     p.set(w);
-    store8<Eight<P>, sizeof(P)>(bytes(e.p, at, sizeof(P)), n, p);
+    store8<Eight<P>, sizeof(P)>(bytes(e.p, at, sizeof(P)), n, wide, p);
     if constexpr (kMaster) {
         Eight<float> q;
         q.set(w);
-        store8<Eight<float>, 4>(e.master + at, n, q);
+        store8<Eight<float>, 4>(e.master + at, n, wide, q);
     }
     typename R::M mo, vo;
     if constexpr (k8Bit) {
@@ -283,8 +291,8 @@ __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_ada
         mo.set(m);
         vo.set(v);
     }
-    store8<typename R::M, kMoment>(bytes(e.m, at, kMoment), n, mo);
-    store8<typename R::M, kMoment>(bytes(e.v, at, kMoment), n, vo);
+    store8<typename R::M, kMoment>(bytes(e.m, at, kMoment), n, wide, mo);
+    store8<typename R::M, kMoment>(bytes(e.v, at, kMoment), n, wide, vo);
 }
 
 using StepKernel = void (*)(const StepArgs);
@@ -324,8 +332,12 @@ cudaError_t adamw_step(const rlm_adamw_tensor *tensors, int count, rlm_dtype par
             const int64_t c = (t.n + kChunk - 1) / kChunk;
             if (a.count > 0 && c > (int64_t)0x7fffffff - chunks) break;     // the grid's limit
             a.first[a.count] = chunks;
+            const uintptr_t all = reinterpret_cast<uintptr_t>(t.param) | reinterpret_cast<uintptr_t>(t.grad) |
+                                  reinterpret_cast<uintptr_t>(t.master);
+            const uintptr_t moments = reinterpret_cast<uintptr_t>(t.exp_avg) | reinterpret_cast<uintptr_t>(t.exp_avg_sq);
+            const bool wide = (all & 15) == 0 && (moments & (bits == 8 ? 7 : 15)) == 0;
             a.t[a.count] = {t.param, const_cast<void *>(t.grad), t.exp_avg, t.exp_avg_sq, t.master, t.exp_avg_scale,
-                            t.exp_avg_sq_scale, t.n};
+                            t.exp_avg_sq_scale, t.n, wide};
             ++a.count;
             chunks += (unsigned)c;
         }
