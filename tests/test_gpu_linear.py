@@ -195,3 +195,22 @@ def test_gradients_against_differences(act):
             want[i] = (up - loss(*v)) / 2e-6
         # pre's own rounding moves act' by at most 2^-8 |z| |act''| (below 2^-8 here) beside dz's and the result's.
         near(got, want, 3 * B16, act)
+
+
+def test_offsets_past_2_31_elements():
+    """Rows of y (and of dy, dx) beyond 2^31 elements, against the same rows by themselves."""
+    R, K, N = 530000, 8, 4104
+    if torch.cuda.mem_get_info()[0] < 3 * 2 * R * N:
+        pytest.skip("no room for fields of 2^31 elements")
+    x = torch.randn(R, K, device="cuda").bfloat16()
+    w = torch.randn(N, K, device="cuda").bfloat16()
+    y = torch.empty(R, N, dtype=torch.bfloat16, device="cuda")
+    rlm.rlm_linear(x, w, y, act="silu")
+    tail = torch.empty(300, N, dtype=torch.bfloat16, device="cuda")
+    rlm.rlm_linear(x[-300:], w, tail, act="silu")
+    assert torch.equal(y[-300:], tail)
+    dx, part = torch.empty_like(x), torch.empty(300, K, dtype=torch.bfloat16, device="cuda")
+    rlm.rlm_linear_backward(y, x, w, dx=dx)
+    rlm.rlm_linear_backward(y[-300:], x[-300:], w, dx=part)
+    near(dx[-300:], y[-300:].double() @ w.double(), B16, "dx")
+    near(part, y[-300:].double() @ w.double(), B16, "dx of the tail")

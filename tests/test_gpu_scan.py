@@ -233,3 +233,16 @@ def test_long_strides():
     rlm.rlm_scan_prefill(x, g, y)
     rlm.rlm_scan_prefill(at, g, z)
     assert torch.equal(y, z)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_inputs_shared_by_the_batch(dtype):
+    """A batch stride of zero: every row reads the same drive (or gate)."""
+    (x, g, dy), _ = fields(3, 150, 64, dtype, 12)
+    one = x[:1].expand(3, -1, -1)
+    want = run(one.contiguous(), g, dy, True, None, None, None)
+    got = run(one, g, dy, True, None, None, None)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    got = run(x, g[:1].expand(3, -1, -1), dy, True, None, None, None)
+    want = run(x, g[:1].expand(3, -1, -1).contiguous(), dy, True, None, None, None)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
