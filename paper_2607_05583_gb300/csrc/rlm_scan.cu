@@ -27,8 +27,11 @@
 // Two more warps turn runs into states, a tile each in turn.  A lane holds one channel
 // pair of 8 consecutive runs (64 tokens, one saved chunk): it composes them, scans across
 // lanes, adds the carry (which one warp hands the other) and gives every run its start
-// state.  The data warps work on the next tile's first pass meanwhile: the second pass of
-// tile w follows the first pass of tile w + 1.  (One such warp took 3100 cycles a tile where
+// state.  The data warps work on other tiles meanwhile: the second pass of tile w follows
+// the first pass of tile w + 1, in the bf16 forward pass that of w + 2 (46 -> 44 us at B = 4,
+// L = 32768, D = 256; fp32 and the backward pass have no room for its rings).  x, needed
+// again then, and g, needed once, have rings of their own: two CTAs per SM in fp32 (73 -> 66
+// us).  (One such warp took 3100 cycles a tile where
 // a cluster shares a chain, half of them the exchange, and bounded the kernel: 54 us at
 // B = 4, L = 32768, D = 256.)
 //
@@ -41,11 +44,11 @@
 // no field is read twice.  Every wait is bounded.  The order of all products and sums is
 // fixed by the shape: results repeat bit for bit.
 //
-// Measured (bf16): B = 256, L = 512, D = 512, no segments, forward 68 us and backward 107 us,
-// 88 and 93 % of the copy rate; B = 4, L = 32768, D = 512, 8 segments, 82 and 129 us (73 and
-// 77 %).  With segments the data warps' own latency bounds a wave (40 % of issue slots, a third
-// of the stalls at the hand-over); a lag of two tiles in place of one gained 3 % and its rings
-// leave room for one CTA per SM at P = 32.
+// Measured, forward and backward: bf16, B = 256, L = 512, D = 512, no segments, 68 and 107
+// us, 88 and 93 % of the copy rate; bf16, B = 4, L = 32768, 8 segments, 81 and 129 us with D =
+// 512 (73 and 77 %), 44 and 73 us with D = 256; fp32, D = 256, 66 and 110 us (90 %).  With
+// segments the data warps' own latency bounds a wave (40 % of issue slots, a third of the
+// stalls at the hand-over).
 #include <algorithm>
 #include <atomic>
 
@@ -776,10 +779,16 @@ int64_t resident(const ScanKernel<T> &k, int nseg, std::atomic<int> &known) {
     return (int64_t)n * nseg;
 }
 
+// With lengths, rounds after the first are shorter: CTAs of short rows make room early.
+// 0.35 + 0.65 rounds in place of rounds, forward and backward of bf16 B = 32, L = 1500,
+// D = 320, lengths of 0 to L: 30.8 -> 24.7 and 56.4 -> 36.8 us; the order of the rows by
+// length changes either by 4 % at most.
+constexpr double kFirstRound = 0.35;
+
 // Channel pairs per CTA and segments per chain: the least of rounds of resident CTAs times
 // a CTA's waves, with a few waves' worth for its start and end.
 template <typename T>
-ScanPlan scan_plan(int64_t B, int64_t L, int D, bool backward, bool leak) {
+ScanPlan scan_plan(int64_t B, int64_t L, int D, bool backward, bool leak, bool ragged) {
     static std::atomic<int> known[64][2][2][4][4];          // resident CTAs: device, direction, leak, pairs, segments
     int dev = 0;
     cudaGetDevice(&dev);
@@ -798,9 +807,10 @@ ScanPlan scan_plan(int64_t B, int64_t L, int D, bool backward, bool leak) {
         for (p.nseg = 1; p.nseg <= kMaxSeg && p.nseg <= p.ntiles; p.nseg *= 2, ++at) {
             const int64_t room = resident(k, p.nseg, known[dev & 63][backward][leak][lp - 2][at]);
             if (room < 1) continue;
-            const int64_t rounds = (p.chains * p.nseg + room - 1) / room;
+            double rounds = (double)((p.chains * p.nseg + room - 1) / room);
+            if (ragged) rounds = kFirstRound + (1 - kFirstRound) * rounds;
             const int waves = (p.ntiles + p.nseg - 1) / p.nseg;
-            const double cost = (double)rounds * (waves + 4) * kRowCost[lp - 2];
+            const double cost = rounds * (waves + 4) * kRowCost[lp - 2];
             if (best_cost == 0 || cost < best_cost * 0.999) {
                 best_cost = cost;
                 best = p;
@@ -812,7 +822,7 @@ ScanPlan scan_plan(int64_t B, int64_t L, int D, bool backward, bool leak) {
 
 template <typename T>
 cudaError_t launch_scan(bool backward, bool leak, ScanArgs<T> &a, int64_t B, cudaStream_t st) {
-    const ScanPlan p = scan_plan<T>(B, a.L, a.D, backward, leak);
+    const ScanPlan p = scan_plan<T>(B, a.L, a.D, backward, leak, a.lengths != nullptr);
     if (p.nseg < 1) return cudaErrorInvalidConfiguration;
     const ScanKernel<T> k = leak ? kernel_of<T, true>(backward, p.log2p) : kernel_of<T, false>(backward, p.log2p);
     a.groups = p.groups;
