@@ -86,14 +86,18 @@ __device__ __forceinline__ f32x2 act2(f32x2 z) {
     return z;
 }
 // act'(z) of two values.  1 - sigma(u) is e^-u sigma(u): the difference would lose it for large
-// u.  u is held above -80, where sigma and its slope are below 2^-115 either way.
-__device__ __forceinline__ f32x2 act_grad2(int kind, f32x2 z) {
-    constexpr float l2e = 1.44269504f;
-    const f32x2 one = 0x3f8000003f800000ull;
-    const f32x2 zz = mul2(z, z);
-    const f32x2 u = kind == RLM_ACT_GELU ? mul2(z, fma2(zz, twice(kBend3), twice(kBend1))) : z;
-    float2 f = unpack(u);
-    f = unpack(mul2(pack(make_float2(fmaxf(f.x, -80.f), fmaxf(f.y, -80.f))), twice(-l2e)));
+// u.  z is held where |u| < 85.2, so that e^-u, its inverse and z's powers stay within fp32 (the
+// slope is 0 or 1 to 2^-110 from there on); min and max of NaN are NaN.
+__device__ __forceinline__ float held(float z, float most) {
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(z) : "f"(most));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(z) : "f"(-most));
+    return z;
+}
+template <int kAct>
+__device__ __forceinline__ f32x2 act_grad2(float z0, float z1) {
+    constexpr float l2e = 1.44269504f, most = kAct == RLM_ACT_GELU ? 9.9f : 85.f;
+    const f32x2 one = 0x3f8000003f800000ull, z = pack(make_float2(held(z0, most), held(z1, most))), zz = mul2(z, z);
+    float2 f = unpack(mul2(kAct == RLM_ACT_GELU ? mul2(z, fma2(zz, twice(kBend3), twice(kBend1))) : z, twice(-l2e)));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(f.x));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(f.y));
     const f32x2 e = pack(f);
@@ -101,8 +105,8 @@ __device__ __forceinline__ f32x2 act_grad2(int kind, f32x2 z) {
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(f.x));
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(f.y));
     const f32x2 s = pack(f), rest = mul2(e, s);
-    if (kind == RLM_ACT_SIGMOID) return mul2(s, rest);
-    const f32x2 slope = kind == RLM_ACT_GELU ? mul2(z, fma2(zz, twice(3.0f * kBend3), twice(kBend1))) : z;
+    if (kAct == RLM_ACT_SIGMOID) return mul2(s, rest);
+    const f32x2 slope = kAct == RLM_ACT_GELU ? mul2(z, fma2(zz, twice(3.0f * kBend3), twice(kBend1))) : z;
     return mul2(s, fma2(slope, rest, one));
 }
 
@@ -585,7 +589,7 @@ __global__ void __launch_bounds__(256) k_dz(const DzArgs a) {
                 uint32_t w[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[i] = mul2(v[i], act_grad2(kAct, pack(make_float2(lo16(pw[i]), hi16(pw[i])))));
+                    v[i] = mul2(v[i], act_grad2<kAct>(lo16(pw[i]), hi16(pw[i])));
                     const float2 f = unpack(v[i]);
                     w[i] = pack2(f.x, f.y);
                 }

@@ -214,3 +214,26 @@ def test_offsets_past_2_31_elements():
     rlm.rlm_linear_backward(y[-300:], x[-300:], w, dx=part)
     near(dx[-300:], y[-300:].double() @ w.double(), B16, "dx")
     near(part, y[-300:].double() @ w.double(), B16, "dx of the tail")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "sigmoid"])
+def test_slopes_of_extreme_pre_activations(act):
+    """act'(z) over all of bf16's range: its limits far out, NaN of NaN.  One row, so that dbias is dz
+    itself.  Bound: the approximate instructions on arguments up to 128 (2^-15), and 1e-30 where the
+    slope itself is nothing."""
+    mags = [0.0, 1e-30, 1e-3, 0.5, 1.0, 3.0, 5.0, 8.0, 9.5, 10.5, 20.0, 60.0, 84.0, 90.0, 300.0, 1e4, 1e9, 1e13, 1e20,
+            3e38, float("inf")]
+    z = torch.tensor([s * m for m in mags for s in (1, -1)] + [float("nan")] * 6).bfloat16().cuda()
+    N = z.numel()
+    x, w = torch.zeros(1, 8, device="cuda").bfloat16(), torch.zeros(N, 8, device="cuda").bfloat16()
+    got = torch.empty(N, device="cuda")
+    rlm.rlm_linear_backward(torch.ones(1, N, device="cuda").bfloat16(), x, w, pre=z[None], act=act, dbias=got)
+    done()
+    z64 = z.double().clamp(-400, 400)
+    bend = 2 * (2 / np.pi) ** 0.5
+    u = bend * (z64 + 0.044715 * z64 ** 3) if act == "gelu" else z64
+    slope = bend * z64 * (1 + 3 * 0.044715 * z64 ** 2) if act == "gelu" else z64
+    s, rest = torch.sigmoid(u), torch.sigmoid(-u)           # (1 - s would lose rest)
+    want = s * rest if act == "sigmoid" else s * (1 + slope * rest)
+    assert torch.isnan(got[-6:]).all()
+    assert ((got.double() - want)[:-6].abs() <= 2.0 ** -15 * want[:-6].abs() + 1e-30).all()
