@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_ada
     const int64_t at = (int64_t)(blockIdx.x - a.first[lo]) * kChunk + threadIdx.x * 8;
     float scale = 1.f;
     if (a.grad_scale) {
-        scale = __ldg(a.grad_scale);
+        scale = *a.grad_scale;
         if (!isfinite(scale)) return;           // an overflowed step: nothing changes
     }
     constexpr int kMoment = k8Bit ? 1 : 4;

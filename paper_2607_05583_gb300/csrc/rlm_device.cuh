@@ -53,9 +53,20 @@ __device__ __forceinline__ float2 lambda_pow(float gamma, float omega, float n) 
 // Programmatic dependent launch: returns once the kernels before this one in the stream have
 // finished, and lets the next one start its own set-up (it waits here in turn).  For kernels
 // launched with launch_dependent().
+// What that kernel may have written is read by coherent loads that stay behind the wait: plain
+// ones or the volatile one below.  The read-only path (ld.global.nc, __ldg) may be used for
+// nothing that changes while a kernel is resident, and a dependent kernel is resident early;
+// neither __ldg nor __ldcs is bound to stay behind the wait.
 __device__ __forceinline__ void wait_for_previous() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// 16 bytes that are read once.
+__device__ __forceinline__ uint4 load_once(const void *p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
 }
 
 // Two fp32 values in one 64-bit register, and the packed arithmetic on them (each half

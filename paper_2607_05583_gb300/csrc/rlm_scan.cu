@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> 
     Where w = where<kLog2P>(a);
     open_peers(peers, a.nseg);
     wait_for_previous();
-    w.len = a.lengths ? min(max(__ldg(a.lengths + w.row), 0), a.L) : a.L;
+    w.len = a.lengths ? min(max(a.lengths[w.row], 0), a.L) : a.L;
 
     if (w.warp >= kDataThreads / 32) {
         // Runs to states, the two warps in turn: lane (part, cp) holds runs 8 part .. 8 part + 7.
@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, kBwdPerSm<T>) k_scan_backward(const 
     constexpr int ST = kBwdStages<T>;
     open_peers(peers, a.nseg);
     wait_for_previous();
-    w.len = a.lengths ? min(max(__ldg(a.lengths + w.row), 0), a.L) : a.L;
+    w.len = a.lengths ? min(max(a.lengths[w.row], 0), a.L) : a.L;
 
     if (w.warp >= kDataThreads / 32) {
         // A lane's 8 runs are one chunk: their states follow from the chunk's saved state.
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, kBwdPerSm<T>) k_scan_backward(const 
         auto saved_at = [&](int k) {
             const int t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens + part * kChunk;
             if (k >= w.n || !w.on || t0 < 0 || t0 >= w.len) return make_float2(0.f, 0.f);
-            return __ldg(reinterpret_cast<const float2 *>(a.saved + ((int64_t)w.row * a.nchunks + t0 / kChunk) * a.D + w.c));
+            return *reinterpret_cast<const float2 *>(a.saved + ((int64_t)w.row * a.nchunks + t0 / kChunk) * a.D + w.c);
         };
         bool gave_up = false;
         float2 next = saved_at(me);
@@ -713,7 +713,6 @@ __global__ void __launch_bounds__(256) k_scan_step(const T *x, const T *g, T *y,
             row = i / half;
             c = 2 * (int)(i - row * half);
         }
-        // Plain loads: the previous kernel may still have been writing these when this one started.
         using Raw = typename Pair<T>::Raw;
         const float2 gv = Pair<T>::value(*reinterpret_cast<const Raw *>(g + row * g_b + c));
         const float2 xv = Pair<T>::value(*reinterpret_cast<const Raw *>(x + row * x_b + c));
