@@ -395,10 +395,17 @@ def _check(status: int, where: str):
         raise RlmError(status, where, load_library().rlm_last_error().decode())
 
 
-def _workspace(nbytes: int, device) -> torch.Tensor | None:
+def _workspace(nbytes: int, device, stream=None) -> torch.Tensor | None:
+    """A call's own workspace, from the allocator's pool of the stream that the call runs on: once
+    released it goes to that stream's later work only."""
     if nbytes == 0:
         return None
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 # --------------------------------------------------------------- entry points
@@ -433,7 +440,7 @@ def rlm_mix_prefill(x: torch.Tensor, params: Params, y: torch.Tensor,
     xt, yt = _field(x), _field(y)
     if workspace is None:
         workspace = _workspace(lib.rlm_prefill_workspace_size(xt.B, xt.L, xt.D, params.M, xt.dtype),
-                               x.device)
+                               x.device, stream)
     st = state_out._c() if state_out is not None else None
     _check(lib.rlm_mix_prefill(ctypes.byref(xt), ctypes.byref(params._c()), ctypes.byref(yt),
                                ctypes.byref(st) if st is not None else None,
@@ -450,7 +457,7 @@ def rlm_mix_prefill_from(x: torch.Tensor, params: Params, state_in: State | None
     xt, yt = _field(x), _field(y)
     if workspace is None:
         workspace = _workspace(lib.rlm_prefill_workspace_size(xt.B, xt.L, xt.D, params.M, xt.dtype),
-                               x.device)
+                               x.device, stream)
     si = state_in._c() if state_in is not None else None
     so = state_out._c() if state_out is not None else None
     _check(lib.rlm_mix_prefill_from(ctypes.byref(xt), ctypes.byref(params._c()),
@@ -494,7 +501,7 @@ def rlm_mix_backward(dy: torch.Tensor, x: torch.Tensor, params: Params, dx: torc
     dyt, xt, dxt = _field(dy), _field(x), _field(dx)
     if workspace is None:
         workspace = _workspace(lib.rlm_backward_workspace_size(xt.B, xt.L, xt.D, params.M,
-                                                               xt.dtype), x.device)
+                                                               xt.dtype), x.device, stream)
     _check(lib.rlm_mix_backward(ctypes.byref(dyt), ctypes.byref(xt), ctypes.byref(params._c()),
                                 ctypes.byref(dxt), ctypes.byref(dparams._c()),
                                 ctypes.byref(_launch(stream, workspace))), "rlm_mix_backward")
@@ -512,7 +519,7 @@ def rlm_mix_backward_from(dy: torch.Tensor, x: torch.Tensor, params: Params, sta
     dyt, xt, dxt = _field(dy), _field(x), _field(dx)
     if workspace is None:
         workspace = _workspace(lib.rlm_backward_workspace_size(xt.B, xt.L, xt.D, params.M, xt.dtype),
-                               x.device)
+                               x.device, stream)
     opt = lambda st: ctypes.byref(st._c()) if st is not None else None
     _check(lib.rlm_mix_backward_from(ctypes.byref(dyt), ctypes.byref(xt), ctypes.byref(params._c()),
                                      opt(state_in), opt(d_state_out), ctypes.byref(dxt),
@@ -543,7 +550,7 @@ def rlm_mixer_prefill(x: torch.Tensor, g: torch.Tensor | None, params: Params, l
     gt = _field(g) if g is not None else None
     if workspace is None:
         workspace = _workspace(lib.rlm_prefill_workspace_size(xt.B, xt.L, xt.D, params.M, xt.dtype),
-                               x.device)
+                               x.device, stream)
     ref = lambda c: ctypes.byref(c) if c is not None else None
     opt = lambda o: ref(o._c()) if o is not None else None
     _check(lib.rlm_mixer_prefill(ctypes.byref(xt), ref(gt), ctypes.byref(params._c()), opt(local), opt(coupling),
@@ -655,7 +662,7 @@ def rlm_linear(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, bias: torch.Te
     rt = _matrix(residual, "residual") if residual is not None else None
     pt = _matrix(pre, "pre") if pre is not None else None
     if workspace is None:
-        workspace = _workspace(lib.rlm_linear_workspace_size(xt.rows, xt.cols, wt.rows), x.device)
+        workspace = _workspace(lib.rlm_linear_workspace_size(xt.rows, xt.cols, wt.rows), x.device, stream)
     _check(lib.rlm_linear(xt, wt, _opt(bias, torch.float32, (wt.rows,), "bias"), _act(act),
                           rt, pt, yt, _launch(stream, workspace)), "rlm_linear")
 
@@ -670,7 +677,8 @@ def rlm_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, dx: 
     opt = lambda t, name: _matrix(t, name) if t is not None else None
     pt, dxt, dwt = opt(pre, "pre"), opt(dx, "dx"), opt(dw, "dw")
     if workspace is None:
-        workspace = _workspace(lib.rlm_linear_backward_workspace_size(xt.rows, xt.cols, wt.rows, _act(act)), x.device)
+        workspace = _workspace(lib.rlm_linear_backward_workspace_size(xt.rows, xt.cols, wt.rows, _act(act)), x.device,
+                               stream)
     _check(lib.rlm_linear_backward(dyt, xt, wt, pt, _act(act), dxt,
                                    dwt, _opt(dbias, torch.float32, (wt.rows,), "dbias"),
                                    _launch(stream, workspace)), "rlm_linear_backward")

@@ -237,3 +237,25 @@ def test_slopes_of_extreme_pre_activations(act):
     want = s * rest if act == "sigmoid" else s * (1 + slope * rest)
     assert torch.isnan(got[-6:]).all()
     assert ((got.double() - want)[:-6].abs() <= 2.0 ** -15 * want[:-6].abs() + 1e-30).all()
+
+
+def test_workspace_belongs_to_the_stream_of_the_call():
+    """A call's own workspace is not handed to the current stream while the call's stream uses it."""
+    R, K, N = 515, 8192, 1024
+    x, w, _, _, dy = make(R, K, N)
+    size = rlm.rlm_linear_workspace_size(R, K, N)
+    assert size > 0
+    want, got = torch.empty_like(dy), torch.empty_like(dy)
+    rlm.rlm_linear(x, w, want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        torch.cuda.empty_cache()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(4_000_000)
+        rlm.rlm_linear(x, w, got, stream=stream)
+        other = torch.empty(size, dtype=torch.uint8, device="cuda")
+        for _ in range(1500):                   # on the current stream, while the call runs
+            other.fill_(255)
+        done()
+        assert torch.equal(got, want)
