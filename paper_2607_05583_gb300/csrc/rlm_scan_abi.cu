@@ -32,11 +32,14 @@ rlm_status check_field(const rlm_strided *t, const char *name, rlm_strided *out)
     if (t->L == 1) out->stride_l = t->D;
     if (t->B == 1) out->stride_b = t->L * out->stride_l;
     const int64_t per16 = 16 / (int64_t)elem_size(t->dtype);
-    for (int64_t st : {out->stride_b, out->stride_l}) {
-        if (st < 0 || st > (int64_t)1 << 40 || st % per16 != 0)
-            return fail(RLM_ERR_INVALID_ARG, "%s has a stride of %lld elements (need a multiple of 16 bytes, >= 0)", name,
-                        (long long)st);
-    }
+    // (No field reaches over 2^44 elements; that every extent below does not pass 64 bits.)
+    const int64_t most = (int64_t)1 << 44;
+    if (out->stride_l < 0 || out->stride_l > most / t->L || out->stride_l % per16 != 0)
+        return fail(RLM_ERR_INVALID_ARG, "%s has a stride of %lld elements (need a multiple of 16 bytes, >= 0)", name,
+                    (long long)out->stride_l);
+    if (out->stride_b < 0 || out->stride_b > most / t->B || out->stride_b % per16 != 0)
+        return fail(RLM_ERR_INVALID_ARG, "%s has a stride of %lld elements (need a multiple of 16 bytes, >= 0)", name,
+                    (long long)out->stride_b);
     return RLM_OK;
 }
 

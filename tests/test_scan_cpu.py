@@ -101,3 +101,12 @@ def test_decode_refusals(lib):
 def test_sizes(lib):
     assert rlm.rlm_scan_saved_size(2, 65, 8) == 2 * 2 * 8 * 4
     assert rlm.rlm_scan_saved_size(0, 65, 8) == 0
+
+
+def test_strides_beyond_any_memory(lib):
+    """Extents that would pass 64 bits (2^24 rows, 2^40 apart) are refused, not wrapped round."""
+    L, sl = 1 << 24, 1 << 40
+    far = field(0, B=1, L=L, sl=sl, sb=0)
+    assert prefill(lib, far, field(1, B=1, L=L, sl=64), field(2, B=1, L=L, sl=64), ln=ctypes.POINTER(rlm._Launch)()) \
+        == rlm.RLM_ERR_INVALID_ARG
+    assert b"x has a stride" in lib.rlm_last_error()
