@@ -134,6 +134,7 @@ struct GemmCfg {
 struct GemmArgs {
     int M, N, K;                // output rows and columns, contraction
     int tiles_m, tiles_n, splits, steps_per_split, steps;
+    int whole, units;           // units that are whole tiles (of a split), and all (see unit_of())
     const float *bias;          // nullable [N]
     const bf16 *residual;       // nullable [M][ld]
     int64_t residual_ld;
@@ -150,6 +151,24 @@ __device__ __forceinline__ void tile_of(int t, const GemmArgs &g, int &tm, int &
     const int rows = min(kGroup, g.tiles_m - first), in = t - grp * per;
     tn = in / rows;
     tm = first + in - tn * rows;
+}
+
+// Unit u of the work: a tile, or a split's share of one; of 256 columns also half a tile, where
+// the last round of tiles would leave more than half the pairs idle (launch_gemm()).
+struct Unit {
+    int tm, split, col, half;   // row tile, split, first column, whether 128 columns in place of 256
+};
+template <int kBN>
+__device__ __forceinline__ Unit unit_of(int u, const GemmArgs &g) {
+    Unit r;
+    const int past = u - g.whole;
+    r.half = kBN == 256 && past >= 0;
+    const int t = r.half ? g.whole + (past >> 1) : u;
+    r.split = t % g.splits;
+    int tn;
+    tile_of(t / g.splits, g, r.tm, tn);
+    r.col = tn * kBN + (r.half && (past & 1) ? 128 : 0);
+    return r;
 }
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -219,24 +238,24 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     fence_after();
     wait_for_previous();
     const uint32_t tmem = *tmem_at;
-    const int units = g.tiles_m * g.tiles_n * g.splits;
+    const int units = g.units;
 
     if (warp == kEpiWarps) {
         int it = 0;
         bool ok = true;
         for (int u = unit0; ok && u < units; u += unit_step) {
-            const int split = u % g.splits;
-            int tm, tn;
-            tile_of(u / g.splits, g, tm, tn);
-            const int s0 = split * g.steps_per_split, s1 = min(g.steps, s0 + g.steps_per_split);
-            const int ra = tm * Cfg::kTileM + rank * kBM, rb = tn * kBN + rank * Cfg::kRowsB;
+            const Unit unit = unit_of<kBN>(u, g);
+            const int s0 = unit.split * g.steps_per_split, s1 = min(g.steps, s0 + g.steps_per_split);
+            const int boxes = Cfg::kRowsB / 64 >> unit.half;            // of 64 rows of B each
+            const int ra = unit.tm * Cfg::kTileM + rank * kBM, rb = unit.col + rank * boxes * 64;
+            const uint32_t bytes = (kPair ? 2 : 1) * (Cfg::kA + boxes * 8192);
             for (int s = s0; s < s1; ++s, ++it) {
                 const int st = it % ST;
                 if (it >= ST && !(ok = wait_bar(empty + st * 8, (it / ST - 1) & 1, abort_flag, &g_linear_status))) break;
                 const uint32_t a = base + st * Cfg::kStage, b = a + Cfg::kA;
                 const uint32_t bar = kPair ? map_rank(full + st * 8, 0) : full + st * 8;
                 if (elect()) {
-                    if (rank == 0) bar_expect_tx(full + st * 8, (kPair ? 2 : 1) * Cfg::kStage);
+                    if (rank == 0) bar_expect_tx(full + st * 8, bytes);
                     auto load = [&](uint32_t to, const CUtensorMap *map, int c0, int c1) {
                         if constexpr (kPair) tma_load_2d_pair(to, map, c0, c1, bar);
                         else tma_load_2d(to, map, c0, c1, bar);
@@ -247,11 +266,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                     } else {
                         load(a, &map_a, s * kBK, ra);
                     }
-                    if (kBMn) {
 #pragma unroll
-                        for (int j = 0; j < Cfg::kRowsB / 64; ++j) load(b + j * 8192, &map_b, rb + j * 64, s * kBK);
-                    } else {
-                        load(b, &map_b, s * kBK, rb);
+                    for (int j = 0; j < Cfg::kRowsB / 64; ++j) {
+                        if (j >= boxes) break;
+                        if (kBMn) load(b + j * 8192, &map_b, rb + j * 64, s * kBK);
+                        else load(b + j * 8192, &map_b, s * kBK, rb + j * 64);
                     }
                 }
                 __syncwarp();
@@ -263,14 +282,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 for (int n = 0; n < 1 << 22 && !bar_try(full + (i % ST) * 8, (i / ST) & 1); ++n) {}
     } else if (warp == kEpiWarps + 1) {
         if (rank == 0) {
-            constexpr uint32_t id = idesc(Cfg::kTileM, kBN, kAMn, kBMn);
             constexpr uint32_t a_k = (kAMn ? 2048 : 32) >> 4, b_k = (kBMn ? 2048 : 32) >> 4;       // 16 contraction indexes on
             const uint64_t da0 = desc(base, kAMn ? 8192 : 16, 1024), db0 = desc(base + Cfg::kA, kBMn ? 8192 : 16, 1024);
             int it = 0, n = 0;
             bool ok = true;
             for (int u = unit0; ok && u < units; u += unit_step, ++n) {
-                const int split = u % g.splits;
-                const int s0 = split * g.steps_per_split, s1 = min(g.steps, s0 + g.steps_per_split);
+                const Unit unit = unit_of<kBN>(u, g);
+                const int s0 = unit.split * g.steps_per_split, s1 = min(g.steps, s0 + g.steps_per_split);
+                const uint32_t id = unit.half ? idesc(Cfg::kTileM, 128, kAMn, kBMn) : idesc(Cfg::kTileM, kBN, kAMn, kBMn);
                 const int buf = n & 1;
                 const uint32_t d = tmem + buf * kBN;
                 if (n >= 2 && !(ok = wait_bar(acc_empty + buf * 8, (n / 2 - 1) & 1, abort_flag, &g_linear_status))) break;
@@ -295,7 +314,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     } else {
         constexpr bool kF32 = kOut == kOutF32;
         constexpr int kCols = kF32 ? 16 : 32;               // output columns handled at a time, 64 bytes
-        constexpr int kWarpCols = kBN / (kEpiWarps / 4);    // a warp's columns of a tile
+        constexpr int kWarpCols = kBN / (kEpiWarps / 4);    // a warp's columns of a tile (of half a tile 32)
         const uint32_t staging = base + Cfg::kOffOut + warp * kStageOut;
         int n = 0;
         // The staged rows to memory, eight rows of 64 bytes a request; to: (row0, col), `cols` columns there.
@@ -324,10 +343,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             send(reinterpret_cast<char *>(to), ld * 2, row0, cols);
         };
         for (int u = unit0; u < units; u += unit_step, ++n) {
-            const int split = u % g.splits;
-            int tm, tn;
-            tile_of(u / g.splits, g, tm, tn);
-            const int row0 = tm * Cfg::kTileM + rank * kBM + (warp & 3) * 32, col0 = tn * kBN + (warp >> 2) * kWarpCols;
+            const Unit unit = unit_of<kBN>(u, g);
+            const int cols = kWarpCols >> unit.half;
+            const int row0 = unit.tm * Cfg::kTileM + rank * kBM + (warp & 3) * 32, col0 = unit.col + (warp >> 2) * cols;
             const int buf = n & 1;
             // The residual's chunk and a lane's bias, asked for ahead of the accumulator; both are handed
             // to the lanes that need them through the staging buffer.
@@ -348,9 +366,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             // The next tile's into L2, a row a lane, where the products leave no time for its latency (72 ->
             // 63 us at 131072 x 256 x 512).
             if (!kF32 && g.residual && g.steps <= 16 && u + unit_step < units) {
-                int nm, nn;
-                tile_of((u + unit_step) / g.splits, g, nm, nn);
-                const int r = nm * Cfg::kTileM + rank * kBM + (warp & 3) * 32 + lane, c = nn * kBN + (warp >> 2) * kWarpCols;
+                const Unit next = unit_of<kBN>(u + unit_step, g);
+                const int r = next.tm * Cfg::kTileM + rank * kBM + (warp & 3) * 32 + lane;
+                const int c = next.col + (warp >> 2) * (kWarpCols >> next.half);
                 if (r < g.M && c < g.N) {
                     const bf16 *p = g.residual + (int64_t)r * g.residual_ld + c;
                     asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
@@ -364,15 +382,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             }
             if (!wait_bar(acc_full + buf * 8, (n / 2) & 1, abort_flag, &g_linear_status)) break;
             fence_after();
-            const uint32_t acc = tmem + buf * kBN + (warp >> 2) * kWarpCols + ((uint32_t)(warp & 3) << 21);
+            const uint32_t acc = tmem + buf * kBN + (warp >> 2) * cols + ((uint32_t)(warp & 3) << 21);
 #pragma unroll 1
-            for (int c = 0; c < kWarpCols; c += kCols) {
+            for (int c = 0; c < cols; c += kCols) {
                 const int col = col0 + c;
                 uint32_t v[kCols];
 #pragma unroll
                 for (int i = 0; i < kCols; i += 16) tmem_ld16(acc + c + i, v + i);
                 tmem_wait_ld();
-                if (c + kCols >= kWarpCols) {               // the last read of this accumulator
+                if (c + kCols >= cols) {                    // the last read of this accumulator
                     fence_before();
                     __syncwarp();
                     if (lane == 0) {
@@ -385,7 +403,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 #pragma unroll
                     for (int p = 0; p < 4; ++p)
                         st_shared16(staging + piece(lane, p), make_uint4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]));
-                    send(reinterpret_cast<char *>(static_cast<float *>(g.out) + ((int64_t)split * g.M + row0) * g.out_ld + col),
+                    send(reinterpret_cast<char *>(static_cast<float *>(g.out) + ((int64_t)unit.split * g.M + row0) * g.out_ld + col),
                          g.out_ld * 4, row0, g.N - col);
                 } else {
                     f32x2 z[16];
@@ -409,7 +427,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) st_shared16(staging + piece(i * 8 + (lane >> 2), lane & 3), res[i]);
                         __syncwarp();
-                        if (c + kCols < kWarpCols) ask(col + kCols);
+                        if (c + kCols < cols) ask(col + kCols);
 #pragma unroll
                         for (int p = 0; p < 4; ++p) {
                             const uint4 r = ld_shared16(staging + piece(lane, p));
@@ -682,6 +700,14 @@ struct TileKind {
 };
 constexpr TileKind kTiles[] = {{true, 256, 5.7, 0.285, 1.9}, {true, 128, 5.1, 0.17, 1.2}, {false, 128, 4.0, 0.19, 1.0}};
 
+// Tiles of 256 x 256 whose halves are units of their own: those of the last round, where their
+// halves fit into one.  (4096 x 4096 x 4096: 256 tiles on 76 pairs, three rounds and a half in
+// place of four.)
+int64_t halved(int64_t tiles, int64_t slots) {
+    const int64_t last = tiles % slots;
+    return tiles > slots && 2 * last <= slots ? last : 0;
+}
+
 GemmPlan find_plan(int64_t M, int64_t N, int64_t K) {
     GemmPlan best = {};
     double best_cost = 0;
@@ -694,11 +720,13 @@ GemmPlan find_plan(int64_t M, int64_t N, int64_t K) {
             const int per = (steps + splits - 1) / splits;
             if ((steps + per - 1) / per != splits) continue;
             if (splits > 1 && tm * tn * splits > slots) break;      // more work units than SMs: nothing to fill
-            const int64_t rounds = (tm * tn * splits + slots - 1) / slots;
+            const bool halves = t.bn == 256 && splits == 1 && halved(tm * tn, slots) > 0;
+            const int64_t rounds = (tm * tn * splits + slots - 1) / slots - halves;
             // Bytes from memory, and from L2: every unit's operands, at 20 TB/s beside the output.
             const double out = 2.0 * M * N, bytes = 2.0 * ((double)M * K + (double)N * K) + out;
             const double l2 = (double)(tm * tn) * steps * kBK * 2.0 * ((t.pair ? 256 : 128) + t.bn);
-            const double work = (double)rounds * std::max(per * t.step, t.epilogue);
+            double work = (double)rounds * std::max(per * t.step, t.epilogue);
+            if (halves) work += std::max(per * kTiles[1].step, kTiles[1].epilogue);
             double cost = t.launch + std::max({work, bytes / 6.0e6, l2 / 20.0e6 + out / 8.0e6});
             if (splits > 1) cost += 3.0 + 8.0 * splits * (double)M * N / 8.0e6;
             if (best_cost == 0 || cost < best_cost) {
@@ -747,7 +775,7 @@ struct Epilogue {
 };
 
 template <bool kPair, bool kAMn, bool kBMn, int kBN, int kOut, int kAct>
-cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const GemmArgs &g, cudaStream_t st) {
+cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, GemmArgs g, cudaStream_t st) {
     using Cfg = GemmCfg<kPair, kBN>;
     auto *fn = k_gemm<kPair, kAMn, kBMn, kBN, kOut, kAct>;
     static std::atomic<int> ctas[64];               // per device: CTAs that fit, once the kernel is set up
@@ -776,9 +804,15 @@ cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, const Gemm
         }
         ctas[dev & 63].store(room, std::memory_order_relaxed);
     }
-    const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits * (kPair ? 2 : 1);
-    return launch_dependent(fn, dim3((unsigned)std::min<int64_t>(units, room)), kGemmThreads, Cfg::kSmem, st, kPair ? 2 : 1,
-                            ma, mb, g);
+    constexpr int kCtas = kPair ? 2 : 1;
+    g.whole = g.units = g.tiles_m * g.tiles_n * g.splits;
+    if (kBN == 256 && g.splits == 1) {
+        const int last = halved(g.units, room / kCtas);
+        g.whole -= last;
+        g.units += last;
+    }
+    return launch_dependent(fn, dim3((unsigned)std::min<int64_t>((int64_t)g.units * kCtas, room)), kGemmThreads, Cfg::kSmem, st,
+                            kCtas, ma, mb, g);
 }
 
 template <bool kPair, bool kAMn, bool kBMn, int kBN>
@@ -806,7 +840,7 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
     const GemmPlan p = gemm_plan(M, N, K);
     CUtensorMap ma, mb;
     if (!(kAMn ? operand_map(&ma, a.ptr, M, K, a.ld, 64) : operand_map(&ma, a.ptr, K, M, a.ld, kBM)) ||
-        !(kBMn ? operand_map(&mb, b.ptr, N, K, b.ld, 64) : operand_map(&mb, b.ptr, K, N, b.ld, p.pair ? p.bn / 2 : p.bn)))
+        !(kBMn ? operand_map(&mb, b.ptr, N, K, b.ld, 64) : operand_map(&mb, b.ptr, K, N, b.ld, 64)))
         return cudaErrorInvalidValue;
     const bool split = p.splits > 1;
     const int out = split || ep.out_f32 ? kOutF32 : ep.pre ? kOutPre : kOutBf16;

@@ -259,3 +259,20 @@ def test_workspace_belongs_to_the_stream_of_the_call():
             other.fill_(255)
         done()
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("shape", [(8000, 2048, 1160), (16387, 1160, 2056), (4096, 4096, 4096)])
+def test_last_round_of_tiles_in_halves(shape):
+    """Products whose last round of 256 x 256 tiles is cut into halves, some with few columns."""
+    R, K, N = shape
+    x, w, bias, res, dy = make(R, K, N)
+    y, pre = torch.empty_like(dy), torch.empty_like(dy)
+    rlm.rlm_linear(x, w, y, bias=bias, residual=res, act="silu", pre=pre)
+    z = x.double() @ w.double().T + bias.double()
+    near(pre, z, B16, "pre")
+    near(y, act64(z, "silu") + res.double(), B16, "y")
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    rlm.rlm_linear_backward(dy, x, w, dx=dx, dw=dw)
+    done()
+    near(dx, dy.double() @ w.double(), B16, "dx")
+    near(dw, dy.double().T @ x.double(), B16, "dw")
