@@ -484,11 +484,15 @@ __global__ void __launch_bounds__(kWarps * 32) k_few(const FewArgs a) {
     for (int i = 0; i < kTok; ++i) xp[i] = a.x + (int64_t)min(i * 8 + g, a.R - 1) * a.x_ld + q * 8;
     float d[kTok][4] = {};
     constexpr int kDeep = kTok > 2 ? 2 : 4;         // blocks in flight
+    // They follow one another in w's rows where that leaves no warp without a share (from HBM, us,
+    // kWarps blocks apart / one after the other: 8 rows, K = N = 4096 8.0 / 7.5, 4096 x 11008 17.0 /
+    // 16.4; 16 rows, 4096 x 4096 10.4 / 9.1; but 8 rows, 1024 x 1024 2.4 / 3.0).
+    const int apart = a.K >= kDeep * kWarps * 32 ? 32 : kWarps * 32;
     auto blocks = [&](int k, auto whole) {
         uint4 w[kDeep][2], x[kDeep][kTok];
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) {
-            const int at = k + u * kWarps * 32;
+            const int at = k + u * apart;
             const bool ok = decltype(whole)::value || at + q * 8 < a.K;
             w[u][0] = ok ? load_once(w0 + at) : make_uint4(0, 0, 0, 0);
             w[u][1] = ok ? load_once(w8 + at) : make_uint4(0, 0, 0, 0);
@@ -504,8 +508,8 @@ __global__ void __launch_bounds__(kWarps * 32) k_few(const FewArgs a) {
                 mma16816(d[t], w[u][0].z, w[u][1].z, w[u][0].w, w[u][1].w, x[u][t].z, x[u][t].w);
             }
     };
-    int k = warp * 32;
-    for (; k + (kDeep - 1) * kWarps * 32 + 32 <= a.K; k += kDeep * kWarps * 32) blocks(k, std::true_type{});
+    int k = warp * (apart == 32 ? kDeep * 32 : 32);
+    for (; k + (kDeep - 1) * apart + 32 <= a.K; k += kDeep * kWarps * 32) blocks(k, std::true_type{});
     if (k < a.K) blocks(k, std::false_type{});
 #pragma unroll
     for (int t = 0; t < kTok; ++t)
@@ -883,8 +887,8 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
 
 // Whether k_few serves a product: always up to 8 rows; from there its reads of x grow with the
 // rows while the tiles' cost does not (us, from HBM, k_few / tiles): 16 rows, K x N = 4096 x 4096
-// 10.9 / 12.6, 8192 x 1024 15.6 / 11.1, 4096 x 11008 30 / 21; 32 rows, 1024 x 1024 4.1 / 5.6,
-// 2048 x 4096 10.2 / 10.0, 512 x 16384 10.3 / 7.7.
+// 8.8 / 10.8, 8192 x 1024 10.1 / 8.8, 4096 x 11008 22 / 19; 32 rows, 1024 x 1024 3.4 / 5.4,
+// 2048 x 2048 5.2 / 6.7, 2048 x 4096 9.1 / 8.7, 512 x 16384 10.0 / 6.3.
 bool few_rows(int64_t R, int64_t K, int64_t N) {
     if (R <= 8) return true;
     if (R <= 16) return K <= 4096 && K * N <= 24 << 20;
@@ -894,7 +898,7 @@ bool few_rows(int64_t R, int64_t K, int64_t N) {
 template <int kTok>
 cudaError_t launch_few(const FewArgs &a, cudaStream_t st) {
     // Sixteen warps share the contraction, eight where there are three CTAs and more for each SM:
-    // 8.8 against 11.5 us (K = N = 4096, 8 rows), 21.1 against 18.2 us (K = 4096, N = 11008).
+    // 7.5 against 10.0 us (K = N = 4096, 8 rows), 18.6 against 17.0 us (K = 4096, N = 11008).
     const unsigned ctas = (unsigned)((a.N + 15) / 16);
     if (ctas >= 3u * (unsigned)sm_count())
         return launch_dependent(k_few<kTok, 8>, dim3(ctas), 8 * 32, 0, st, 1, a);
