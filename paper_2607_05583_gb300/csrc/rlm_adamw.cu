@@ -5,7 +5,8 @@
 //
 // Bound by memory: 28 bytes a value with fp32 weights, gradients and moments, 10 with bf16
 // weights and gradients and 8-bit moments.  Every tensor is cut into chunks of kChunk
-// values; a block takes one chunk, found by bisection in the tensors' running chunk counts.
+// values; a block takes one chunk, found by one warp's bisection in the tensors' running
+// chunk counts.
 // The tensors' pointers travel in the kernel's parameters (up to kMaxTensors a launch), so
 // a step copies nothing to the device first.  A thread holds 8 values in registers, moved
 // by 16-byte accesses; tensors whose pointers do not allow that, and ends, go value by value.
@@ -23,7 +24,7 @@
 // fused product would decide them (and with them whole steps) otherwise than its definition.
 // Scalar instructions, because mul and add on packed pairs were fused.  sqrt and the
 // quotient of the step are the approximate instructions (2^-22): with the exact sequences
-// the 8-bit step, which its instructions bound (78 % of issue slots), took 379 us at 120 M
+// the 8-bit step, which its instructions bound (82 % of issue slots), took 379 us at 120 M
 // values against 211 us now and 178 us for its bytes.  The 32-bit steps run at the copy
 // rate: 478 us for 3.36 GB (fp32, and bf16 with masters), 7.0 TB/s.
 #include <cuda_fp8.h>
@@ -43,8 +44,8 @@ constexpr int kBlock = RLM_ADAMW_BLOCK;         // values that share a scale
 constexpr int kThreads = 256;
 // Values of a thread block: 8 a thread.  Several rounds a thread, the next round's loads issued
 // before this one's arithmetic or not, measured slower (the blocks at work then spread over more
-// of each buffer): 276 against 227 us for the 8-bit step (as it was then) at 120 M values with two rounds, 491
-// against 478 us for the fp32 one with four.
+// of each buffer): 276 against 227 us for the 8-bit step (as it was then) at 120 M values with
+// two rounds, 491 against 478 us for the fp32 one with four.
 constexpr int kChunk = 8 * kThreads;
 constexpr int kMaxTensors = 400;
 
@@ -190,8 +191,8 @@ struct Reads {
 };
 
 // The 8-bit step has more arithmetic to hide its loads behind, so its registers are held down
-// for more warps: 246 -> 211 us (bf16 weights), 291 -> 276 us (fp32) and 297 -> 281 us (masters) at 120 M
-// values; the 32-bit step loses by it.
+// for more warps: 246 -> 211 us (bf16 weights), 291 -> 276 us (fp32) and 297 -> 281 us
+// (masters) at 120 M values; the 32-bit step loses by it.
 template <typename P, typename G, bool kMaster, bool k8Bit>
 __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_adamw(const __grid_constant__ StepArgs a) {
     wait_for_previous();

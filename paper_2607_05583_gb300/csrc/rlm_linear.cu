@@ -8,21 +8,24 @@
 // (MN-major): x w^T is K, K; dz w is K, MN; dz^T x is MN, MN.  TMA brings either form into
 // 128-byte swizzled shared memory and tcgen05.mma reads either, so nothing is transposed.
 //
-// k_gemm.  Persistent, one CTA per SM, contraction steps of 64; tiles of 256 x 256 or
-// 256 x 128 by pairs of CTAs (cta_group::2), or 128 x 128 by single ones where pairs would be
+// k_gemm.  Persistent, one CTA per SM, contraction steps of 64; tiles of 256 x 256 or 256 x
+// 128 by pairs of CTAs (cta_group::2), or 128 x 128 by single ones where pairs would be
 // few.  Warp 16 feeds a ring of operand stages, warp 17 issues the MMAs into one of two TMEM
 // accumulators, warps 0-15 empty the other: warp w owns TMEM lanes 32 (w mod 4) .. + 31 and
 // quarter w / 4 of the columns, 64 bytes of output at a time, from registers through its own
 // 2 KB of shared memory to 64-byte row pieces.  (TMA stores share the copy engine with the
 // operands, a row a request: 48 against 36 us at 131072 x 256 x 512.)  Long contractions are
-// bound by the tensor pipe (91 % busy at 8192 x 2048 x 4096; 8192 x 4096 x 8192 takes 271 us,
-// 2030 TFLOP/s), short ones by memory and this path's latency: sixteen warps where eight would
-// do, 35 us at 131072 x 256 x 512 (5.7 TB/s).  A pair halves what a CTA reads of B: the same
-// kernel with single 128 x 256 tiles took 319 us.  The MMA and copy warps run warp-uniform
-// code and elect a lane at the instruction itself; issued from a divergent thread an MMA took
-// 130 cycles, whatever its width.  A product of few tiles is cut along the contraction
-// (splits): partial sums go to the workspace in fp32 and k_finish adds them in order and
-// applies the epilogue.  Accumulation is fp32 throughout; results repeat bit for bit.
+// bound by the tensor pipe (91 % busy at 8192 x 2048 x 4096; 8192 x 4096 x 8192 takes 271 to
+// 285 us by the machine, 1930 to 2030 TFLOP/s), short ones by memory and this path's latency:
+// sixteen warps where eight would do, 35 us at 131072 x 256 x 512 (5.7 TB/s).  A pair halves
+// what a CTA reads of B: the same kernel with single 128 x 256 tiles took 319 us.  The MMA and
+// copy warps run warp-uniform code and elect a lane at the instruction itself; issued from a
+// divergent thread an MMA took 130 cycles, whatever its width.  Where the last round of 256 x
+// 256 tiles would leave half the pairs idle its tiles are cut into halves (4096 x 4096 x 4096
+// with gelu, bias and residual 80 -> 74 us, gradients of 8192 x 2048 x 8192 387 -> 366).  A
+// product of few tiles is cut along the contraction (splits): partial sums go to the
+// workspace in fp32 and k_finish adds them in order and applies the epilogue.  Accumulation is
+// fp32 throughout; results repeat bit for bit.
 //
 // dz is rounded to bf16 once, the operand type of the two products that read it; dbias is
 // summed from the fp32 values.

@@ -24,16 +24,15 @@
 // A thread composes its run (first pass), keeps -b in registers, and once it knows the
 // state at the run's start walks the run again for the outputs (second pass).
 //
-// Two more warps turn runs into states, a tile each in turn.  A lane holds one channel
-// pair of 8 consecutive runs (64 tokens, one saved chunk): it composes them, scans across
+// Two more warps turn runs into states, a tile each in turn.  A lane holds one channel pair
+// of 8 consecutive runs (64 tokens, one saved chunk): it composes them, scans across
 // lanes, adds the carry (which one warp hands the other) and gives every run its start
 // state.  The data warps work on other tiles meanwhile: the second pass of tile w follows
-// the first pass of tile w + 1, in the bf16 forward pass that of w + 2 (46 -> 44 us at B = 4,
-// L = 32768, D = 256; fp32 and the backward pass have no room for its rings).  x, needed
-// again then, and g, needed once, have rings of their own: two CTAs per SM in fp32 (73 -> 66
-// us).  (One such warp took 3100 cycles a tile where
-// a cluster shares a chain, half of them the exchange, and bounded the kernel: 54 us at
-// B = 4, L = 32768, D = 256.)
+// the first pass of tile w + 1, in the bf16 forward pass that of w + 2 (46 -> 44 us at B =
+// 4, L = 32768, D = 256; fp32 and the backward pass have no room for its rings).  x, needed
+// again then, and g, needed once, have rings of their own: two CTAs per SM in fp32 (73 ->
+// 66 us).  (One such warp took 3100 cycles a tile where a cluster shares a chain, half of
+// them the exchange, and bounded the kernel: 54 us at B = 4, L = 32768, D = 256.)
 //
 // Segments.  Few channels would leave SMs idle, so a cluster of nseg CTAs (2, 4 or 8)
 // shares a chain of tiles: in wave w CTA s takes tile w nseg + s and sends the tile's
