@@ -320,6 +320,10 @@ RLM_API rlm_status rlm_mixer_decode(const rlm_tensor *x_t, const rlm_tensor *g_t
  * elements.  Strides are multiples of 16 bytes (those of an extent of 1 are not
  * read) and ptr is 16-byte aligned; the rows of an output must not overlap one
  * another, nor any input.  State and its gradient are fp32 [B][D], contiguous.
+ * D is a multiple of 8 up to 2^20, B at most 65535, L at most 2^24.
+ *
+ * A token that is not finite (NaN, or an infinite x or state) makes its channel's later
+ * states not finite, infinities among them NaN; g of +-infinity is exact (keep, forget).
  *
  * lengths (nullable): int32 [B] on the device; row b's tokens from lengths[b] on are
  * padding (values outside 0..L are clamped): x, g and dy are not read there, y, dx and

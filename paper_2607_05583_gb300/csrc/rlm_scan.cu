@@ -181,9 +181,8 @@ __device__ __forceinline__ void wait_full(uint32_t bar, uint32_t parity, bool &g
 
 // One wave's exchange by its state warp: sends this tile's run `mine` (held by every lane of a
 // pair) to all members and returns the composition of the tiles before it (*pre) and of the
-// whole wave.  A member sends wave w + 4 into the place of wave w once its data warps have
-// passed wave w + 2, which took this CTA's run of wave w + 2, sent by the warp that read wave w
-// just before.
+// whole wave.  A member's warp sends wave w + 4 into the place of wave w after its own wave
+// w + 2, which took this CTA's run of wave w + 2, sent by the warp that read wave w just before.
 template <int P>
 __device__ __forceinline__ void exchange(Run mine, Peers<P> &peers, int wave, int seg, int nseg, int cp, bool &gave_up,
                                          Run *pre, Run *all) {
