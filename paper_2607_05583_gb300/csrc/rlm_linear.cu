@@ -915,6 +915,7 @@ size_t linear_ws_bytes(int64_t R, int64_t K, int64_t N) {
 namespace {
 int dz_rows(int64_t R, int64_t N) {
     int rows = 128;
+    if (R <= 64) return rows;               // one block of rows: its sums are dbias, without a second kernel
     while (rows > 16 && ((R + rows - 1) / rows) * ((N + 255) / 256) < 8 * sm_count()) rows /= 2;
     return rows;
 }
@@ -982,7 +983,7 @@ cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm
             at += round256((size_t)R * N * 2);
             dz = {a.dz, N};
         }
-        if (dbias) sums = a.part = reinterpret_cast<float *>(at);
+        if (dbias) sums = a.part = blocks > 1 ? reinterpret_cast<float *>(at) : dbias;
         at += round256((size_t)blocks * N * sizeof(float));
         auto *fn = act_kind == RLM_ACT_SILU      ? k_dz<RLM_ACT_SILU>
                    : act_kind == RLM_ACT_GELU    ? k_dz<RLM_ACT_GELU>
@@ -1008,7 +1009,9 @@ cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm
         if (e != cudaSuccess) return e;
     }
     // Last: ahead of the products its few large blocks would hold up the first of them.
-    if (dbias) return launch_dependent(k_column_sum, dim3((unsigned)((N + 31) / 32)), 1024, 0, st, 1, sums, blocks, (int)N, dbias);
+    if (dbias && blocks > 1)
+        return launch_dependent(k_column_sum, dim3((unsigned)((N + 31) / 32)), 1024, 0, st, 1, sums, blocks, (int)N,
+                                dbias);
     return cudaSuccess;
 }
 
