@@ -14,7 +14,7 @@
 // before the state update, so they add no round trip to the step.
 //
 // Launch: programmatic dependent launch.  The kernel waits on the previous
-// grid (griddepcontrol.wait) before touching memory and lets the next step's
+// grid (griddepcontrol.wait) before reading memory and lets the next step's
 // grid be scheduled (right after the wait; for the batched plain step, before
 // it), which hides most of the per-step launch latency when decode steps are
 // issued back to back or captured in a graph.
@@ -40,9 +40,13 @@ struct MixStep {
     int K;
 };
 
-// Plain (coherent) load of the drive history, which every step rewrites.
+// The steps' kernels may be resident while kernels before them still write what they read (a token,
+// weights that an optimizer updates), so they read by plain, coherent loads behind the wait alone:
+// nothing through the read-only path, which __ldg and pointers to __restrict__ const take.
 __device__ __forceinline__ float as_float(float v) { return v; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ float coherent(const T *p) { return as_float(*p); }
 
 // One thread's share of the mixer step: the thread of rank g in its (b, d) group
 // (tpg threads) loads history entries j = g, g + tpg, ... (at most one when
@@ -65,14 +69,14 @@ __device__ __forceinline__ MixPart<T> mix_part(const MixStep<T> &m, int64_t b, i
     r.l = 0.0f;
     r.gate = 0.0f;
     r.sc = 0.0f;
-    if (m.g && g == 0) r.gate = ld_elem(m.g + bd);
+    if (m.g && g == 0) r.gate = coherent(m.g + bd);
     if (m.K > 0) {
         const float *w = m.conv_w + (int64_t)d * m.K;
         if (g == 0) {
             // Every load of the step is issued here, before the reductions.
             r.xr = x_t[bd];
-            r.sc = __ldg(m.scale + d);
-            r.l = __ldg(w) * as_float(r.xr);
+            r.sc = m.scale[d];
+            r.l = w[0] * as_float(r.xr);
         }
         const T *h = m.hist + b * (m.K - 1) * (int64_t)D + d;
 #pragma unroll
@@ -80,7 +84,7 @@ __device__ __forceinline__ MixPart<T> mix_part(const MixStep<T> &m, int64_t b, i
             const int j = g + i * tpg;              // entry j holds u_{t-(K-1-j)}
             if (j < m.K - 1) {
                 r.hv[i] = h[(int64_t)j * D];
-                r.l = fmaf(__ldg(w + (m.K - 1 - j)), as_float(r.hv[i]), r.l);
+                r.l = fmaf(w[m.K - 1 - j], as_float(r.hv[i]), r.l);
             }
         }
     }
@@ -141,8 +145,8 @@ __device__ __forceinline__ void pdl_launch_dependents() {
 // 11.1 us a step at B = 64, D = 2048, M = 16 against 10.6.
 template <typename T, int R, bool kMix>
 __global__ void __launch_bounds__(R * 32, 2048 / (R * 32)) k_decode_tile(
-    const T *__restrict__ x_t, T *__restrict__ y_t, int B, int D, int M, int log2_tpg,
-    float4 *__restrict__ s, const float4 *__restrict__ coef, MixStep<T> mix, bool late) {
+    const T *x_t, T *y_t, int B, int D, int M, int log2_tpg,
+    float4 *s, const float4 *coef, MixStep<T> mix, bool late) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int tpg = 1 << log2_tpg;
     const int g = lane & (tpg - 1);
@@ -169,9 +173,9 @@ __global__ void __launch_bounds__(R * 32, 2048 / (R * 32)) k_decode_tile(
     if (kMix && rowok) mp = mix_part(mix, (int64_t)b, d, bd, D, g, tpg, x_t);  // every rank, with or without modes
     float acc = 0.0f;
     if (on) {
-        const float4 c0 = __ldg(coef + d * M + 2 * g);
-        const float4 c1 = __ldg(coef + d * M + 2 * g + 1);
-        const float xv = ld_elem(x_t + bd);
+        const float4 c0 = coef[d * M + 2 * g];
+        const float4 c1 = coef[d * M + 2 * g + 1];
+        const float xv = coherent(x_t + bd);
         const int64_t si = (bd * M) / 2 + g;
         const float4 q = s[si];
         const float r0 = fmaf(c0.x, q.x, fmaf(-c0.y, q.y, xv));
@@ -200,8 +204,8 @@ __global__ void __launch_bounds__(R * 32, 2048 / (R * 32)) k_decode_tile(
 // Any M: each thread owns up to MPT modes, accessed as float2.
 template <typename T, bool kMix>
 __global__ void __launch_bounds__(kDecodeBlock) k_decode_any(
-    const T *__restrict__ x_t, T *__restrict__ y_t, int64_t BD, int D, int M, int log2_tpg,
-    int mpt, float2 *__restrict__ s, const float4 *__restrict__ coef, MixStep<T> mix) {
+    const T *x_t, T *y_t, int64_t BD, int D, int M, int log2_tpg,
+    int mpt, float2 *s, const float4 *coef, MixStep<T> mix) {
     const int64_t gid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     const int64_t bd = gid >> log2_tpg;
     const int g = (int)(gid & ((1 << log2_tpg) - 1));
@@ -215,11 +219,11 @@ __global__ void __launch_bounds__(kDecodeBlock) k_decode_any(
     if (kMix && bd < BD) mp = mix_part(mix, b, d, bd, D, g, tpg, x_t);
     float acc = 0.0f;
     if (bd < BD) {
-        const float xv = ld_elem(x_t + bd);
+        const float xv = coherent(x_t + bd);
         for (int j = 0; j < mpt; ++j) {
             const int m = g * mpt + j;
             if (m >= M) break;
-            const float4 cf = __ldg(coef + d * M + m);
+            const float4 cf = coef[d * M + m];
             const float2 st = s[bd * M + m];
             const float re = fmaf(cf.x, st.x, fmaf(-cf.y, st.y, xv));
             const float im = fmaf(cf.x, st.y, cf.y * st.x);
@@ -285,8 +289,9 @@ cudaError_t launch_pdl(Kern kern, dim3 grid, cudaStream_t st, Args... args) {
 // threads of a channel form one aligned shuffle group.  Phase 1 updates the
 // states and puts each channel's readout y_t[d] in shared memory (fp32); after
 // the block barrier, phase 2 forms (C y_t)[d], applies the gate and the local
-// path, shifts the history and writes z_t[d].  C depends on the parameters only,
-// so it is built before the wait.  H = 0: no coupling (the mixer step alone).
+// path, shifts the history and writes z_t[d].  C is built behind the wait like the
+// rest (an optimizer step may be writing c_raw until then), while the other loads are
+// in flight.  H = 0: no coupling (the mixer step alone).
 constexpr int kCoupledBlock = 512;
 constexpr int kCoupledIters = 4;               // mode pairs per thread
 constexpr int kCoupledMaxModesPerRow = 2 * kCoupledIters * kCoupledBlock;   // D * M <= 4096
@@ -294,13 +299,12 @@ constexpr int kHistMax = RLM_MAX_LOCAL_K - 1;
 
 template <typename T>
 __global__ void __launch_bounds__(kCoupledBlock, 1) k_decode_coupled(
-    const T *__restrict__ x_t, T *__restrict__ z_t, int D, int M, float4 *__restrict__ s,
-    const float4 *__restrict__ coef, MixStep<T> mix, const float *__restrict__ c_raw, float lam, int H) {
+    const T *x_t, T *z_t, int D, int M, float4 *s,
+    const float4 *coef, MixStep<T> mix, const float *c_raw, float lam, int H) {
     extern __shared__ __align__(16) float smf[];
     float *C = smf;                              // [H][H]
     float *ys = smf + ((H * H + 3) & ~3);        // [D]
     const int64_t b = blockIdx.x;
-    if (H > 0) build_coupling(C, c_raw, lam, H);
     pdl_wait();
     pdl_launch_dependents();
     const T *xb = x_t + b * D;
@@ -312,15 +316,15 @@ __global__ void __launch_bounds__(kCoupledBlock, 1) k_decode_coupled(
     T *hc = K > 1 ? mix.hist + b * (K - 1) * (int64_t)D + d2 : nullptr;   // used only when K > 1
     if (ch) {
         xraw = xb[d2];
-        if (mix.g) gv = ld_elem(mix.g + b * D + d2);
+        if (mix.g) gv = coherent(mix.g + b * D + d2);
         if (K > 0) {
-            sc = __ldg(mix.scale + d2);
-            w0 = __ldg(mix.conv_w + (int64_t)d2 * K);
+            sc = mix.scale[d2];
+            w0 = mix.conv_w[(int64_t)d2 * K];
 #pragma unroll
             for (int j = 0; j < kHistMax; ++j) {
                 if (j < K - 1) {
                     hv[j] = hc[(int64_t)j * D];
-                    wj[j] = __ldg(mix.conv_w + (int64_t)d2 * K + (K - 1 - j));
+                    wj[j] = mix.conv_w[(int64_t)d2 * K + (K - 1 - j)];
                 }
             }
         }
@@ -337,12 +341,13 @@ __global__ void __launch_bounds__(kCoupledBlock, 1) k_decode_coupled(
         const int i = (int)threadIdx.x + k * kCoupledBlock;
         const int d = i >> lp, g = i & (pairs - 1);
         if (i < n4) {
-            xv[k] = ld_elem(xb + d);
+            xv[k] = coherent(xb + d);
             stv[k] = sb[i];
-            c0v[k] = __ldg(coef + (int64_t)d * M + 2 * g);
-            c1v[k] = __ldg(coef + (int64_t)d * M + 2 * g + 1);
+            c0v[k] = coef[(int64_t)d * M + 2 * g];
+            c1v[k] = coef[(int64_t)d * M + 2 * g + 1];
         }
     }
+    if (H > 0) build_coupling(C, c_raw, lam, H);
     // ---- phase 1: every thread runs every iteration, so whole warps shuffle
 #pragma unroll
     for (int k = 0; k < kCoupledIters; ++k) {
