@@ -324,6 +324,7 @@ RLM_API rlm_status rlm_mixer_decode(const rlm_tensor *x_t, const rlm_tensor *g_t
  *
  * A token that is not finite (NaN, or an infinite x or state) makes its channel's later
  * states not finite, infinities among them NaN; g of +-infinity is exact (keep, forget).
+ * a and 1 - a are formed to fp32's accuracy at every g, the smaller of them 0 below 2^-126.
  *
  * lengths (nullable): int32 [B] on the device; row b's tokens from lengths[b] on are
  * padding (values outside 0..L are clamped): x, g and dy are not read there, y, dx and

@@ -2,9 +2,16 @@
 //
 //   a_t = sigma(g_t),  h_t = a_t h_{t-1} + i_t,  i_t = (1 - a_t) x_t (leak) or x_t
 //
-// per channel, with b_t = 1 - a_t = 1 / (1 + e^{g_t}) formed directly: gates sit near
-// a = 1 and 1 - a would lose b's leading bits.  The kernels keep b and use
-//   leak  h += b (x - h)          unit  h = (h + x) - b h
+// per channel.  The smaller of a and b = 1 - a is formed directly, b = 1 / (1 + e^g) where gates
+// are open and a = e^g b where they are closed: as a difference from 1 either would lose its
+// leading bits (2 % of the gradients at g = -15).  The kernels keep one number, q = -b or q = a,
+// whose sign says which, and
+//   a v = [q < 0] v + q v         b v = [q > 0] v - q v         a b = |q| (1 - |q|)
+//   leak  h = [q < 0 ? h : x] + q (h - x)         unit  h = x + a h
+// lose nothing at any gate, and keep and forget exactly where it saturates.  Where all gates of a
+// warp's runs have a > 1 / 32, q is -b and the selections go: they are two thirds of a token's
+// arithmetic (bf16, B = 4, L = 32768, D = 512, gates 2.5 + 1.5 N(0, 1): 86 and 132 us forward and
+// backward; gates -2.5 + 1.5 N(0, 1), where no warp is without a closed one: 125 and 188 us).
 //
 // A run of tokens maps the state by h -> A h + H (A the product of its a, H its end
 // state from zero), and runs compose: (A2, H2) o (A1, H1) = (A2 A1, A2 H1 + H2).
@@ -15,23 +22,23 @@
 // Bound by memory: 3 fields move in the forward pass and 5 in the backward pass, and
 // each is read once.  At the measured copy rate an SM has about 33 instructions for each
 // bf16 element of the forward pass, so the arithmetic runs on channel pairs as packed
-// fp32 (f32x2), with -b in place of b (all signs then fall into the fma).
+// fp32 (f32x2); the selections by q's sign go half by half.
 //
 // Tiles.  Eight data warps of a CTA cover P channel pairs (P = 4, 8, 16 or 32) by
 // 256 / P runs of kS = 8 tokens, a thread per run and pair.  A warp copies the rows
 // that its own threads need (16-byte cp.async, out-of-range rows and padding filled
 // with zeros) into a private ring of kStages tiles, so no barrier guards the data.
-// A thread composes its run (first pass), keeps -b in registers, and once it knows the
+// A thread composes its run (first pass), keeps q in registers, and once it knows the
 // state at the run's start walks the run again for the outputs (second pass).
 //
 // Two more warps turn runs into states, a tile each in turn.  A lane holds one channel pair
 // of 8 consecutive runs (64 tokens, one saved chunk): it composes them, scans across
 // lanes, adds the carry (which one warp hands the other) and gives every run its start
 // state.  The data warps work on other tiles meanwhile: the second pass of tile w follows
-// the first pass of tile w + 1, in the bf16 forward pass that of w + 2 (46 -> 44 us at B =
-// 4, L = 32768, D = 256; fp32 and the backward pass have no room for its rings).  x, needed
-// again then, and g, needed once, have rings of their own: two CTAs per SM in fp32 (73 ->
-// 66 us).  (One such warp took 3100 cycles a tile where a cluster shares a chain, half of
+// the first pass of tile w + 1 (that of w + 2 costs more, by the code of a third tile: 49
+// against 47 us in bf16 at B = 4, L = 32768, D = 256, 91 against 71 us without segments).  x,
+// needed again then, and g, needed once, have rings of their own: two CTAs per SM in fp32 (73
+// -> 66 us).  (One such warp took 3100 cycles a tile where a cluster shares a chain, half of
 // them the exchange, and bounded the kernel: 54 us at B = 4, L = 32768, D = 256.)
 //
 // Segments.  Few channels would leave SMs idle, so a cluster of nseg CTAs (2, 4 or 8)
@@ -43,13 +50,14 @@
 // no field is read twice.  Every wait is bounded.  The order of all products and sums is
 // fixed by the shape: results repeat bit for bit.
 //
-// Measured, forward and backward: bf16, B = 256, L = 512, D = 512, no segments, 68 and 107
-// us, 88 and 93 % of the copy rate; bf16, B = 4, L = 32768, 8 segments, 81 and 129 us with D =
-// 512 (73 and 77 %), 44 and 73 us with D = 256; fp32, D = 256, 66 and 110 us (90 %).  With
+// Measured, forward and backward, gates 2.5 + 1.5 N(0, 1): bf16, B = 256, L = 512, D = 512, no
+// segments, 71 and 110 us, 84 and 90 % of the copy rate; bf16, B = 4, L = 32768, 8 segments, 86
+// and 132 us with D = 512 (69 and 75 %), 47 and 73 us with D = 256; fp32, D = 256, 64 and 111 us.  With
 // segments the data warps' own latency bounds a wave (40 % of issue slots, a third of the
 // stalls at the hand-over).
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "rlm_device.cuh"
 #include "rlm_internal.h"
@@ -63,7 +71,7 @@ namespace {
 constexpr int kDataThreads = 256;
 constexpr int kThreads = kDataThreads + 64;         // and the two warps that turn runs into states
 constexpr int kS = 8;                               // tokens of a run
-constexpr int kBarRuns = 1, kBarStates = 4, kBarCarry = 7;      // named barriers: up to three by tile, three, two by parity
+constexpr int kBarRuns = 1, kBarStates = 3, kBarCarry = 5;      // named barriers, two each by a tile's parity
 constexpr int kHandOver = kDataThreads + 32;        // threads of the first two: the data warps and one state warp
 constexpr int kChunk = RLM_SCAN_CHUNK;              // tokens between saved states
 constexpr long long kWaitLimit = 4000000000ll;      // SM cycles: about 2 s
@@ -101,7 +109,11 @@ struct ScanArgs {
     int L, D, groups, nseg, ntiles, nchunks;
 };
 
-constexpr f32x2 kOne = 0x3f8000003f800000ull, kMinus = 0xbf800000bf800000ull;
+constexpr f32x2 kOne = 0x3f8000003f800000ull, kMinus = 0xbf800000bf800000ull, kKeep = 0x8000000080000000ull;   // (q of a = 1)
+
+// Gates whose b passes this (g below -3.43) count as closed: v - b v is off by 2^-24 v, so by less
+// than 2^-19 of a v short of it.
+constexpr float kClosed = 31.f / 32.f;
 
 // A run of two channels: h -> A h + H.
 struct alignas(16) Run {
@@ -346,36 +358,83 @@ __device__ __forceinline__ void copies_wait() {
     __syncwarp();
 }
 
-// -b = -1 / (1 + e^g); g = +inf gives -0, -inf gives -1.
+__device__ __forceinline__ float exp2_approx(float v) {
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v));
+    return e;
+}
+__device__ __forceinline__ float reciprocal_approx(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+constexpr f32x2 kLog2e = 0x3fb8aa3b3fb8aa3bull;
+
 template <typename T>
-__device__ __forceinline__ f32x2 minus_rest(f32x2 g) {
-    float2 e;
+__device__ __forceinline__ f32x2 exponential(f32x2 g) {
     if constexpr (sizeof(T) == 2) {
-        const float2 p = unpack(mul2(g, 0x3fb8aa3b3fb8aa3bull));       // log2(e)
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(p.x));
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(p.y));
-    } else {
-        const float2 p = unpack(g);
-        e = make_float2(expf(p.x), expf(p.y));
+        const float2 p = unpack(mul2(g, kLog2e));
+        return pack(make_float2(exp2_approx(p.x), exp2_approx(p.y)));
     }
-    const float2 d = unpack(fma2(pack(e), kMinus, kMinus));
-    float2 r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(d.x));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(d.y));
-    return pack(r);
+    const float2 p = unpack(g);
+    return pack(make_float2(expf(p.x), expf(p.y)));
+}
+// -b = -1 / (1 + e), e = e^g: q where gates are not closed; g = +inf gives -0.
+__device__ __forceinline__ f32x2 minus_rest(f32x2 e) {
+    const float2 d = unpack(fma2(e, kMinus, kMinus));
+    return pack(make_float2(reciprocal_approx(d.x), reciprocal_approx(d.y)));
+}
+// q of any gate: a = e b where b > 1 / 2 (g = -inf gives +0; a below 2^-126 is 0), else -b.
+__device__ __forceinline__ f32x2 smaller(f32x2 e, f32x2 minus_b) {
+    f32x2 s;
+    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(s) : "l"(e), "l"(minus_b ^ kKeep));
+    const float2 a = unpack(s), r = unpack(minus_b);
+    return pack(make_float2(r.x < -0.5f ? a.x : r.x, r.y < -0.5f ? a.y : r.y));
 }
 
-// One token: h - b (h - x) or (h + x) - b h; nb = -b.
-template <bool kLeak>
-__device__ __forceinline__ f32x2 advance(f32x2 h, f32x2 nb, f32x2 x) {
-    return kLeak ? fma2(nb, fma2(x, kMinus, h), h) : fma2(nb, h, add2(h, x));
+// A run's q, and whether all of the warp's runs are free of closed gates.
+struct Gates {
+    f32x2 q[kS];
+    bool open;
+};
+template <typename T, typename Value>
+__device__ __forceinline__ void gates_of(Gates &t, Value g) {
+    float low = 0.f;
+#pragma unroll
+    for (int i = 0; i < kS; ++i) {
+        t.q[i] = minus_rest(exponential<T>(g(i)));
+        const float2 v = unpack(t.q[i]);
+        low = fminf(low, fminf(v.x, v.y));
+    }
+    t.open = !__any_sync(~0u, low < -kClosed);
+    if (!t.open) {
+#pragma unroll
+        for (int i = 0; i < kS; ++i) t.q[i] = smaller(exponential<T>(g(i)), t.q[i]);
+    }
 }
 
-// first(0), first(1), second(0), first(2), second(1), ...: each pass's -b in one of two
+// Half by half: v where q < 0 (-0 among them), else o.
+__device__ __forceinline__ f32x2 where_open(f32x2 q, f32x2 v, f32x2 o) {
+    const float2 s = unpack(q), a = unpack(v), b = unpack(o);
+    return pack(make_float2(__float_as_int(s.x) < 0 ? a.x : b.x, __float_as_int(s.y) < 0 ? a.y : b.y));
+}
+// a v; kOpen: q is -b throughout.
+template <bool kOpen>
+__device__ __forceinline__ f32x2 decayed(f32x2 q, f32x2 v) { return fma2(q, v, kOpen ? v : where_open(q, v, 0)); }
+// One token.
+template <bool kLeak, bool kOpen>
+__device__ __forceinline__ f32x2 advance(f32x2 h, f32x2 q, f32x2 x) {
+    if (kLeak) return fma2(q, fma2(x, kMinus, h), kOpen ? h : where_open(q, h, x));
+    return fma2(q, h, add2(x, kOpen ? h : where_open(q, h, 0)));
+}
+template <bool kOpen>
+using Open = std::integral_constant<bool, kOpen>;
+
+// first(0), first(1), second(0), first(2), second(1), ...: each pass's q in one of two
 // register arrays.
 template <typename First, typename Second>
 __device__ __forceinline__ void two_passes(int n, First first, Second second) {
-    f32x2 even[kS], odd[kS];
+    Gates even, odd;
     first(0, even);
     for (int k = 1;; k += 2) {
         if (k < n) first(k, odd);
@@ -387,39 +446,16 @@ __device__ __forceinline__ void two_passes(int n, First first, Second second) {
     }
 }
 
-// The same with a lag of two tiles, for the forward pass in bf16 (its registers and ring have room;
-// 3 to 5 % where a cluster shares a chain).
-template <typename First, typename Second>
-__device__ __forceinline__ void three_passes(int n, First first, Second second) {
-    f32x2 n0[kS], n1[kS], n2[kS];
-    first(0, n0);
-    if (n > 1) first(1, n1);
-    for (int k = 2;; k += 3) {
-        if (k < n) first(k, n2);
-        second(k - 2, n0);
-        if (k - 1 >= n) return;
-        if (k + 1 < n) first(k + 1, n0);
-        second(k - 1, n1);
-        if (k >= n) return;
-        if (k + 2 < n) first(k + 2, n1);
-        second(k, n2);
-        if (k + 1 >= n) return;
-    }
-}
-
 // Resident CTAs per SM: what the rings leave room for.
 template <typename T>
 constexpr int kBwdPerSm = sizeof(T) == 2 ? 2 : 1;
 
 // ----------------------------------------------------------------- forward
-// Tiles between a tile's first and second pass, and tiles of g (needed until the first) and of x
-// (until the second) in the ring.
-template <typename T>
-constexpr int kLag = sizeof(T) == 2 ? 2 : 1;
+// Tiles of g (needed until the first pass) and of x (until the second, a tile later) in the ring.
 template <typename T>
 constexpr int kGStages = sizeof(T) == 2 ? 3 : 2;
 template <typename T>
-constexpr int kXStages = kGStages<T> + kLag<T>;
+constexpr int kXStages = kGStages<T> + 1;
 template <typename T, int kLog2P>
 using XRing = Ring<T, 1, kXStages<T>, kLog2P>;
 template <typename T, int kLog2P>
@@ -429,9 +465,9 @@ template <typename T, bool kLeak, int kLog2P>
 __global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> a) {
     extern __shared__ __align__(16) unsigned char ring_mem[];
     __shared__ Peers<1 << kLog2P> peers;
-    constexpr int X = kXStages<T>, G = kGStages<T>, NB = kLag<T> + 1;
-    __shared__ Run runs[NB][kDataThreads];
-    __shared__ f32x2 states[NB][kDataThreads], carries[2][32];
+    constexpr int X = kXStages<T>, G = kGStages<T>;
+    __shared__ Run runs[2][kDataThreads];
+    __shared__ f32x2 states[2][kDataThreads], carries[2][32];
     constexpr int P = 1 << kLog2P;
     Where w = where<kLog2P>(a);
     open_peers(peers, a.nseg);
@@ -445,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> 
         if (a.state_in && w.on) carry = pack(*reinterpret_cast<const float2 *>(a.state_in + (int64_t)w.row * a.D + w.c));
         bool gave_up = false;
         for (int k = me; k < w.n; k += 2) {
-            const int par = k % NB, tile = k * a.nseg + w.seg;
+            const int par = k & 1, tile = k * a.nseg + w.seg;
             bar_sync(kBarRuns + par);
             Run f = identity();
 #pragma unroll
@@ -486,47 +522,52 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> 
     };
 #pragma unroll
     for (int k = 0; k < G; ++k) copy(k);
-    auto first = [&](int k, f32x2 (&nb)[kS]) {
-        // Copies are one group a tile, asked for G at the start, one after each of the first kLag first
-        // passes and then one after each second pass: always G are open or to come, tile k the first.
+    auto first = [&](int k, Gates &t) {
+        // Copies are one group a tile, asked for G at the start, one after the first tile's first pass and
+        // then one after each second pass: always G are open or to come, tile k the first.
         copies_wait<G - 1>();
         const int t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
-#pragma unroll
-        for (int i = 0; i < kS; ++i) nb[i] = minus_rest<T>(gs.value(k % G, 0, i));
+        gates_of<T>(t, [&](int i) { return gs.value(k % G, 0, i); });
         if (t0 + kS > w.len) {                          // past the end: the identity (x is 0 there)
 #pragma unroll
             for (int i = 0; i < kS; ++i)
-                if (t0 + i >= w.len) nb[i] = 0;
+                if (t0 + i >= w.len) t.q[i] = kKeep;
         }
         f32x2 A = kOne, H = 0;
-#pragma unroll
-        for (int i = 0; i < kS; ++i) {
-            A = fma2(nb[i], A, A);
-            H = advance<kLeak>(H, nb[i], xs.value(k % X, 0, i));
-        }
-        runs[k % NB][threadIdx.x] = {A, H};
-        bar_arrive(kBarRuns + k % NB);
-        if (k < kLag<T>) {
-            __syncwarp();
-            copy(G + k);
-        }
-    };
-    auto second = [&](int k, const f32x2 (&nb)[kS]) {
-        const int t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
-        bar_sync(kBarStates + k % NB);
-        f32x2 h = states[k % NB][threadIdx.x];
-        T *out = yp + (int64_t)t0 * a.y_l;
-        if (w.on && t0 + kS <= w.len) {
+        auto run = [&](auto open) {
+            constexpr bool kOpen = decltype(open)::value;
 #pragma unroll
             for (int i = 0; i < kS; ++i) {
-                h = advance<kLeak>(h, nb[i], xs.value(k % X, 0, i));
-                Pair<T>::store(out, unpack(h));
-                out += a.y_l;
+                A = decayed<kOpen>(t.q[i], A);
+                H = advance<kLeak, kOpen>(H, t.q[i], xs.value(k % X, 0, i));
+            }
+        };
+        if (t.open) run(Open<true>{}); else run(Open<false>{});
+        runs[k & 1][threadIdx.x] = {A, H};
+        bar_arrive(kBarRuns + (k & 1));
+        if (k == 0) {
+            __syncwarp();
+            copy(G);
+        }
+    };
+    auto second = [&](int k, const Gates &t) {
+        const int t0 = (k * a.nseg + w.seg) * w.tile_tokens + w.sc * kS;
+        bar_sync(kBarStates + (k & 1));
+        f32x2 h = states[k & 1][threadIdx.x];
+        T *out = yp + (int64_t)t0 * a.y_l;
+        if (t.open && t0 + kS <= w.len) {
+            if (w.on) {
+#pragma unroll
+                for (int i = 0; i < kS; ++i) {
+                    h = advance<kLeak, true>(h, t.q[i], xs.value(k % X, 0, i));
+                    Pair<T>::store(out, unpack(h));
+                    out += a.y_l;
+                }
             }
         } else if (w.on) {
 #pragma unroll
             for (int i = 0; i < kS; ++i) {
-                h = advance<kLeak>(h, nb[i], xs.value(k % X, 0, i));
+                h = advance<kLeak, false>(h, t.q[i], xs.value(k % X, 0, i));
                 if (t0 + i < a.L) Pair<T>::store(out, t0 + i < w.len ? unpack(h) : make_float2(0.f, 0.f));
                 out += a.y_l;
             }
@@ -534,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_forward(const ScanArgs<T> 
         __syncwarp();
         copy(k + X);            // x into the stage that this pass has just left
     };
-    if constexpr (kLag<T> == 2) three_passes(w.n, first, second); else two_passes(w.n, first, second);
+    two_passes(w.n, first, second);
     close_peers(a.nseg);
 }
 
@@ -547,7 +588,7 @@ using BwdRing = Ring<T, 3, kBwdStages<T>, kLog2P>;          // fields: x, g, dy
 template <typename T, bool kLeak, int kLog2P>
 __global__ void __launch_bounds__(kThreads, kBwdPerSm<T>) k_scan_backward(const ScanArgs<T> a) {
     extern __shared__ __align__(16) unsigned char ring_mem[];
-    // Gradients are carried negated: with -b at hand, b G = (-b)(-G) needs no sign.
+    // Gradients are carried negated: the signs of b G and of a b G then fall into the fma.
     __shared__ Peers<1 << kLog2P> peers;
     __shared__ Run runs[2][kDataThreads];
     __shared__ f32x2 ends[2][kDataThreads];         // a run's -C from a zero C after it; then its -C
@@ -620,73 +661,85 @@ __global__ void __launch_bounds__(kThreads, kBwdPerSm<T>) k_scan_backward(const 
     };
 #pragma unroll
     for (int k = 0; k < ST; ++k) copy(k);
-    auto first = [&](int k, f32x2 (&nb)[kS]) {
+    auto first = [&](int k, Gates &t) {
         if (k == 0) copies_wait<ST - 1>(); else copies_wait<ST - 2>();
         const int st = k % ST, t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens + w.sc * kS;
-#pragma unroll
-        for (int i = 0; i < kS; ++i) nb[i] = minus_rest<T>(ring.value(st, 1, i));
+        gates_of<T>(t, [&](int i) { return ring.value(st, 1, i); });
         if (t0 < 0 || t0 + kS > w.len) {
 #pragma unroll
             for (int i = 0; i < kS; ++i)
-                if (t0 < 0 || t0 + i >= w.len) nb[i] = 0;
+                if (t0 < 0 || t0 + i >= w.len) t.q[i] = kKeep;
         }
         f32x2 A = kOne, H = 0, R = 0;
+        auto run = [&](auto open) {
+            constexpr bool kOpen = decltype(open)::value;
 #pragma unroll
-        for (int i = 0; i < kS; ++i) {
-            A = fma2(nb[i], A, A);
-            H = advance<kLeak>(H, nb[i], ring.value(st, 0, i));
-        }
+            for (int i = 0; i < kS; ++i) {
+                A = decayed<kOpen>(t.q[i], A);
+                H = advance<kLeak, kOpen>(H, t.q[i], ring.value(st, 0, i));
+            }
 #pragma unroll
-        for (int i = kS - 1; i >= 0; --i) {
-            const f32x2 G = fma2(ring.value(st, 2, i), kMinus, R);
-            R = fma2(nb[i], G, G);
-        }
+            for (int i = kS - 1; i >= 0; --i) R = decayed<kOpen>(t.q[i], fma2(ring.value(st, 2, i), kMinus, R));
+        };
+        if (t.open) run(Open<true>{}); else run(Open<false>{});
         runs[k & 1][threadIdx.x] = {A, H};
         ends[k & 1][threadIdx.x] = R;
         bar_arrive(kBarRuns + (k & 1));
     };
-    auto second = [&](int k, const f32x2 (&nb)[kS]) {
+    auto second = [&](int k, const Gates &t) {
         const int st = k % ST, t0 = (a.ntiles - 1 - (k * a.nseg + w.seg)) * w.tile_tokens + w.sc * kS;
         bar_sync(kBarStates + (k & 1));
         f32x2 h = states[k & 1][threadIdx.x], C = ends[k & 1][threadIdx.x];
-        f32x2 v[kS];                                    // h_{t-1} - x or h_{t-1}
-#pragma unroll
-        for (int i = 0; i < kS; ++i) {
-            const f32x2 x = ring.value(st, 0, i);
-            v[i] = kLeak ? fma2(x, kMinus, h) : h;
-            h = advance<kLeak>(h, nb[i], x);
-        }
         T *ox = dxp + (int64_t)(t0 + kS - 1) * a.dx_l, *og = dgp + (int64_t)(t0 + kS - 1) * a.dg_l;
-        auto token = [&](int i, float2 &vx, float2 &vg) {
-            const f32x2 G = fma2(ring.value(st, 2, i), kMinus, C);
-            C = fma2(nb[i], G, G);                      // a G
-            vx = unpack(mul2(kLeak ? nb[i] : kMinus, G));
-            vg = unpack(mul2(mul2(C, nb[i]), v[i]));
-        };
-        if (w.on && t0 >= 0 && t0 + kS <= w.len) {
+        auto run = [&](auto open) {
+            constexpr bool kOpen = decltype(open)::value;
+            f32x2 v[kS];                                // h_{t-1} - x or h_{t-1}
 #pragma unroll
-            for (int i = kS - 1; i >= 0; --i) {
-                float2 vx, vg;
-                token(i, vx, vg);
-                Pair<T>::store(ox, vx);
-                Pair<T>::store(og, vg);
-                ox -= a.dx_l;
-                og -= a.dg_l;
+            for (int i = 0; i < kS; ++i) {
+                const f32x2 x = ring.value(st, 0, i);
+                v[i] = kLeak ? fma2(x, kMinus, h) : h;
+                h = advance<kLeak, kOpen>(h, t.q[i], x);
             }
-        } else if (w.on && t0 >= 0) {
+            auto token = [&](int i, float2 &vx, float2 &vg) {
+                const f32x2 q = t.q[i], G = fma2(ring.value(st, 2, i), kMinus, C);
+                if (kOpen) {
+                    C = fma2(q, G, G);                  // a G
+                    vx = unpack(mul2(kLeak ? q : kMinus, G));
+                    vg = unpack(mul2(mul2(C, q), v[i]));
+                } else {
+                    const f32x2 kept = where_open(q, G, 0);
+                    C = fma2(q, G, kept);
+                    vx = unpack(kLeak ? fma2(q, G, fma2(G, kMinus, kept)) : mul2(G, kMinus));
+                    const f32x2 less = q | kKeep, n = mul2(less, mul2(G, v[i]));        // -|q|
+                    vg = unpack(fma2(less, n, n));
+                }
+            };
+            if (w.on && t0 >= 0 && t0 + kS <= w.len) {
 #pragma unroll
-            for (int i = kS - 1; i >= 0; --i) {
-                float2 vx, vg;
-                token(i, vx, vg);
-                if (t0 + i >= w.len) vx = vg = make_float2(0.f, 0.f);
-                if (t0 + i < a.L) {
+                for (int i = kS - 1; i >= 0; --i) {
+                    float2 vx, vg;
+                    token(i, vx, vg);
                     Pair<T>::store(ox, vx);
                     Pair<T>::store(og, vg);
+                    ox -= a.dx_l;
+                    og -= a.dg_l;
                 }
-                ox -= a.dx_l;
-                og -= a.dg_l;
+            } else if (w.on && t0 >= 0) {
+#pragma unroll
+                for (int i = kS - 1; i >= 0; --i) {
+                    float2 vx, vg;
+                    token(i, vx, vg);
+                    if (t0 + i >= w.len) vx = vg = make_float2(0.f, 0.f);
+                    if (t0 + i < a.L) {
+                        Pair<T>::store(ox, vx);
+                        Pair<T>::store(og, vg);
+                    }
+                    ox -= a.dx_l;
+                    og -= a.dg_l;
+                }
             }
-        }
+        };
+        if (t.open) run(Open<true>{}); else run(Open<false>{});
         __syncwarp();
         copy(k + ST);
     };
@@ -715,7 +768,8 @@ __global__ void __launch_bounds__(256) k_scan_step(const T *x, const T *g, T *y,
         const float2 gv = Pair<T>::value(*reinterpret_cast<const Raw *>(g + row * g_b + c));
         const float2 xv = Pair<T>::value(*reinterpret_cast<const Raw *>(x + row * x_b + c));
         float2 *sp = reinterpret_cast<float2 *>(state) + i;
-        const float2 h = unpack(advance<kLeak>(pack(*sp), minus_rest<T>(pack(gv)), pack(xv)));
+        const f32x2 e = exponential<T>(pack(gv)), q = smaller(e, minus_rest(e));
+        const float2 h = unpack(advance<kLeak, false>(pack(*sp), q, pack(xv)));
         *sp = h;
         Pair<T>::store(y + row * y_b + c, h);
     }
