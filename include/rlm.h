@@ -419,15 +419,25 @@ RLM_API size_t rlm_linear_backward_workspace_size(int64_t R, int64_t K, int64_t 
  *   p = p (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  *
  * Weights and gradients are RLM_F32 or RLM_BF16 (one type each for the call); moments are
- * fp32 (bits = 32) or 8-bit floats (bits = 8).  With a master copy (bf16 weights only) the
+ * fp32 (bits = 32) or 8-bit floats (bits = 8, or 8 | RLM_ADAMW_DRAW).  With a master copy (bf16 weights only) the
  * step reads and writes the fp32 master and the weight receives it rounded; without one,
  * bf16 weights are rounded to nearest at every step.
  *
  * 8-bit moments: exp_avg holds m and exp_avg_sq holds sqrt(v) as E4M3 codes (4 exponent
  * bits, 3 mantissa bits, one byte each) of blocks of RLM_ADAMW_BLOCK values; value = code *
  * scale of its block, the scale a power of two.  All-zero codes with any finite scale are
- * zero moments.  A nonzero sqrt(v) is never rounded to zero. */
+ * zero moments.  A nonzero sqrt(v) is never rounded to zero.  How the codes are rounded:
+ *   bits = 8                    to nearest.  A moment that a step moves by less than half a code
+ *       (codes lie 6 to 12 % apart) then stays where it is: sqrt(v) never decays at any usual
+ *       beta2, and small gradients never enter it.  For single steps from given moments.
+ *   bits = 8 | RLM_ADAMW_DRAW   for training: a moment that a step moves by less than 3/4 of a
+ *       code goes up or down by chance, with the right mean, so that over many steps it follows
+ *       the 32-bit one; larger changes go to the nearest code.  The draw is a hash of step, the
+ *       tensor's place in the call and the value's index: the same call gives the same codes (a
+ *       captured call replays those of its step).  m stays zero under gradients below 2^-14 of
+ *       its block's largest m, unless a step's change alone is nearer to the smallest code. */
 #define RLM_ADAMW_BLOCK 256
+#define RLM_ADAMW_DRAW 0x100
 
 typedef struct {
     void *param;
@@ -446,8 +456,8 @@ typedef struct {
 /* tensors: HOST array of count entries (>= 1), read before the call returns; buffers of a
  * call must not overlap.  Any n and any element alignment; 16-byte aligned buffers (8 for
  * codes) move fastest.  grad_scale: nullable device scalar s (1 if NULL); if it is not
- * finite the step changes nothing.  Non-finite gradients are not looked for.  One launch
- * per 400 tensors, no workspace. */
+ * finite the step changes nothing.  Non-finite gradients are not looked for (an infinite one
+ * makes its block's 8-bit sqrt(v) infinite).  One launch per 400 tensors, no workspace. */
 RLM_API rlm_status rlm_adamw_step(const rlm_adamw_tensor *tensors, int count, rlm_dtype param, rlm_dtype grad, int bits,
                                   const rlm_adamw_hyper *hyper, const float *grad_scale, const rlm_launch *launch);
 

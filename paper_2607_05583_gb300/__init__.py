@@ -686,16 +686,22 @@ def rlm_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, dx: 
 
 # --------------------------------------------------------------- optimizer
 ADAMW_BLOCK = 256       # RLM_ADAMW_BLOCK: values that share a scale of the 8-bit moments
+ADAMW_DRAW = 0x100      # RLM_ADAMW_DRAW: 8-bit codes rounded by draw
 
 
 @dataclass
 class AdamState:
     """Moments of one tensor of n values: m and v float32 [n], or (8 bits) codes float8_e4m3fn
-    [n] of m and of sqrt(v) with the scales float32 [ceil(n / 256)] of their blocks."""
+    [n] of m and of sqrt(v) with the scales float32 [ceil(n / 256)] of their blocks.
+
+    ``draw`` says how a step rounds the codes: by draw, so that over many steps they follow the
+    32-bit moments (what ``zeros`` sets, for training), or to nearest, where a change of less
+    than half a code is lost (single steps from given moments)."""
     m: torch.Tensor
     v: torch.Tensor
     m_scale: torch.Tensor | None = None
     v_scale: torch.Tensor | None = None
+    draw: bool = False
 
     @classmethod
     def zeros(cls, param: torch.Tensor, bits: int = 32):
@@ -706,7 +712,7 @@ class AdamState:
             raise ValueError(f"bits must be 8 or 32, got {bits}")
         k = -(-n // ADAMW_BLOCK)
         return cls(*(torch.zeros(n, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn) for _ in range(2)),
-                   *(torch.ones(k, dtype=torch.float32, device=dev) for _ in range(2)))
+                   *(torch.ones(k, dtype=torch.float32, device=dev) for _ in range(2)), draw=True)
 
     @property
     def bits(self) -> int:
@@ -733,6 +739,9 @@ class AdamGroup:
             raise ValueError("AdamGroup needs as many grads, states (and masters) as params, and at least one")
         self.tensors = params, grads, states, masters
         self.param_dtype, self.grad_dtype, self.bits = params[0].dtype, grads[0].dtype, states[0].bits
+        self.draw = bool(states[0].draw) and self.bits == 8
+        if self.bits == 8 and any(bool(s.draw) != self.draw for s in states):
+            raise ValueError("the states of a group are all rounded by draw or all to nearest")
         if self.param_dtype not in _DT or self.grad_dtype not in _DT:
             raise ValueError(f"weights are {self.param_dtype}, gradients {self.grad_dtype}: need float32 or bfloat16")
         self._c = (_AdamTensor * len(params))()
@@ -766,6 +775,6 @@ def rlm_adamw_step(group: AdamGroup, step: int, lr: float, beta1: float = 0.9, b
         raise ValueError("grad_scale must be a CUDA float32 scalar")
     h = _AdamHyper(lr, beta1, beta2, eps, weight_decay, step)
     _check(load_library().rlm_adamw_step(group._c, len(group._c), _DT[group.param_dtype], _DT[group.grad_dtype],
-                                         group.bits, h,
+                                         group.bits | (ADAMW_DRAW if group.draw else 0), h,
                                          grad_scale.data_ptr() if grad_scale is not None else None,
                                          _launch(stream, None)), "rlm_adamw_step")

@@ -13,11 +13,23 @@
 //
 // 8-bit moments.  Blocks of 256 values share a power-of-two scale 2^(e - 8), 2^e the first
 // power of two above the block's largest magnitude, so scaling is exact; the values are
-// kept as 8-bit floats with 3 mantissa bits (relative step 2^-3 over 17 binades), m signed
+// kept as 8-bit floats with 3 mantissa bits (relative step 2^-3 over 14 binades, and three more
+// at the fixed step 2^-9 of the scale), m signed
 // and sqrt(v) in place of v, which halves the binades v needs.  A sqrt(v) that would round
 // to zero is kept at the smallest code: a zero under a nonzero m would let the step grow
 // to m / eps.  The step itself uses the moments before they are rounded.  A warp's 32 x 8
 // values are one block.
+//
+// Rounding the codes.  A step moves sqrt(v) by at most 1 - sqrt(beta2) of itself, 2.5 % at 0.95
+// and 0.05 % at 0.999, and codes lie 6 to 12 % apart: rounded to nearest it goes back to the code
+// that it came from, and never decays.  By draw (kDraw), a value less than 3/4 of a code from the
+// one it came from goes up or down by chance, with the mean that it has; over many steps the
+// moments then follow the 32-bit ones (N(0, 1) gradients, 1000 steps: mean sqrt(v) within 1.5 %;
+// with nearest codes 2.0 times too large at beta2 = 0.95 and 0.4 at 0.999).  The draw is a hash of
+// the step, the tensor's place and the value's index: the same call gives the same codes.  Larger
+// changes go to the nearest code, whose error is half of the draw's.  A zero m is left by chance
+// where the gradient is one that m could hold to all its bits (2^-14 of the block's largest m),
+// below that only by a change that is nearer to the smallest code.
 //
 // The products and sums of m and v are rounded one by one: an 8-bit m and a bf16 gradient have
 // few bits, so 0.9 m + 0.1 g meets the ties of the 4-bit codes about once in 500 values, and a
@@ -25,8 +37,9 @@
 // Scalar instructions, because mul and add on packed pairs were fused.  sqrt and the
 // quotient of the step are the approximate instructions (2^-22): with the exact sequences
 // the 8-bit step, which its instructions bound (82 % of issue slots), took 379 us at 120 M
-// values against 211 us now and 178 us for its bytes.  The 32-bit steps run at the copy
-// rate: 478 us for 3.36 GB (fp32, and bf16 with masters), 7.0 TB/s.
+// values against 211 us now (bf16 weights, codes to nearest) and 178 us for its bytes.  By draw it
+// takes 336 us (361 with fp32 weights, 374 with masters): some 30 instructions a value more.  The
+// 32-bit steps run at the copy rate: 478 us for 3.36 GB (fp32, and bf16 with masters), 7.0 TB/s.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -60,6 +73,8 @@ struct StepArgs {
     const float *grad_scale;        // nullable
     float beta1, one_minus_beta1, beta2, one_minus_beta2, inv_sqrt_bc2, eps, decay, step_size;
     int count;
+    uint32_t draw, before;                  // 8-bit moments: hash of the step; the call's tensors in earlier launches
+    float leave_zero;                       // (1 - beta1) of the smallest normal code
     unsigned first[kMaxTensors + 1];        // chunks before each tensor
     Entry t[kMaxTensors];
 };
@@ -90,14 +105,10 @@ struct Eight {
 struct Codes {
     static constexpr int kWords = 2;
     uint32_t w[2];
-    __device__ __forceinline__ void get(float (&v)[8]) const {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> 16 * (i & 1)), __NV_E4M3);
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-            v[2 * i] = f.x;
-            v[2 * i + 1] = f.y;
-        }
+    // Values i and i + 1.
+    __device__ __forceinline__ f32x2 two(int i) const {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 2] >> 8 * (i & 3)), __NV_E4M3);
+        return pack(__half22float2(*reinterpret_cast<const __half2 *>(&h)));
     }
     __device__ __forceinline__ void set(const float (&v)[8]) {
         w[0] = w[1] = 0u;
@@ -179,6 +190,23 @@ __device__ __forceinline__ void unpair(f32x2 p, float *v) {
     v[1] = f.y;
 }
 
+// 32 bits that look random, of 32 (multipliers: fractional digits of the roots of 2 and 3).
+__host__ __device__ __forceinline__ uint32_t scramble(uint32_t x) {
+    x = (x ^ (x >> 16)) * 0x6A09E667u;
+    x = (x ^ (x >> 15)) * 0xBB67AE85u;
+    return x ^ (x >> 16);
+}
+// Rounding to codes is done on fp32 numbers 2^-120 times those that the codes stand for: the bits
+// from 20 on are then the code, below its normal range too, and neighbours are 2^20 apart.
+constexpr float kDown = 0x1p-120f, kUp = 0x1p120f;
+constexpr int kCode = 1 << 20, kNear = 3 * kCode / 4;
+// Bits of the code that x goes to: by the draw (0 .. 2^20 - 1), or the nearest.  (NaN stays NaN.)
+__device__ __forceinline__ int to_code(int x, bool by_draw, uint32_t draw) {
+    return (min(x, 0x7ff00000) + (by_draw ? (int)draw : kCode / 2)) & -kCode;
+}
+// Whether two numbers of one sign are less than 3/4 of a code apart.
+__device__ __forceinline__ bool near_code(int a, int b) { return (unsigned)(a - b + kNear) < 2u * kNear; }
+
 // What a thread reads of 8 values.
 template <typename P, typename G, bool kMaster, bool k8Bit>
 struct Reads {
@@ -191,10 +219,17 @@ struct Reads {
 };
 
 // The 8-bit step has more arithmetic to hide its loads behind, so its registers are held down
-// for more warps: 246 -> 211 us (bf16 weights), 291 -> 276 us (fp32) and 297 -> 281 us
-// (masters) at 120 M values; the 32-bit step loses by it.
-template <typename P, typename G, bool kMaster, bool k8Bit>
-__global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_adamw(const __grid_constant__ StepArgs a) {
+// for more warps.  To nearest: 246 -> 211 us (bf16 weights), 291 -> 276 us (fp32) and 297 -> 281 us
+// (masters) at 120 M values.  By draw: 420 us with three blocks per SM, 369 with four, 336 with five,
+// 342 with six (bf16 weights; fp32 361 with five, 401 with six; masters 373 with four, 375 with
+// five).  The 32-bit step loses by it.
+enum : int { k32Bit = 0, kNearest = 1, kDrawn = 2 };        // moments, and how 8-bit codes are rounded
+constexpr int blocks_per_sm(int moments, bool master) {
+    return moments == k32Bit ? 1 : moments == kNearest ? (master ? 5 : 6) : (master ? 4 : 5);
+}
+template <typename P, typename G, bool kMaster, int kMoments>
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(kMoments, kMaster)) k_adamw(const __grid_constant__ StepArgs a) {
+    constexpr bool k8Bit = kMoments != k32Bit;
     wait_for_previous();
     // The tensor whose chunks this block's index falls into: found by one warp for all.
     __shared__ int tensor;
@@ -232,13 +267,11 @@ __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_ada
     }
     float m[8], v[8], w[8], root[8];
     if constexpr (k8Bit) {
-        cur.m.get(m);
-        cur.v.get(v);
         const f32x2 ms = twice(cur.ms), vs = twice(cur.vs);
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-            const f32x2 r = mul2(pair(v + i), vs);
-            unpair(mul2(pair(m + i), ms), m + i);
+            const f32x2 r = mul2(cur.v.two(i), vs);
+            unpair(mul2(cur.m.two(i), ms), m + i);
             unpair(mul2(r, r), v + i);
         }
     } else {
@@ -273,14 +306,43 @@ __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_ada
     typename R::M mo, vo;
     if constexpr (k8Bit) {
         const int em = exponent(block_top(m)), ev = exponent(__float_as_uint(__fsqrt_rn(__uint_as_float(block_top(v)))));
-        const f32x2 im = twice(power_of_two(8 - em)), iv = twice(power_of_two(8 - ev));
+        const float im = power_of_two(8 - em), iv = power_of_two(8 - ev);
+        if constexpr (kMoments == kDrawn) {
+            const f32x2 old_m = twice(cur.ms * im * kDown), old_v = twice(cur.vs * iv * kDown);
+            const int64_t eighth = at >> 3;
+            const uint32_t seed = scramble((uint32_t)eighth * 0x9E3779B9u + (uint32_t)(eighth >> 32) * 0x6A09E667u + (a.before + lo) * 0xBB67AE85u + a.draw);
+            // Odd multipliers (fractional digits of square roots): each turns the uniform seed into another.
+            constexpr uint32_t kDraws[8] = {0x9E3779B9u, 0x3C6EF373u, 0xA54FF53Bu, 0x510E527Fu, 0x9B05688Du, 0x1F83D9ABu, 0x5BE0CD19u, 0xCBBB9D5Du};
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            float c[2];
-            unpair(mul2(pair(m + i), im), m + i);
-            unpair(mul2(pair(root + i), iv), c);
-            root[i] = root[i] > 0.f ? fmaxf(c[0], 0x1p-9f) : c[0];
-            root[i + 1] = root[i + 1] > 0.f ? fmaxf(c[1], 0x1p-9f) : c[1];
+            for (int i = 0; i < 8; i += 2) {
+                float x[2], o[2], y[2], p[2];
+                unpair(mul2(mul2(pair(m + i), twice(im)), twice(kDown)), x);
+                unpair(mul2(cur.m.two(i), old_m), o);
+                unpair(mul2(mul2(pair(root + i), twice(iv)), twice(kDown)), y);
+                unpair(mul2(cur.v.two(i), old_v), p);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t z = seed * kDraws[i + j];
+                    const int xi = __float_as_int(x[j]), yi = __float_as_int(y[j]);
+                    const bool from_zero = fabsf(o[j]) < __int_as_float(kCode);
+                    const bool draw_m = near_code(xi, from_zero ? xi & 0x80000000 : __float_as_int(o[j])) && (!from_zero || fabsf(x[j]) >= a.leave_zero);
+                    m[i + j] = __int_as_float(to_code(xi, draw_m, z >> 12));
+                    int c = to_code(yi, near_code(yi, __float_as_int(p[j])), z & (kCode - 1));
+                    if (root[i + j] > 0.f) c = max(c, kCode);
+                    root[i + j] = __int_as_float(c);
+                }
+                unpair(mul2(pair(m + i), twice(kUp)), m + i);
+                unpair(mul2(pair(root + i), twice(kUp)), root + i);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                float c[2];
+                unpair(mul2(pair(m + i), twice(im)), m + i);
+                unpair(mul2(pair(root + i), twice(iv)), c);
+                root[i] = root[i] > 0.f ? fmaxf(c[0], 0x1p-9f) : c[0];
+                root[i + 1] = root[i + 1] > 0.f ? fmaxf(c[1], 0x1p-9f) : c[1];
+            }
         }
         mo.set(m);
         vo.set(root);
@@ -297,23 +359,30 @@ __global__ void __launch_bounds__(kThreads, k8Bit ? (kMaster ? 5 : 6) : 1) k_ada
 }
 
 using StepKernel = void (*)(const StepArgs);
+template <typename P, typename G, bool kMaster>
+StepKernel step_kernel(int moments) {
+    return moments == kDrawn     ? k_adamw<P, G, kMaster, kDrawn>
+           : moments == kNearest ? k_adamw<P, G, kMaster, kNearest>
+                                 : k_adamw<P, G, kMaster, k32Bit>;
+}
 template <typename P, typename G>
-StepKernel step_kernel(bool master, bool bits8) {
+StepKernel step_kernel(bool master, int moments) {
     if constexpr (sizeof(P) == 2) {
-        if (master) return bits8 ? k_adamw<P, G, true, true> : k_adamw<P, G, true, false>;
+        if (master) return step_kernel<P, G, true>(moments);
     }
-    return bits8 ? k_adamw<P, G, false, true> : k_adamw<P, G, false, false>;
+    return step_kernel<P, G, false>(moments);
 }
 
 }  // namespace
 
 cudaError_t adamw_step(const rlm_adamw_tensor *tensors, int count, rlm_dtype param, rlm_dtype grad, bool master, int bits,
-                       const rlm_adamw_hyper &h, const float *grad_scale, cudaStream_t st) {
+                       bool draw, const rlm_adamw_hyper &h, const float *grad_scale, cudaStream_t st) {
+    const int moments = bits == 32 ? k32Bit : draw ? kDrawn : kNearest;
     const StepKernel fn = param == RLM_BF16
-                              ? (grad == RLM_BF16 ? step_kernel<__nv_bfloat16, __nv_bfloat16>(master, bits == 8)
-                                                  : step_kernel<__nv_bfloat16, float>(master, bits == 8))
-                              : (grad == RLM_BF16 ? step_kernel<float, __nv_bfloat16>(master, bits == 8)
-                                                  : step_kernel<float, float>(master, bits == 8));
+                              ? (grad == RLM_BF16 ? step_kernel<__nv_bfloat16, __nv_bfloat16>(master, moments)
+                                                  : step_kernel<__nv_bfloat16, float>(master, moments))
+                              : (grad == RLM_BF16 ? step_kernel<float, __nv_bfloat16>(master, moments)
+                                                  : step_kernel<float, float>(master, moments));
     StepArgs a;
     const double bc1 = 1.0 - std::pow(h.beta1, (double)h.step), bc2 = 1.0 - std::pow(h.beta2, (double)h.step);
     a.grad_scale = grad_scale;
@@ -325,8 +394,11 @@ cudaError_t adamw_step(const rlm_adamw_tensor *tensors, int count, rlm_dtype par
     a.eps = (float)h.eps;
     a.decay = (float)(1.0 - h.lr * h.weight_decay);
     a.step_size = (float)(h.lr / bc1);
+    a.draw = scramble((uint32_t)h.step + scramble((uint32_t)((uint64_t)h.step >> 32)));
+    a.leave_zero = a.one_minus_beta1 * 0x1p-6f * kDown;
     for (int i = 0; i < count;) {
         a.count = 0;
+        a.before = (uint32_t)i;
         unsigned chunks = 0;
         for (; i < count && a.count < kMaxTensors; ++i) {
             const rlm_adamw_tensor &t = tensors[i];

@@ -46,7 +46,9 @@ rlm_status rlm_adamw_step(const rlm_adamw_tensor *tensors, int count, rlm_dtype 
     if (!tensors || count < 1) return fail(RLM_ERR_INVALID_ARG, "tensors is NULL or count=%d < 1", count);
     if ((param != RLM_F32 && param != RLM_BF16) || (grad != RLM_F32 && grad != RLM_BF16))
         return fail(RLM_ERR_INVALID_ARG, "param or grad dtype is not RLM_F32 or RLM_BF16");
-    if (bits != 8 && bits != 32) return fail(RLM_ERR_INVALID_ARG, "bits=%d (need 8 or 32)", bits);
+    const bool draw = bits == (8 | RLM_ADAMW_DRAW);
+    if (draw) bits = 8;
+    if (bits != 8 && bits != 32) return fail(RLM_ERR_INVALID_ARG, "bits=%d (need 8, 8 | RLM_ADAMW_DRAW or 32)", bits);
     if (!h) return fail(RLM_ERR_INVALID_ARG, "hyper is NULL");
     // Written so that NaN fails.
     if (!(h->lr >= 0 && std::isfinite(h->lr) && h->eps >= 0 && std::isfinite(h->eps) && h->weight_decay >= 0 &&
@@ -63,7 +65,7 @@ rlm_status rlm_adamw_step(const rlm_adamw_tensor *tensors, int count, rlm_dtype 
         if (s != RLM_OK) return s;
     }
     if (!ln) return fail(RLM_ERR_INVALID_ARG, "launch is NULL");
-    const cudaError_t e = adamw_step(tensors, count, param, grad, master, bits, *h, grad_scale,
+    const cudaError_t e = adamw_step(tensors, count, param, grad, master, bits, draw, *h, grad_scale,
                                      static_cast<cudaStream_t>(ln->stream));
     if (e != cudaSuccess) return cuda_fail(e, "rlm_adamw_step launch");
     return RLM_OK;

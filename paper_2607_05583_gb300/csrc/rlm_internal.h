@@ -132,7 +132,7 @@ cudaError_t read_and_clear_linear_status(int *status, cudaStream_t st);
 
 // ---- optimizer (rlm_adamw.cu) -------------------------------------------------
 cudaError_t adamw_step(const rlm_adamw_tensor *tensors, int count, rlm_dtype param, rlm_dtype grad, bool master, int bits,
-                       const rlm_adamw_hyper &h, const float *grad_scale, cudaStream_t st);
+                       bool draw, const rlm_adamw_hyper &h, const float *grad_scale, cudaStream_t st);
 
 // ---- decode (rlm_decode.cu) -----------------------------------------------
 cudaError_t decode_step(const void *x_t, void *y_t, rlm_dtype dt, int B, int D, int M,
