@@ -1,6 +1,7 @@
 // rlm_scan_abi.cu -- the extern "C" entry points of the gated linear recurrence:
 // host-side argument checks and dispatch (kernels in rlm_scan.cu).
 #include <initializer_list>
+#include <numeric>
 
 #include "rlm_check.h"
 
@@ -66,16 +67,16 @@ size_t extent_bytes(const rlm_strided &t) {
 }
 
 // Whether two fields may touch the same bytes.  Fields whose address ranges cross are
-// apart only as column ranges of one wider tensor: equal strides, rows that do not
-// reach each other's columns.
+// apart only as column ranges of one wider tensor, batch or time first: equal strides, whose
+// common divisor all rows are multiples of apart, and columns that do not meet within it.
 bool fields_overlap(const rlm_strided &a, const rlm_strided &b) {
     if (!overlap(a.ptr, extent_bytes(a), b.ptr, extent_bytes(b))) return false;
-    const int64_t ea = (int64_t)elem_size(a.dtype);
-    const int64_t pitch = (a.L > 1 ? a.stride_l : a.stride_b) * ea;
     if (a.dtype != b.dtype || a.B != b.B || a.L != b.L || (a.L > 1 && a.stride_l != b.stride_l) ||
-        (a.B > 1 && a.stride_b != b.stride_b) || pitch <= 0)
+        (a.B > 1 && a.stride_b != b.stride_b))
         return true;
-    if (a.B > 1 && a.L > 1 && (a.stride_b * ea) % pitch != 0) return true;
+    const int64_t ea = (int64_t)elem_size(a.dtype);
+    const int64_t pitch = std::gcd(a.L > 1 ? a.stride_l : 0, a.B > 1 ? a.stride_b : 0) * ea;
+    if (pitch == 0) return true;
     int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b.ptr) - reinterpret_cast<uintptr_t>(a.ptr)) % pitch;
     if (d < 0) d += pitch;
     return !(d >= a.D * ea && d + b.D * ea <= pitch);
