@@ -449,7 +449,7 @@ typedef struct {
 } rlm_adamw_tensor;
 
 typedef struct {
-    double lr, beta1, beta2, eps, weight_decay;     /* lr, eps, wd >= 0; betas in [0, 1) */
+    double lr, beta1, beta2, eps, weight_decay;     /* lr, eps, wd >= 0; betas in [0, 1); (eps = 0: 0 / 0 where both moments are 0) */
     int64_t step;                                   /* t, >= 1 */
 } rlm_adamw_hyper;
 

@@ -43,6 +43,7 @@
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -391,7 +392,9 @@ cudaError_t adamw_step(const rlm_adamw_tensor *tensors, int count, rlm_dtype par
     a.beta2 = (float)h.beta2;
     a.one_minus_beta2 = (float)(1.0 - h.beta2);
     a.inv_sqrt_bc2 = (float)(1.0 / std::sqrt(bc2));
-    a.eps = (float)h.eps;
+    // The step's reciprocal takes denormal numbers for zero; beside a root, which is 0 or above 2^-75,
+    // so small an eps is nothing anyway.
+    a.eps = h.eps > 0 ? std::max((float)h.eps, FLT_MIN) : 0.f;
     a.decay = (float)(1.0 - h.lr * h.weight_decay);
     a.step_size = (float)(h.lr / bc1);
     a.draw = scramble((uint32_t)h.step + scramble((uint32_t)((uint64_t)h.step >> 32)));
