@@ -730,7 +730,8 @@ class AdamGroup:
     """The tensors of an optimizer step, checked and laid out once: weights (float32 or
     bfloat16), gradients (float32 or bfloat16), their AdamState and, for bfloat16 weights,
     optional float32 master copies.  It keeps the tensors; gradients are read from the same
-    buffers at every step."""
+    buffers at every step.  A gradient that is its weight's ``.grad`` has to stay it (zeroed in
+    place, not set to None): a step raises ValueError where it no longer is."""
 
     def __init__(self, params, grads, states, masters=None):
         params, grads, states = list(params), list(grads), list(states)
@@ -745,6 +746,7 @@ class AdamGroup:
         if self.param_dtype not in _DT or self.grad_dtype not in _DT:
             raise ValueError(f"weights are {self.param_dtype}, gradients {self.grad_dtype}: need float32 or bfloat16")
         self._c = (_AdamTensor * len(params))()
+        self._watched = []              # weights whose .grad the group reads
         code = torch.float32 if self.bits == 32 else torch.float8_e4m3fn
         self.device = params[0].device
         for i, (p, g, s, w) in enumerate(zip(params, grads, states, masters)):
@@ -761,6 +763,8 @@ class AdamGroup:
                         or t.device != self.device:
                     raise ValueError(f"tensor {i}: {name} must be a contiguous {dtype} tensor of {size} values on "
                                      f"{self.device}")
+            if p.requires_grad and p.is_leaf and p.grad is not None and p.grad.data_ptr() == g.data_ptr():
+                self._watched.append((i, p, g.data_ptr()))
             ptr = lambda t: t.data_ptr() if t is not None else None
             self._c[i] = _AdamTensor(ptr(p), ptr(g), ptr(s.m), ptr(s.v), ptr(s.m_scale) if self.bits == 8 else None,
                                      ptr(s.v_scale) if self.bits == 8 else None, ptr(w), n)
@@ -773,6 +777,9 @@ def rlm_adamw_step(group: AdamGroup, step: int, lr: float, beta1: float = 0.9, b
     CUDA scalar, multiplies every gradient; a value that is not finite skips the step."""
     if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or not grad_scale.is_cuda):
         raise ValueError("grad_scale must be a CUDA float32 scalar")
+    for i, p, grad in group._watched:
+        if p.grad is None or p.grad.data_ptr() != grad:
+            raise ValueError(f"tensor {i}: its weight's .grad is no longer the gradient that the group was given")
     h = _AdamHyper(lr, beta1, beta2, eps, weight_decay, step)
     _check(load_library().rlm_adamw_step(group._c, len(group._c), _DT[group.param_dtype], _DT[group.grad_dtype],
                                          group.bits | (ADAMW_DRAW if group.draw else 0), h,
