@@ -106,7 +106,7 @@ rlm_status rlm_linear(const rlm_matrix *x, const rlm_matrix *w, const float *bia
     if (pre && (s = check_as(pre, "pre", R, N)) != RLM_OK) return s;
     if ((s = check_vector(bias, "bias")) != RLM_OK) return s;
     const rlm_matrix b = row_of(bias, N);
-    const bool in_place = residual && residual->ptr == y->ptr && residual->ld == y->ld;
+    const bool in_place = residual && residual->ptr == y->ptr && (residual->ld == y->ld || R == 1);
     if ((s = check_apart({{y, "y"}, {pre, "pre"}}, {{x, "x"}, {w, "w"}, {bias ? &b : nullptr, "bias"}})) != RLM_OK)
         return s;
     if (residual && ((!in_place && matrices_overlap(*residual, *y)) || (pre && matrices_overlap(*residual, *pre))))
