@@ -38,7 +38,7 @@
 // quotient of the step are the approximate instructions (2^-22): with the exact sequences
 // the 8-bit step, which its instructions bound (82 % of issue slots), took 379 us at 120 M
 // values against 211 us now (bf16 weights, codes to nearest) and 178 us for its bytes.  By draw it
-// takes 336 us (361 with fp32 weights, 374 with masters): some 30 instructions a value more.  The
+// takes 337 us (370 with fp32 weights, 376 with masters): some 30 instructions a value more.  The
 // 32-bit steps run at the copy rate: 478 us for 3.36 GB (fp32, and bf16 with masters), 7.0 TB/s.
 #include <cuda_fp8.h>
 
@@ -129,10 +129,10 @@ __device__ __forceinline__ V load8(const void *p, int n, bool wide) {
 #pragma unroll
         for (int i = 0; i < kBytes / kWide; ++i) {
             if constexpr (kWide == 16) {
-                const uint4 q = __ldcs(static_cast<const uint4 *>(p) + i);
+                const uint4 q = load_once(static_cast<const uint4 *>(p) + i);
                 v.w[4 * i] = q.x, v.w[4 * i + 1] = q.y, v.w[4 * i + 2] = q.z, v.w[4 * i + 3] = q.w;
             } else {
-                const uint2 q = __ldcs(static_cast<const uint2 *>(p));
+                const uint2 q = load_once8(p);
                 v.w[0] = q.x, v.w[1] = q.y;
             }
         }

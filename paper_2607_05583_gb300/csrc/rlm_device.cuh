@@ -62,10 +62,16 @@ __device__ __forceinline__ void wait_for_previous() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// 16 bytes that are read once.
+// 16 bytes that are read once, and 8.
 __device__ __forceinline__ uint4 load_once(const void *p) {
     uint4 v;
     asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+__device__ __forceinline__ uint2 load_once8(const void *p) {
+    uint2 v;
+    asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
     return v;
 }
 
