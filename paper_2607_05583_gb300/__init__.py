@@ -395,17 +395,35 @@ def _check(status: int, where: str):
         raise RlmError(status, where, load_library().rlm_last_error().decode())
 
 
-def _workspace(nbytes: int, device, stream=None) -> torch.Tensor | None:
+class _StreamMemory:
+    """Bytes from the caching allocator's pool of a stream that need not be the current one."""
+
+    def __init__(self, nbytes: int, device, stream: int):
+        self._n = nbytes
+        self._ptr = torch.cuda.caching_allocator_alloc(nbytes, device, stream)
+
+    def data_ptr(self) -> int:
+        return self._ptr
+
+    def numel(self) -> int:
+        return self._n
+
+    def element_size(self) -> int:
+        return 1
+
+    def __del__(self):
+        if self.__dict__.get("_ptr"):
+            torch.cuda.caching_allocator_delete(self._ptr)
+
+
+def _workspace(nbytes: int, device, stream=None):
     """A call's own workspace, from the allocator's pool of the stream that the call runs on: once
     released it goes to that stream's later work only."""
     if nbytes == 0:
         return None
-    if stream is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
-    with torch.cuda.stream(stream):
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if stream is not None and (handle := _stream(stream)) != _stream(None):
+        return _StreamMemory(nbytes, device, handle)
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 # --------------------------------------------------------------- entry points

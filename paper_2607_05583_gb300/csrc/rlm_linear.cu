@@ -41,6 +41,7 @@
 namespace rlm {
 
 __device__ int g_linear_status = 0;
+static std::atomic<bool> g_linear_waits{false};      // whether a kernel that may set it was launched
 
 namespace {
 
@@ -811,6 +812,7 @@ cudaError_t launch_gemm(const CUtensorMap &ma, const CUtensorMap &mb, GemmArgs g
         }
         ctas[dev & 63].store(room, std::memory_order_relaxed);
     }
+    g_linear_waits.store(true, std::memory_order_relaxed);
     constexpr int kCtas = kPair ? 2 : 1;
     g.whole = g.units = g.tiles_m * g.tiles_n * g.splits;
     if (kBN == 256 && g.splits == 1) {
@@ -1016,6 +1018,8 @@ cudaError_t linear_backward(const rlm_matrix &dy, const rlm_matrix &x, const rlm
 }
 
 cudaError_t read_and_clear_linear_status(int *status, cudaStream_t st) {
+    *status = RLM_OK;
+    if (!g_linear_waits.load(std::memory_order_relaxed)) return cudaSuccess;
     cudaError_t e = cudaMemcpyFromSymbolAsync(status, g_linear_status, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
     if (e != cudaSuccess) return e;
     if ((e = cudaStreamSynchronize(st)) != cudaSuccess) return e;

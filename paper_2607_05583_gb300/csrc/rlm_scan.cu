@@ -65,6 +65,7 @@
 namespace rlm {
 
 __device__ int g_scan_status = 0;
+static std::atomic<bool> g_scan_waits{false};        // whether a kernel that may set it was launched
 
 namespace {
 
@@ -880,6 +881,7 @@ cudaError_t launch_scan(bool backward, bool leak, ScanArgs<T> &a, int64_t B, cud
     a.nseg = p.nseg;
     a.ntiles = p.ntiles;
     a.nchunks = (a.L + kChunk - 1) / kChunk;
+    if (p.nseg > 1) g_scan_waits.store(true, std::memory_order_relaxed);
     // (resident() has set the kernel's shared memory size.)
     return launch_dependent(k.fn, dim3((unsigned)(p.chains * p.nseg)), kThreads, (size_t)k.smem, st, p.nseg, a);
 }
@@ -959,6 +961,8 @@ cudaError_t scan_step(const rlm_strided &x, const rlm_strided &g, const rlm_stri
 }
 
 cudaError_t read_and_clear_scan_status(int *status, cudaStream_t st) {
+    *status = RLM_OK;
+    if (!g_scan_waits.load(std::memory_order_relaxed)) return cudaSuccess;
     cudaError_t e = cudaMemcpyFromSymbolAsync(status, g_scan_status, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
     if (e != cudaSuccess) return e;
     if ((e = cudaStreamSynchronize(st)) != cudaSuccess) return e;
