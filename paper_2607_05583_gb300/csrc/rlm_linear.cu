@@ -136,7 +136,7 @@ struct GemmCfg {
 };
 
 struct GemmArgs {
-    int M, N, K;                // output rows and columns, contraction
+    int M, N;                   // output rows and columns
     int tiles_m, tiles_n, splits, steps_per_split, steps;
     int whole, units;           // units that are whole tiles (of a split), and all (see unit_of())
     const float *bias;          // nullable [N]
@@ -854,7 +854,7 @@ cudaError_t gemm(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const Ep
     const bool split = p.splits > 1;
     const int out = split || ep.out_f32 ? kOutF32 : ep.pre ? kOutPre : kOutBf16;
     GemmArgs g = {};
-    g.M = (int)M, g.N = (int)N, g.K = (int)K;
+    g.M = (int)M, g.N = (int)N;
     g.tiles_m = p.tiles_m, g.tiles_n = p.tiles_n;
     g.splits = p.splits, g.steps_per_split = p.steps_per_split, g.steps = p.steps;
     g.out = split ? part : ep.out;

@@ -831,10 +831,11 @@ int64_t resident(const ScanKernel<T> &k, int nseg, std::atomic<int> &known) {
     return (int64_t)n * nseg;
 }
 
-// With lengths, rounds after the first are shorter: CTAs of short rows make room early.
-// 0.35 + 0.65 rounds in place of rounds, forward and backward of bf16 B = 32, L = 1500,
-// D = 320, lengths of 0 to L: 30.8 -> 24.7 and 56.4 -> 36.8 us; the order of the rows by
-// length changes either by 4 % at most.
+// With lengths, rounds after the first count for less: a CTA walks all waves of L whatever its
+// row's length, but those past the row's end without memory, so short rows make some room.  A
+// figure fitted to one shape: 0.35 + 0.65 rounds in place of rounds, forward and backward of
+// bf16 B = 32, L = 1500, D = 320, lengths of 0 to L: 30.8 -> 24.7 and 56.4 -> 36.8 us (27 and 34
+// now); the order of the rows by length changed either by 4 % at most.
 constexpr double kFirstRound = 0.35;
 
 // Channel pairs per CTA and segments per chain: the least of rounds of resident CTAs times
