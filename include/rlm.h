@@ -27,6 +27,10 @@
  *    check returns RLM_ERR_INVALID_ARG or RLM_ERR_UNSUPPORTED and enqueues
  *    nothing.  rlm_last_error() then describes the failure.
  *  - A failed kernel launch returns RLM_ERR_CUDA.
+ *  - Many kernels launch programmatically dependent and let the kernel after them in the
+ *    stream start early.  One of the caller's that is launched with that attribute has to
+ *    wait (griddepcontrol.wait, cudaGridDependencySynchronize) before it reads their outputs;
+ *    one launched without it needs nothing.
  *  - Kernels that wait on one another (the prefill's cross-block carry) wait a
  *    bounded number of iterations; on expiry they record RLM_ERR_TIMEOUT in a
  *    device status word and return without hanging.  rlm_get_device_status()

@@ -112,8 +112,8 @@ struct ScanArgs {
 
 constexpr f32x2 kOne = 0x3f8000003f800000ull, kMinus = 0xbf800000bf800000ull, kKeep = 0x8000000080000000ull;   // (q of a = 1)
 
-// Gates whose b passes this (g below -3.43) count as closed: v - b v is off by 2^-24 v, so by less
-// than 2^-19 of a v short of it.
+// Gates whose b passes this (g below -3.43) count as closed.  b is within 2^-23 (1 + e and its
+// reciprocal), so short of it v - b v is within 2^-18 of a v.
 constexpr float kClosed = 31.f / 32.f;
 
 // A run of two channels: h -> A h + H.
