@@ -244,13 +244,18 @@ __device__ __forceinline__ void advance(Quad (&h)[4], const Quad (&a2)[4], float
 // Whether h is mended before token t, the middle of kMendEvery.  (After them the states that forget sooner would have gained
 // more than they lost.)
 __device__ __forceinline__ bool mend_at(int t, int len) { return t % kMendEvery == kMendEvery / 2 && t + kMendEvery / 4 <= len; }
+// h + k h for a small k.  An infinite h stays (k h is infinite with k's sign, or NaN where k is 0).
+__device__ __forceinline__ f32x2 grow(f32x2 h, f32x2 k) {
+    const float2 v = unpack(h), t = unpack(mul2(k, h));
+    return pack(make_float2(v.x + (fabsf(t.x) < __builtin_huge_valf() ? t.x : 0.f), v.y + (fabsf(t.y) < __builtin_huge_valf() ? t.y : 0.f)));
+}
 // What kMendEvery tokens' decays take too much from h; D of one of them.
 __device__ __forceinline__ void mend(Quad (&h)[4], const Quad (&a2)[4], float4 delta) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float d = i == 0 ? delta.x : i == 1 ? delta.y : i == 2 ? delta.z : delta.w;
         const f32x2 most = both(kMendEvery * kMendMost);
-        h[i] = {fma2(bent(d, a2[i].lo), mul2(most, h[i].lo), h[i].lo), fma2(bent(d, a2[i].hi), mul2(most, h[i].hi), h[i].hi)};
+        h[i] = {grow(h[i].lo, mul2(bent(d, a2[i].lo), most)), grow(h[i].hi, mul2(bent(d, a2[i].hi), most))};
     }
 }
 
