@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kThreads) k_ends(Args<T> a) {
 }
 
 template <typename T, int N, bool kGate>
-__global__ void __launch_bounds__(kThreads) k_forward(Args<T> a) {
+__global__ void __launch_bounds__(kThreads, 6) k_forward(Args<T> a) {
     using S = Block<N>;
     __shared__ __align__(16) float4 delta[S::kTok * S::kGroups], drive[S::kTok * S::kGroups], bs[S::kTok * S::P], cs[S::kTok * S::P];
     __shared__ __align__(16) float4 share[S::kTok][kThreads + S::kGroups];     // of o: P a group, one more to keep the banks apart
@@ -103,13 +103,10 @@ __global__ void __launch_bounds__(kThreads) k_forward(Args<T> a) {
     w.load_decays(a2, a);
     if (a.nseg > 1) {
         const int64_t end = (int64_t)w.b * a.nseg;
-        w.load_states(h, a.end_state + w.state(a, end + a.nseg - 1));
-#pragma unroll 2
-        for (int s = 0; s < w.seg; ++s) {
-            Quad H[4];
-            w.load_states(H, a.end_state + w.state(a, end + s));
-            advance(h, a2, four_of(a.end_delta + (end + s) * a.D, w.c, w.on), H);
-        }
+        auto load = [&](int s, Quad (&H)[4]) { w.load_states(H, a.end_state + w.state(a, end + s)); };
+        through_segments(
+            h, a2, w.seg, [&](Quad (&H)[4]) { load(a.nseg - 1, H); },
+            [&](int s, float4 &S, Quad (&H)[4]) { load(s, H), S = four_of(a.end_delta + (end + s) * a.D, w.c, w.on); });
     } else {
         w.load_states(h, a.state_in ? a.state_in + w.state(a, w.b) : nullptr);
     }

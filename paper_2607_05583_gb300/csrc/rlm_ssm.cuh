@@ -241,6 +241,46 @@ __device__ __forceinline__ void advance(Quad (&h)[4], const Quad (&a2)[4], float
     }
 }
 
+// The states before a segment from those before the first one, which start(h) gives: step after step h <- e^(A S) h + v over
+// the segments before it, S a segment's sum of D and v what it leaves of a zero state; load(s, delta, v) gives the s-th's.
+// Where decays grow past fp32's range a factor is infinite, and what it makes is infinite or NaN whatever the later steps do.
+// Then the steps are taken again with the factor in three: what is 0 stays 0, and what the whole factor would bring back
+// into range does so.
+__device__ __forceinline__ f32x2 grown(f32x2 delta, f32x2 a2, f32x2 h, f32x2 v) {
+    const float2 x = unpack(mul2(fma2(delta, a2, both(kShift)), both(1 / 3.f)));
+    const f32x2 third = pack(make_float2(ex2(fminf(x.x, 126.f)), ex2(fminf(x.y, 126.f))));
+    return fma2(third, mul2(third, mul2(third, h)), v);
+}
+template <typename Start, typename Load>
+__device__ __forceinline__ void through_segments(Quad (&h)[4], const Quad (&a2)[4], int count, Start start, Load load) {
+    start(h);
+    float4 delta;
+    Quad v[4];
+#pragma unroll 2
+    for (int s = 0; s < count; ++s) {
+        load(s, delta, v);
+        advance(h, a2, delta, v);
+    }
+    bool fine = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 f = unquad(h[i]);
+        fine &= fabsf(f.x) < __builtin_huge_valf() && fabsf(f.y) < __builtin_huge_valf() && fabsf(f.z) < __builtin_huge_valf() &&
+                fabsf(f.w) < __builtin_huge_valf();
+    }
+    if (fine) return;
+    start(h);
+#pragma unroll 1
+    for (int s = 0; s < count; ++s) {
+        load(s, delta, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 d = both(i == 0 ? delta.x : i == 1 ? delta.y : i == 2 ? delta.z : delta.w);
+            h[i] = {grown(d, a2[i].lo, h[i].lo, v[i].lo), grown(d, a2[i].hi, h[i].hi, v[i].hi)};
+        }
+    }
+}
+
 // Whether h is mended before token t, the middle of kMendEvery.  (After them the states that forget sooner would have gained
 // more than they lost.)
 __device__ __forceinline__ bool mend_at(int t, int len) { return t % kMendEvery == kMendEvery / 2 && t + kMendEvery / 4 <= len; }

@@ -198,14 +198,19 @@ __global__ void __launch_bounds__(4 * N) k_backward(Args<T> a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) a2.v[j] = mul4(both(kLog2e), a2.v[j]);
         if (a.nseg > 1) {
-            G = load_states<N>(a.end_state + state((int64_t)bi * a.nseg), q);
+            const int64_t end = (int64_t)bi * a.nseg;
+            auto load = [&](int k, Quad (&E)[4]) {
+                const States e = load_states<N>(a.end_state + state(end + k), q);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) E[j] = e.v[j];
+            };
+            through_segments(
+                G.v, a2.v, a.nseg - 1 - seg, [&](Quad (&E)[4]) { load(0, E); },
+                [&](int k, float4 &S, Quad (&E)[4]) {
+                    load(a.nseg - 1 - k, E), S = *reinterpret_cast<const float4 *>(a.end_delta + (end + a.nseg - 1 - k) * a.D + c);
+                });
         } else if (a.d_state_out) {
             G = load_states<N>(a.d_state_out + state(bi), q);
-        }
-        for (int k = a.nseg - 1; k > seg; --k) {
-            const int64_t end = (int64_t)bi * a.nseg + k;
-            const States E = load_states<N>(a.end_state + state(end), q);
-            advance(G.v, a2.v, *reinterpret_cast<const float4 *>(a.end_delta + end * a.D + c), E.v);
         }
     }
     float dskip[4] = {}, dbias[4] = {};
