@@ -449,7 +449,10 @@ RLM_API rlm_status rlm_conv_decode(const rlm_strided *x_t, const float *conv_w, 
  *   h_tn = a_tn h_{t-1,n} + D_t x_t B_tn,   y_t = (sum_n C_tn h_tn + skip x_t) silu(z_t)
  *
  * A, skip and dt_bias are of a channel, B_t and C_t of a token (all channels share them).  A is given as it
- * enters the exponent (negative for a decay; a keeps 2^-22 of relative accuracy).  State: fp32 [B][D][N]. */
+ * enters the exponent (negative for a decay).  Each a keeps 2^-22 of relative accuracy.  Over a sequence their errors do not
+ * add up: after every 32 tokens of a call (16 in the gradients) a state is multiplied by e^(A sum of D) over the product of
+ * the decays that it went through.  That differs from 1 by 2^-20 at most, and a state's last bits depend on where a
+ * sequence is cut into calls.  State: fp32 [B][D][N]. */
 typedef struct {
     const float *A;             /* fp32 [D][N] */
     const float *skip;          /* nullable (0), fp32 [D] */

@@ -4,9 +4,11 @@
 // A token, channel and state cost one ex2 and four multiply-adds; an SM has units for 32 of the former and 128
 // of the latter a clock (measured: 62.6 and 243 a nanosecond), so N states bound a token and channel by N / 32 clocks
 // of an SM, against 8 bytes of memory (bf16): above N = 8 or so the kernel is bound by arithmetic, in
-// practice by the issue of its instructions (28 a warp's 32 x 4 states and token, 10 of them for staging and output).
-// B = 4, L = 4096, D = 1024, N = 16, bf16: 91 us, and 59 for the segments' ends; 6 blocks on an SM issue in 55 % of
-// the cycles; more of them with fewer registers each were slower (128 registers: 128 us where 158 took 109).
+// practice by the issue of its instructions (31 a warp's 32 x 4 states and token: 10 of them for staging and output, 3 for
+// keeping the decays' product and putting the states right by it).  B = 4, L = 4096, D = 1024, N = 16: 103 us in bf16, 115 in
+// fp32, and 66 for the segments' ends.  The registers are bounded for 6 blocks on an SM, which k_forward needs no spills of
+// more than a few bytes for; z is loaded before a tile's tokens and used behind them, where x and dt are a tile ahead (a
+// tile ahead too, z takes registers that fp32 has not got: 128 us; 5 blocks an SM without a bound: 130).
 //
 // Segments.  Where rows and channels give too few warps the sequence is cut into nseg runs of tiles.
 // A run maps its first state to its last by h -> e^(A S) h + H, S the sum of its D and H its end state
@@ -52,7 +54,9 @@ __global__ void __launch_bounds__(kThreads) k_ends(Args<T> a) {
     const Quad bias = quad(four_of(a.bias, w.cu, w.on_u));
     w.load_decays(a2, a);
     w.load_states(h, nullptr);
-    Quad sum = {0, 0};
+    Quad minus = {0, 0};
+    Passed passed;
+    passed.clear();
     Four<T> rx[S::kUnits], rd[S::kUnits], rb[S::kRows];
     auto fetch = [&](int t0) {
         w.load(rx, x, a.x_l, t0);
@@ -72,20 +76,21 @@ __global__ void __launch_bounds__(kThreads) k_ends(Args<T> a) {
         w.store_row(bs, rb);
         __syncthreads();
         if (tile + 1 < last) fetch((tile + 1) * S::kTok);
-        if (mend_at(tile * S::kTok, w.len)) mend(h, a2, delta[mine]);
-        Quad s = {0, 0};
 #pragma unroll 8
         for (int t = 0; t < S::kTok; ++t) {
             const float4 d = delta[t * S::kGroups + mine], u = drive[t * S::kGroups + mine];
             const Quad B = quad(bs[t * S::P + p]), v[4] = {mul4(both(u.x), B), mul4(both(u.y), B), mul4(both(u.z), B), mul4(both(u.w), B)};
-            advance(h, a2, d, v);
-            s = {add2(s.lo, quad(d).lo), add2(s.hi, quad(d).hi)};
+            advance(h, a2, d, v, passed);
         }
-        sum = {add2(sum.lo, s.lo), add2(sum.hi, s.hi)};
+        if ((tile + 1) * S::kTok % kPeriod == 0 || tile + 1 == last) {
+            put_right(h, a2, passed);
+            minus = {add2(minus.lo, passed.minus.lo), add2(minus.hi, passed.minus.hi)};
+            passed.clear();
+        }
         __syncthreads();
     }
     w.store_states(h, a.end_state + w.state(a, end));
-    if (w.on && p == 0) *reinterpret_cast<float4 *>(a.end_delta + end * a.D + w.c) = unquad(sum);
+    if (w.on && p == 0) *reinterpret_cast<float4 *>(a.end_delta + end * a.D + w.c) = unquad(mul4(both(-1.f), minus));
 }
 
 template <typename T, int N, bool kGate>
@@ -110,16 +115,17 @@ __global__ void __launch_bounds__(kThreads, 6) k_forward(Args<T> a) {
     } else {
         w.load_states(h, a.state_in ? a.state_in + w.state(a, w.b) : nullptr);
     }
-    Four<T> rx[S::kUnits], rz[S::kUnits], nx[S::kUnits], nd[S::kUnits], nz[S::kUnits], nb[S::kRows], nc[S::kRows];
+    Four<T> rx[S::kUnits], rz[S::kUnits], nx[S::kUnits], nd[S::kUnits], nb[S::kRows], nc[S::kRows];
     auto fetch = [&](int t0) {
         w.load(nx, x, a.x_l, t0);
         w.load(nd, dt, a.dt_l, t0);
-        if (kGate) w.load(nz, z, a.z_l, t0);
         w.load_row(nb, b, a.b_l, t0);
         w.load_row(nc, c, a.c_l, t0);
     };
     const int last = min(w.last, (w.len + S::kTok - 1) / S::kTok);
     const int mine = threadIdx.x / S::P, p = w.p;
+    Passed passed;
+    passed.clear();
     if (w.first < last) fetch(w.first * S::kTok);
     for (int tile = w.first; tile < last; ++tile) {
         const int t0 = tile * S::kTok;
@@ -129,20 +135,23 @@ __global__ void __launch_bounds__(kThreads, 6) k_forward(Args<T> a) {
             delta[w.unit(k)] = unquad(d);
             drive[w.unit(k)] = unquad(mul4(d, quad(nx[k].values())));
             rx[k] = nx[k];
-            if (kGate) rz[k] = nz[k];
         }
         w.store_row(bs, nb);
         w.store_row(cs, nc);
         __syncthreads();
+        if (kGate) w.load(rz, z, a.z_l, t0);         // (used behind the tokens)
         if (tile + 1 < last) fetch(t0 + S::kTok);
-        if (mend_at(t0, w.len)) mend(h, a2, delta[mine]);
+        if (t0 % kPeriod == 0) {
+            put_right(h, a2, passed);
+            passed.clear();
+        }
         if (a.saved && t0 % kTile == 0) w.store_states(h, a.saved + w.state(a, (int64_t)w.b * a.ntiles + t0 / kTile));
 #pragma unroll 4
         for (int t = 0; t < S::kTok; ++t) {
             const float4 d = delta[t * S::kGroups + mine], u = drive[t * S::kGroups + mine];
             const Quad B = quad(bs[t * S::P + p]), C = quad(cs[t * S::P + p]);
             const Quad v[4] = {mul4(both(u.x), B), mul4(both(u.y), B), mul4(both(u.z), B), mul4(both(u.w), B)};
-            advance(h, a2, d, v);
+            advance(h, a2, d, v, passed);
             share[t][threadIdx.x + mine] = make_float4(dot4(C, h[0]), dot4(C, h[1]), dot4(C, h[2]), dot4(C, h[3]));
         }
         __syncthreads();
@@ -172,6 +181,7 @@ __global__ void __launch_bounds__(kThreads, 6) k_forward(Args<T> a) {
             const int to = tile * S::kTok + w.token(k);
             if (w.on_u && to < a.L) Four<T>::store(y + (int64_t)to * a.y_l, make_float4(0.f, 0.f, 0.f, 0.f));
         }
+    put_right(h, a2, passed);
     if (a.state_out && w.seg == a.nseg - 1) w.store_states(h, a.state_out + w.state(a, w.b));
 }
 
@@ -198,7 +208,7 @@ __global__ void __launch_bounds__(kStepThreads) k_step(Args<T> a, int64_t rows, 
         xv = (float)a.x[b * a.x_b + c];
         const float v = (float)a.dt[b * a.dt_b + c] + (a.bias ? a.bias[c] : 0.f), d = a.softplus ? unpack(softplus(both(v))).x : v;
         const Quad u = mul4(both(d * xv), quad(B.values()));
-        const Quad next = {fma2(decay_mended(d, a2.lo), h.lo, u.lo), fma2(decay_mended(d, a2.hi), h.hi, u.hi)};
+        const Quad next = {fma2(decay_alone(both(d), a2.lo), h.lo, u.lo), fma2(decay_alone(both(d), a2.hi), h.hi, u.hi)};
         *s = unquad(next);
         o = dot4(quad(C.values()), next);
     }

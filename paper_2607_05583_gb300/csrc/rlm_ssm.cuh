@@ -22,16 +22,16 @@ namespace ssm {
 
 constexpr int kTile = RLM_SSM_CHUNK;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// ex2.approx is off by 3e-8 of itself (rms) and on the average too small, by 5.5e-9 of itself (within 1.5e-9) at exponents x
+// ex2.approx is off by 3e-8 of itself (rms) and on the average too small: by 5.5e-9 of itself (within 1.5e-9) at exponents x
 // above -2^-8.5, by 1e-8 at -2^-8.2, 2.2e-8 (0.8 to 3e-8) from -2^-7.5 on (means over factors of 1.4).  A state that
-// remembers n steps collects n times the mean.  The part that is the same everywhere is added to the exponents (kShift; at an
-// exponent of 0 a is 1 all the same); the rest is added to the states themselves (and to their gradients G) once in
-// kMendEvery tokens, taken from one token's exponents: it is 1.75e-8 sat((|x| - 0.0025) / 0.0042)
-// a token.  (The error of dA at B = 4, L = 4096, steps of 0.001 to 0.1, A = -1 .. -16: 3.9e-6 with neither,
-// 1.8e-6 with the best shift alone, 8.5e-7 with both, for 1 % of the time.)
-constexpr float kShift = 8e-9f;
-constexpr int kMendEvery = 32;
-constexpr float kMendSlope = 1 / 0.0042f, kMendStart = -0.0025f / 0.0042f, kMendMost = 1.75e-8f;
+// remembers n steps would collect n times the mean.  The middle of it is added to the exponents (kShift; at an exponent of 0
+// a is 1 all the same).  What is left is taken off by what the tokens did: the product P of the decays that a state went
+// through is kept beside it, and after kPeriod tokens it is multiplied by e^(A sum of D) / P (put_right).  So is the
+// gradient G.  (dA at B = 4, L = 4096, steps of 0.001 to 0.1, A = -1 .. -16, is off by 6.0e-7 in norm; by 3.9e-6 with
+// the exponentials as they are, 6.8e-7 with each decay rounded correctly.  With one token's step taken for kPeriod of them it
+// was 8.5e-7, and 5e-5 in a state that only that token moves.)
+constexpr float kShift = 2e-8f;
+constexpr int kPeriod = 32;             // (of the gradients' main kernel: kTile)
 
 __device__ __forceinline__ float ex2(float v) {
     float e;
@@ -93,15 +93,23 @@ __device__ __forceinline__ f32x2 decay(f32x2 delta, f32x2 a2) {
     const float2 v = unpack(fma2(delta, a2, both(kShift)));
     return pack(make_float2(ex2(v.x), ex2(v.y)));
 }
-// The rest of a's mean error at exponents D A log2 e, in parts of kMendMost.
-__device__ __forceinline__ f32x2 bent(float delta, f32x2 a2) {
-    const float2 v = unpack(a2);
-    return pack(make_float2(__saturatef(fmaf(-kMendSlope * delta, v.x, kMendStart)), __saturatef(fmaf(-kMendSlope * delta, v.y, kMendStart))));
+// 2^x for |x| <= 1, by its Taylor series up to the 9th power (the 10th is below 7.1e-9): its rounding has no mean.
+__device__ __forceinline__ f32x2 exp2_series(f32x2 x) {
+    f32x2 f = fma2(x, both(1.0178086e-7f), both(1.3215487e-6f));        // (ln 2)^k / k!, k = 9, 8 ..
+    f = fma2(x, f, both(1.5252734e-5f));
+    f = fma2(x, f, both(1.5403530e-4f));
+    f = fma2(x, f, both(1.3333558e-3f));
+    f = fma2(x, f, both(9.6181291e-3f));
+    f = fma2(x, f, both(5.5504109e-2f));
+    f = fma2(x, f, both(0.24022651f));
+    f = fma2(x, f, both(kLn2));
+    return fma2(x, f, both(1.f));
 }
-// decay() with all of its mean error taken off, for a token by itself.
-__device__ __forceinline__ f32x2 decay_mended(float delta, f32x2 a2) {
-    const float2 v = unpack(fma2(bent(delta, a2), both(kMendMost * kLog2e), fma2(both(delta), a2, both(kShift))));
-    return pack(make_float2(ex2(v.x), ex2(v.y)));
+// decay() for a token by itself: by the series where the state will remember it.
+__device__ __forceinline__ f32x2 decay_alone(f32x2 delta, f32x2 a2) {
+    const f32x2 x = mul2(delta, a2);
+    const float2 v = unpack(x), near = unpack(exp2_series(x)), far = unpack(decay(delta, a2));
+    return pack(make_float2(fabsf(v.x) <= 1.f ? near.x : far.x, fabsf(v.y) <= 1.f ? near.y : far.y));
 }
 // max(v, 0) + log(1 + e), e = e^-|v|, the logarithm as 2 artanh(e / (2 + e)) by its series up to the 13th power
 // (1 / 3 to the 14th over 15 is 1.4e-8): to about (|v| + 9) 2^-24 of itself at every v, where log1pf takes four
@@ -281,21 +289,42 @@ __device__ __forceinline__ void through_segments(Quad (&h)[4], const Quad (&a2)[
     }
 }
 
-// Whether h is mended before token t, the middle of kMendEvery.  (After them the states that forget sooner would have gained
-// more than they lost.)
-__device__ __forceinline__ bool mend_at(int t, int len) { return t % kMendEvery == kMendEvery / 2 && t + kMendEvery / 4 <= len; }
-// h + k h for a small k.  An infinite h stays (k h is infinite with k's sign, or NaN where k is 0).
-__device__ __forceinline__ f32x2 grow(f32x2 h, f32x2 k) {
-    const float2 v = unpack(h), t = unpack(mul2(k, h));
-    return pack(make_float2(v.x + (fabsf(t.x) < __builtin_huge_valf() ? t.x : 0.f), v.y + (fabsf(t.y) < __builtin_huge_valf() ? t.y : 0.f)));
-}
-// What kMendEvery tokens' decays take too much from h; D of one of them.
-__device__ __forceinline__ void mend(Quad (&h)[4], const Quad (&a2)[4], float4 delta) {
+// The product P of the decays that 4 channels' states went through, and the sum of -D.
+struct Passed {
+    Quad product[4], minus;
+    __device__ __forceinline__ void clear() {
+        minus = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) product[i] = {both(1.f), both(1.f)};
+    }
+    __device__ __forceinline__ void add(Quad delta) { minus = {fma2(delta.lo, both(-1.f), minus.lo), fma2(delta.hi, both(-1.f), minus.hi)}; }
+};
+__device__ __forceinline__ void advance(Quad (&h)[4], const Quad (&a2)[4], float4 delta, const Quad (&v)[4], Passed &passed) {
+    passed.add(quad(delta));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float d = i == 0 ? delta.x : i == 1 ? delta.y : i == 2 ? delta.z : delta.w;
-        const f32x2 most = both(kMendEvery * kMendMost);
-        h[i] = {grow(h[i].lo, mul2(bent(d, a2[i].lo), most)), grow(h[i].hi, mul2(bent(d, a2[i].hi), most))};
+        const f32x2 d = both(i == 0 ? delta.x : i == 1 ? delta.y : i == 2 ? delta.z : delta.w);
+        const Quad a = {decay(d, a2[i].lo), decay(d, a2[i].hi)};
+        h[i] = fma4(a, h[i], v[i]);
+        passed.product[i] = mul4(a, passed.product[i]);
+    }
+}
+
+// h 2^-x / P as h + h (1 - P 2^x), x the sum of -D A log2 e and |x| <= 1: what forgets faster (within 46 tokens) collects too
+// little to matter, and there what h has gained since would lose more by x's rounding.  (The factor itself has too few
+// bits.)  An infinite h stays: its second term is infinite or NaN.
+__device__ __forceinline__ f32x2 put_right(f32x2 h, f32x2 product, f32x2 x) {
+    const f32x2 over = fma2(product, exp2_series(x), both(-1.f));
+    const float2 t = unpack(mul2(over, h)), e = unpack(x), v = unpack(h);
+    constexpr float kInf = __builtin_huge_valf();
+    return pack(make_float2(v.x - (fabsf(e.x) <= 1.f && fabsf(t.x) < kInf ? t.x : 0.f), v.y - (fabsf(e.y) <= 1.f && fabsf(t.y) < kInf ? t.y : 0.f)));
+}
+__device__ __forceinline__ void put_right(Quad (&h)[4], const Quad (&a2)[4], const Passed &passed) {
+    const float4 d = unquad(passed.minus);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Quad x = mul4(both(i == 0 ? d.x : i == 1 ? d.y : i == 2 ? d.z : d.w), a2[i]);
+        h[i] = {put_right(h[i].lo, passed.product[i].lo, x.lo), put_right(h[i].hi, passed.product[i].hi, x.hi)};
     }
 }
 

@@ -11,7 +11,8 @@
 // tokens, with one channel a thread, they left 4 warps on an SM: 657 us at B = 4, L = 4096, D = 1024, N = 16 in bf16,
 // against 325.  With 2 channels a thread and runs of 8, 407: bound by shared memory's 128 bytes a clock.  Tiles of
 // 32 tokens leave room for half the blocks; what the states between tiles of 16 move more is nothing beside the
-// arithmetic.)  The G that reaches the tile before is the only thing carried.
+// arithmetic.)  The G that reaches the tile before is the only thing carried.  Putting it right by the decays' product
+// is 8 % of the time (351 us; N = 8, B = 16: 1.21 ms for 1.05).
 //
 // Sums over the state's n are left in shared memory as P shares a channel and added where they are used.  Sums over
 // channels (dB, dC: 4 values each a thread and token) go over the thread's 4, then over the lanes of a warp that hold
@@ -59,7 +60,9 @@ __global__ void __launch_bounds__(kThreads) k_reverse_ends(Args<T> a) {
     const Quad bias = quad(four_of(a.bias, w.cu, w.on_u));
     w.load_decays(a2, a);
     w.load_states(G, nullptr);
-    Quad sum = {0, 0};
+    Quad minus = {0, 0};
+    Passed passed;
+    passed.clear();
     Four<T> ry[S::kUnits], rd[S::kUnits], rz[S::kUnits], rc[S::kRows];
     auto fetch = [&](int t0) {
         w.load(ry, dy, a.dy_l, t0);
@@ -79,25 +82,28 @@ __global__ void __launch_bounds__(kThreads) k_reverse_ends(Args<T> a) {
         w.store_row(cs, rc);
         __syncthreads();
         if (tile > w.first) fetch((tile - 1) * S::kTok);
-        if (mend_at((tile + 1) * S::kTok, w.len)) mend(G, a2, delta[(S::kTok - 1) * S::kGroups + mine]);
-        Quad s = {0, 0};
 #pragma unroll 4
         for (int t = S::kTok - 1; t >= 0; --t) {
             const float4 d = delta[t * S::kGroups + mine], g = dout[t * S::kGroups + mine];
             const Quad C = quad(cs[t * S::P + p]);
+            passed.add(quad(d));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const Quad v = fma4(both(at(g, i)), C, G[i]);
                 const f32x2 di = both(at(d, i));
-                G[i] = {mul2(decay(di, a2[i].lo), v.lo), mul2(decay(di, a2[i].hi), v.hi)};
+                const Quad decays = {decay(di, a2[i].lo), decay(di, a2[i].hi)};
+                G[i] = mul4(decays, fma4(both(at(g, i)), C, G[i]));
+                passed.product[i] = mul4(decays, passed.product[i]);
             }
-            s = {add2(s.lo, quad(d).lo), add2(s.hi, quad(d).hi)};
         }
-        sum = {add2(sum.lo, s.lo), add2(sum.hi, s.hi)};
+        if (tile * S::kTok % kPeriod == 0 || tile == w.first) {
+            put_right(G, a2, passed);
+            minus = {add2(minus.lo, passed.minus.lo), add2(minus.hi, passed.minus.hi)};
+            passed.clear();
+        }
         __syncthreads();
     }
     w.store_states(G, a.end_state + w.state(a, end));
-    if (w.on && p == 0) *reinterpret_cast<float4 *>(a.end_delta + end * a.D + w.c) = unquad(sum);
+    if (w.on && p == 0) *reinterpret_cast<float4 *>(a.end_delta + end * a.D + w.c) = unquad(mul4(both(-1.f), minus));
 }
 
 constexpr int kWide = 64;       // channels of a block of the main kernel
@@ -116,7 +122,7 @@ struct Shared {
         };
         float col[kThreads][8];             // at the end: threads' sums of dskip and dbias
     };
-    Quad mid[kTile / kRun][4][kThreads];    // states at the runs' starts
+    Quad mid[kTile / kRun][4][kThreads];    // states at the runs' starts; the last run's place then holds the decays' product
 };
 
 // Four states of four channels; index j is state j ^ q.
@@ -290,7 +296,6 @@ __global__ void __launch_bounds__(4 * N) k_backward(Args<T> a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) asm volatile("prefetch.global.L2 [%0];" ::"l"(saved - (int64_t)a.D * N + i * N));
         }
-        if (mend_at(t0 + kTile, len)) mend(G.v, a2.v, s.delta[kTile - 1][mine]);
         // The states at the runs' starts.
 #pragma unroll 1
         for (int run = 0; run < kTile / kRun; ++run) {
@@ -324,7 +329,9 @@ __global__ void __launch_bounds__(4 * N) k_backward(Args<T> a) {
                     if (kGate) rz[k].load(z + (int64_t)to * a.z_l);
                 }
             }
-            // The run's states.
+            // The run's states, and its decays' product.
+            Passed passed;
+            passed.clear();
             States hs[kRun];
 #pragma unroll
             for (int i = 0; i < kRun; ++i) {
@@ -333,12 +340,19 @@ __global__ void __launch_bounds__(4 * N) k_backward(Args<T> a) {
                 const Quad B = in_order(brow + t * P, half);
                 const Quad w[4] = {mul4(both(v.x), B), mul4(both(v.y), B), mul4(both(v.z), B), mul4(both(v.w), B)};
                 hs[i] = i ? hs[i ? i - 1 : 0] : h0;
-                advance(hs[i].v, a2.v, d, w);
+                advance(hs[i].v, a2.v, d, w, passed);
                 if (kGate) {
                     const Quad C = in_order(crow + t * P, half);
                     s.o[i][share] = make_float4(dot4(C, hs[i].v[0]), dot4(C, hs[i].v[1]), dot4(C, hs[i].v[2]), dot4(C, hs[i].v[3]));
                 }
             }
+            Quad(&product)[4][kThreads] = s.mid[kTile / kRun - 1];          // (the last run has taken its states from there)
+            if (run < kTile / kRun - 1) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) passed.product[j] = mul4(product[j][tid], passed.product[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) product[j][tid] = passed.product[j];
             // The gradient, token by token backwards.
 #pragma unroll
             for (int i = kRun - 1; i >= 0; --i) {
@@ -406,6 +420,16 @@ __global__ void __launch_bounds__(4 * N) k_backward(Args<T> a) {
             }
             __syncthreads();
         }
+        // After every tile: there is no room for the product over a longer time (in a place of its own it costs N = 8 a block
+        // of the SM's 7).
+        Passed passed;
+        passed.clear();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) passed.product[j] = s.mid[kTile / kRun - 1][j][tid];
+#pragma unroll
+        for (int t = 0; t < kTile; ++t) passed.add(quad(s.delta[t][mine]));
+        put_right(G.v, a2.v, passed);
+        __syncthreads();            // (the next tile's D)
     }
     const int64_t part = (int64_t)bi * a.nseg + seg;
     if (on) {

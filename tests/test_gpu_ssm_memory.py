@@ -1,10 +1,11 @@
-"""The selective scan's long memory: states that overflow, states that stay zero under growing decays."""
+"""The selective scan's long memory: states that overflow, states that stay zero under growing decays, steps of which only some
+are open, and lengths and widths about the kernels' tiles and blocks."""
 import math
 
 import pytest
 
 import _ssm_ref as ref
-from test_gpu_ssm import gen
+from test_gpu_ssm import check, gen, inputs
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -73,3 +74,76 @@ def test_zero_states_under_growing_decays(L, N):
     ref.assert_within(out[0][:, start], want["dx"], "dx")
     for t in out[:3]:
         assert not t[:, n:].any()
+
+
+# Which of a sequence's tokens move the states (place in 32, steps about).
+PATTERNS = {"all": (lambda t: t >= 0, 0.005), "only the 16th": (lambda t: t % 32 == 16, 0.005), "only the 15th": (lambda t: t % 32 == 15, 0.005),
+            "all but the 16th": (lambda t: t % 32 != 16, 0.005), "all but the 15th": (lambda t: t % 32 != 15, 0.005),
+            "only the first of 64": (lambda t: t % 64 == 0, 0.005), "every other 16": (lambda t: t // 16 % 2 == 0, 0.005),
+            "0 to 0.02": (None, 0.01), "all, slowly": (lambda t: t >= 0, 0.0003), "all, fast": (lambda t: t >= 0, 0.05)}
+
+
+@pytest.mark.parametrize("N,rows", [(8, 1), (8, 300), (32, 1), (32, 76)])
+def test_steps_that_depend_on_their_place(N, rows):
+    """States and gradients that only grow, with most of the steps 0 or not: the mean errors of the final state, of the initial
+    state's gradient and of dA, per pattern.  One row runs in segments; with enough empty rows beside it a block walks all of it.
+
+    Over a tile (16 tokens) that moves the states at all, what is carried takes e^(A sum of D), off in the mean by 8e-9 of itself
+    at most; a state remembers 1 / E such tiles, E the mean of what they forget, and no more than there are.  What enters is off
+    once by the exponentials' means (3.1e-8 each at most) over the tokens between corrections, 32.  Single roundings (three of
+    at most 2^-24 a token) cancel over a pattern's channels and states but for their root."""
+    B, L, per = 1, 8192, 24
+    g = gen(N)
+    rand = lambda *s: torch.rand(*s, generator=g, device="cuda")  # noqa: E731
+    t = torch.arange(L, device="cuda")
+    D = per * len(PATTERNS)
+    dt = torch.empty(B, L, D, device="cuda")
+    for k, (fn, step) in enumerate(PATTERNS.values()):
+        r = rand(B, L, per)
+        dt[..., k * per:(k + 1) * per] = 0.02 * r if fn is None else step * (0.8 + 0.4 * r) * fn(t)[None, :, None]
+    x, b, c, dy = 0.5 + rand(B, L, D), 0.5 + rand(B, L, N), 0.5 + rand(B, L, N), 0.5 + rand(B, L, D)
+    A, dh = -torch.ones(D, N, device="cuda"), 0.5 + rand(B, D, N)
+    par = rlm.SsmParams(A, softplus=False)
+    lengths = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    lengths[0] = L
+    ix, idt, ib, ic, idy = (v.expand(rows, -1, -1) for v in (x, dt, b, c, dy))
+    y, state, saved = torch.empty(rows, L, D, device="cuda"), torch.empty(rows, D, N, device="cuda"), rlm.ssm_saved(rows, L, D, N)
+    assert (rlm.rlm_ssm_workspace_size(rows, L, D, N) == 0) == (rows > 1)
+    rlm.rlm_ssm_prefill(ix, idt, ib, ic, par, y, state_out=state, saved=saved, lengths=lengths)
+    out = [torch.empty_like(y) for _ in range(2)] + [torch.empty(rows, L, N, device="cuda") for _ in range(2)]
+    dh0, gr = torch.empty_like(state), rlm.SsmGrads.empty(D, N)
+    rlm.rlm_ssm_backward(idy, ix, idt, ib, ic, par, saved, *out, gr, d_state_out=dh.expand(rows, -1, -1).contiguous(), d_state_in=dh0,
+                         lengths=lengths)
+    h, before = torch.zeros(B, D, N, dtype=torch.float64, device="cuda"), torch.empty(L, B, D, N, dtype=torch.float64, device="cuda")
+    for i in range(L):
+        before[i] = h
+        d = dt[:, i, :, None].double()
+        h = torch.exp(-d) * h + d * x[:, i, :, None].double() * b[:, i, None, :].double()
+    G, dA = dh.double(), torch.zeros(D, N, dtype=torch.float64, device="cuda")
+    for i in range(L - 1, -1, -1):
+        d = dt[:, i, :, None].double()
+        G = torch.exp(-d) * (G + dy[:, i, :, None].double() * c[:, i, None, :].double())
+        dA += (G * d * before[i]).sum(0)
+    far = []
+    for k, name in enumerate(PATTERNS):
+        at = slice(k * per, (k + 1) * per)
+        tiles = dt[..., at].double().view(B, L // 16, 16, per).sum(2)
+        live = (tiles > 0).double().mean().item() * (L // 16)
+        forget = tiles.sum(1).mean().item() / live               # of a tile that moves the states
+        n = min(1 / -math.expm1(-forget), live)                 # tiles remembered
+        tokens = n * (dt[..., at] > 0).sum().item() / per / live
+        one = 8e-9 * n + 32 * 3.1e-8 + 9 * 2.0 ** -24 * math.sqrt(tokens / (per * N))
+        for what, got, want, bound in (("state", state[:1, at], h[:, at], one), ("dh0", dh0[:1, at], G[:, at], one), ("dA", gr.A[at], dA[at], 2 * one)):
+            e = (got / want - 1).mean().item()
+            if not abs(e) <= bound:
+                far.append((name, what, e, bound))
+    assert not far, far
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [8, 16, 32])
+@pytest.mark.parametrize("L,D", [(8, 56), (9, 64), (15, 72), (16, 64), (17, 120), (31, 128), (32, 136), (33, 56), (47, 256), (48, 264), (49, 128)])
+def test_lengths_and_widths_about_tiles_and_blocks(L, D, N, dtype):
+    """Tiles are of 16 tokens (of 8 in the forward pass at N = 8), states are put right every 32, a forward block has 1024 / N
+    channels and a gradient's 64."""
+    check(inputs(2, L, D, N, dtype, gen(L), view=L % 2 == 1), gate=L % 3 != 0)
