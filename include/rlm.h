@@ -426,7 +426,8 @@ RLM_API size_t rlm_linear_backward_workspace_size(int64_t R, int64_t K, int64_t 
  *   state_out nullable; the K - 1 inputs before the token that would come next (may be state_in itself)
  *   lengths   nullable, as for the recurrence: x is not read from there on, y is 0, and state_out is
  *             what row b's last real token leaves
- * With K = 1 there are no states (both NULL, or of K = 1).  One kernel, no workspace. */
+ * With K = 1 there are no states (both NULL, or of K = 1).  One kernel, no workspace.
+ * Sums are fp32.  The sigmoid (here and in the scan's gate) is off by (|v| + 8) 2^-24 of itself, 0 below 2^-126. */
 RLM_API rlm_status rlm_conv_prefill(const rlm_strided *x, const float *conv_w, const float *bias, int K, rlm_act act,
                                     const rlm_conv_state *state_in, const rlm_strided *y, rlm_conv_state *state_out,
                                     const int32_t *lengths, const rlm_launch *launch);
@@ -486,7 +487,8 @@ RLM_API size_t rlm_ssm_saved_size(int64_t B, int64_t L, int D, int N);
 /* Gradients of a scalar loss given dy = dl/dy and (nullable) d_state_out, with the inputs and `saved` of the
  * forward pass.  dx, ddt, dz (with z) [B][L][D], db and dc [B][L][N], the inputs' dtype, are overwritten (0 in
  * padding); d_state_in is a nullable output, and may be d_state_out itself.  Sums over channels, batch and time are
- * fp32 in an order fixed by the shape.  Workspace: rlm_ssm_backward_workspace_size. */
+ * fp32 in an order fixed by the shape.  Workspace: rlm_ssm_backward_workspace_size, most of it B L 2 N ceil(D / 64) floats, the
+ * shares of db and dc of 64 channels each. */
 RLM_API rlm_status rlm_ssm_backward(const rlm_strided *dy, const rlm_strided *x, const rlm_strided *dt, const rlm_strided *b,
                                     const rlm_strided *c, const rlm_strided *z, const rlm_ssm_params *params,
                                     const float *saved, const float *d_state_out, const rlm_strided *dx,
@@ -548,7 +550,8 @@ RLM_API rlm_status rlm_logprob(const rlm_matrix *logits, const rlm_tokens *targe
  *   dz_j = d_logprob ([j = target] - p_j) - d_entropy p_j (log p_j + H)
  *   stats      as rlm_logprob left it;  entropy, d_entropy  nullable, both or neither
  *   dlogits    [R][V] RLM_BF16 or RLM_F32; may be the logits themselves (same ptr, dtype and ld)
- * A row whose factors are 0 (or whose target is outside 0 .. V - 1, with no d_entropy) is 0, its logits unread. */
+ * A row whose factors are 0 (or whose target is outside 0 .. V - 1, with no d_entropy) is 0, its logits unread.
+ * p_j is e^(log p_j) by the special-function unit: off by (|log p_j| + 10) 2^-24 of itself, and 0 below 2^-126. */
 RLM_API rlm_status rlm_logprob_backward(const rlm_matrix *logits, const rlm_tokens *targets, const float *stats,
                                         const float *d_logprob, const float *entropy, const float *d_entropy,
                                         const rlm_matrix *dlogits, const rlm_launch *launch);

@@ -31,10 +31,15 @@
 //   1216 rows of 2000       5.0 / 15.1    3.6 / 10.1        19456 rows of 1100   58.6 / 208.5    18.4 / 54.4
 //   1216 rows of 8000       6.6 / 20.1    8.7 / 25.1         2432 rows of 8000   12.0 / 38.0     14.6 / 28.1
 //   4864 rows of 4000      17.2 / 66.8   14.5 / 35.9        19456 rows of 8000    108 / 297       103 / 167
-// so up to 4096 logits from 8 rows an SM on, up to 8192 from 16 rows on, and always up to 1024.  In registers, without tiles, a
+// so up to 4096 logits from 8 rows an SM on, up to 8192 from 16 rows on, and always up to 1024.  (The rule does not ask for
+// alternatives: 2432 rows of 8000 without any would be faster by blocks.)  In registers, without tiles, a
 // row of up to 500 goes faster (19456 of 300: 7.9 / 31 us, in tiles 9.6 / 36; of 520 15.1 / 68 and 12.3 / 41).
+// A single alternative is the first value equal to the maximum (67108 rows of 1000: 79 us -> 66; the branch
+// costs those with 32 alternatives 190 -> 198).
 //
-// Bound by memory: the logits are read once, by the gradient once more.
+// Bound by memory: the logits are read once, by the gradient once more.  Registers are bounded for the blocks of an SM; three
+// instances spill 4 to 16 bytes for it (bf16: the block form with alternatives, 64 registers, the gradient with
+// entropy, 80).
 #include <algorithm>
 #include <type_traits>
 

@@ -10,8 +10,8 @@
 // and D x of 4 channels and B and C of 4 states, 64 bytes out of shared memory, serve 16 states.  (Shared
 // memory gives a warp 128 bytes a clock: with one channel a thread, 48 bytes for 4 states, it bounded the
 // kernel, 138 us against 36 of arithmetic at B = 4, L = 4096, D = 1024, N = 16.)  A block is 64 threads, 64 / P
-// groups of channels, and walks tiles of 4 P tokens: 4 groups of 4 channels a thread and field.  They are
-// loaded one tile ahead, D and D x formed in fp32 and left in shared memory.
+// groups of channels, and walks tiles of 4 P tokens, 16 at most: 4 groups of 4 channels a thread and field, 2 at N = 32.  They
+// are loaded one tile ahead, D and D x formed in fp32 and left in shared memory.
 #pragma once
 
 #include "rlm_device.cuh"
